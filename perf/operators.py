@@ -250,10 +250,10 @@ def _logprob(c, s):
     d = z - m
     e = torch.exp(d)
     total = e.sum(1, keepdim=True)
-    lse = m + torch.log(total)
-    out = {"lse": lse[:, 0],
-           "logp": (z.gather(1, s["target"].long()[:, None]) - lse)[:, 0],
-           "entropy": (torch.log(total) - (e * d).sum(1, keepdim=True) / total)[:, 0]}
+    ln = torch.log(total)
+    out = {"stats": torch.cat([m, ln], 1),
+           "logp": (z.gather(1, s["target"].long()[:, None]) - m - ln)[:, 0],
+           "entropy": (ln - (e * d).sum(1, keepdim=True) / total)[:, 0]}
     if k:
         left, at = z.clone(), torch.arange(v, device=z.device)
         top, index = [], []
@@ -261,11 +261,12 @@ def _logprob(c, s):
             best = left.amax(1, keepdim=True)
             i = torch.where(left == best, at, v).amin(1, keepdim=True)
             left.scatter_(1, i, float("-inf"))
-            top.append(best - lse)
+            top.append(best - m - ln)
             index.append(i)
         out["top_logp"], out["top_index"] = torch.cat(top, 1), torch.cat(index, 1).int()
     if c["train"]:
-        p, lp = torch.exp(z - lse), z - lse
+        lp = d - ln
+        p = torch.exp(lp)
         g = s["g_logp"][:, None]
         grad = -p * (g + s["g_top"].sum(1, keepdim=True))
         grad -= s["g_entropy"][:, None] * p * (lp + out["entropy"][:, None])
@@ -345,19 +346,19 @@ def _calls(s):
     z, rows, v, k = s["z"], c["rows"], c["v"], c["k"]
     ld = z.stride(0)
     f, dz, index, ws = _buffers(s, lambda: (
-        torch.empty(3 * rows + rows * k, device="cuda"),
+        torch.empty(4 * rows + rows * k, device="cuda"),
         torch.empty(rows, ld, dtype=z.dtype, device="cuda") if c["train"] else None,
         torch.empty(rows, k, dtype=torch.int32, device="cuda"),
         torch.empty(mx.mpx_logprob_workspace(rows, v, k), dtype=torch.uint8, device="cuda")))
-    logp, entropy, lse, top = f[:rows], f[rows:2 * rows], f[2 * rows:3 * rows], f[3 * rows:]
+    logp, entropy, stats, top = f[:rows], f[rows:2 * rows], f[2 * rows:4 * rows], f[4 * rows:]
     mx.mpx_logprob_fwd(z.data_ptr(), ld, s["target"].data_ptr(), rows, v, k, logp.data_ptr(),
-                       entropy.data_ptr(), lse.data_ptr(), top.data_ptr() if k else None,
+                       entropy.data_ptr(), stats.data_ptr(), top.data_ptr() if k else None,
                        index.data_ptr() if k else None, dt, ws.data_ptr(), ws.numel(), stream)
-    out = {"lse": lse, "logp": logp, "entropy": entropy}
+    out = {"stats": stats.view(rows, 2), "logp": logp, "entropy": entropy}
     if k:
         out["top_logp"], out["top_index"] = top.view(rows, k), index
     if c["train"]:
-        mx.mpx_logprob_bwd(z.data_ptr(), ld, s["target"].data_ptr(), rows, v, k, lse.data_ptr(),
+        mx.mpx_logprob_bwd(z.data_ptr(), ld, s["target"].data_ptr(), rows, v, k, stats.data_ptr(),
                            entropy.data_ptr(), index.data_ptr() if k else None,
                            s["g_logp"].data_ptr(), s["g_entropy"].data_ptr(),
                            s["g_top"].data_ptr() if k else None, s["state"].data_ptr(),
@@ -388,7 +389,7 @@ def work(case):
                 "flops": 3 * c["rows"] * c["rot"] * c["hd"]}
     rows, v, k = c["rows"], c["v"], c["k"]
     passes = 3 if c["train"] else 1  # the gradient reads the logits again and writes as much
-    return {"bytes": passes * b * rows * v + rows * (16 + 8 * k), "flops": (14 if c["train"] else 6) * rows * v}
+    return {"bytes": passes * b * rows * v + rows * (20 + 8 * k), "flops": (14 if c["train"] else 6) * rows * v}
 
 
 # ------------------------------------------------------------ in 64 bits --
@@ -437,7 +438,7 @@ def _exact_rope(c, x, pos):
 
 def _exact_logprob(c, s):
     rows, k = c["rows"], c["k"]
-    keys = ["entropy", "logp", "lse"] + (["top_logp"] if k else []) + (["dz"] if c["train"] else [])
+    keys = ["entropy", "logp", "stats"] + (["top_logp"] if k else []) + (["dz"] if c["train"] else [])
     parts = {key: [] for key in keys}
     for r in range(0, rows, 256):
         z = s["z"][r:r + 256].double()
@@ -445,7 +446,8 @@ def _exact_logprob(c, s):
         p, t = lp.exp(), s["target"][r:r + 256].long()
         at = torch.arange(z.shape[0], device=z.device)
         h = -torch.xlogy(p, p).sum(1)
-        parts["lse"].append(torch.logsumexp(z, 1))
+        big = z.max(dim=1).values
+        parts["stats"].append(torch.stack([big, torch.log(torch.exp(z - big[:, None]).sum(1))], 1))
         parts["logp"].append(lp[at, t])
         parts["entropy"].append(h)
         if k:
