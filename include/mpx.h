@@ -251,6 +251,97 @@ int mpx_gemm_batched(int32_t trans_a, int32_t trans_b, int64_t M, int64_t N, int
  * Errors: MPX_ERR_INVALID for a value outside [0, 11]. */
 int mpx_gemm_set_config(int32_t config);
 
+/* ---- Activation checkpoints in 8 bits ----
+ *
+ * The activations a layer keeps for its backward pass, in half the memory of
+ * the half formats (MPX §2.1 keeps forward activations in half precision): one
+ * e4m3 code per value (1 sign, 4 exponent, 3 mantissa bits; magnitudes up to
+ * 448, no infinities) and one power-of-two scale for every MPX_ACT8_GROUP
+ * consecutive rows of a column:
+ *   codes  [M, K] bytes, row-major, dense;
+ *   scales [ceil(M / 32), K] bytes: biased exponents, a scale is 2^(byte - 127).
+ * For a group with largest finite magnitude a, the exponent e is the smallest
+ * one with a <= 448 * 2^e, not below -15 (float16) or -117 (bfloat16), where
+ * the code's smallest step is the half format's own smallest (bfloat16:
+ * smallest normal) value.  code = e4m3(x / 2^e), rounded to nearest even; a
+ * code of 256 at e = 8 (float16) or 120 (bfloat16), infinite once widened, is
+ * held as 240.  A checkpoint's value 2^e * code is so always exactly a value
+ * of the half format, within 2^-4 |x| of x, or within 2^-10 2^e where |x| is
+ * below 2^-6 2^e.
+ * +-inf and NaN are held as NaN and leave the other values of their group
+ * alone, so an overflowing step still shows in the gradients' finite check.
+ * dt is MPX_F16 or MPX_BF16 and the same for packing and use; a checkpoint of
+ * a strided batch of rows has its groups from its own first row on. */
+#define MPX_ACT8_GROUP 32
+
+/* codes, scales = checkpoint of X [M, K] half with row stride ldx (elements,
+ * >= K).  M, K >= 1; any alignment. */
+int mpx_act8_pack(const void* X, int64_t ldx, uint8_t* codes, uint8_t* scales, int64_t M, int64_t K,
+                  mpx_dtype dt, void* stream);
+
+/* Y [M, K] half (row stride ldy >= K) = the checkpoint's values, exact.
+ * Columns past K of a strided Y are left as they are. */
+int mpx_act8_unpack(const uint8_t* codes, const uint8_t* scales, void* Y, int64_t ldy, int64_t M,
+                    int64_t K, mpx_dtype dt, void* stream);
+
+/* mpx_linear_bwd with the layer's kept activations as checkpoints: with X and
+ * P the values of (Xc, Xs) and (Pc, Ps),
+ *   dX = half(dY W), or half(half(dY W) * gelu'(P)) when x_act ==
+ *        MPX_ACT_GELU_TANH (the layer's input was gelu(P); its checkpoint is
+ *        (Xc, Xs));
+ *   dW = half(dY^T X);  db = half(sum_m dY[m,:]).
+ * Shapes, subsets (dX, dW, db may be NULL, not all), d_nonfinite and errors as
+ * mpx_linear_bwd; Xc and Xs are needed for dW only, Pc and Ps for dX through
+ * GELU only.  dt == MPX_F16 or MPX_BF16.  Whatever overlaps needs its own
+ * workspace (device, mpx_linear_bwd_act8_workspace(M, N, K) bytes when dW or
+ * db is requested or x_act is set for dX, else it may be NULL).  That size
+ * never falls as M grows. */
+int mpx_linear_bwd_act8(const uint8_t* Xc, const uint8_t* Xs, const void* W, const void* dY,
+                        const uint8_t* Pc, const uint8_t* Ps, int32_t x_act, void* dX, void* dW,
+                        void* db, int64_t M, int64_t N, int64_t K, mpx_dtype dt, void* workspace,
+                        size_t ws_bytes, int32_t* d_nonfinite, void* stream);
+size_t mpx_linear_bwd_act8_workspace(int64_t M, int64_t N, int64_t K);
+
+/* ---- Rotary positions with several axes ----
+ *
+ * Queries and keys turned by their tokens' positions (time, height, width, ...)
+ * before attention.  A head's hd values hold, from its first one on, axes[0],
+ * axes[1], ... sections of 2 * pairs[a] values; values behind the last section
+ * pass unturned.  Pair i of axis a, at values (i, pairs[a] + i) of the section,
+ * or (2 i, 2 i + 1) when interleaved, turns by the angle
+ *   pos[r % pos_rows, a] * base[a]^(-i / pairs[a])   radians:
+ *   y0 = x0 cos - x1 sin,  y1 = x1 cos + x0 sin.
+ * Angles are taken in float64 and reduced to less than one turn before they
+ * are rounded, so positions far out lose nothing; the turn is computed in
+ * float32 and rounded once.  A position of 0 leaves its values as they are. */
+#define MPX_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t axes;                       /* 1 .. MPX_ROPE_MAX_AXES */
+  int32_t pairs[MPX_ROPE_MAX_AXES];   /* pairs of values turned by each axis, >= 1 */
+  double base[MPX_ROPE_MAX_AXES];     /* > 1, finite */
+  int32_t interleaved;                /* 0 or 1 */
+} mpx_rope_plan;
+
+/* Y[r, h, :] = turn(X[r, h, :]) for the first heads_rot heads of every row and
+ * Y = X for the heads_copy heads behind them (the values V of a QKV output).
+ * X [rows, (heads_rot + heads_copy) * hd] with row stride ldx, Y likewise with
+ * ldy (elements); Y == X with ldy == ldx turns in place, where the copied
+ * heads are not touched; any other overlap is not allowed.  pos: device
+ * float32 [pos_rows, axes], rows a multiple of pos_rows (whole numbers are
+ * exact up to 2^24; a position that is not finite makes its values NaN).  plan
+ * is a host pointer, read during the call.  rows, heads_rot, pos_rows >= 1,
+ * heads_copy >= 0, 2 <= hd <= 512, 2 * sum(pairs) <= hd.  dt: MPX_F16,
+ * MPX_BF16 or MPX_F32; pointers aligned to their element. */
+int mpx_rope_fwd(const void* X, int64_t ldx, void* Y, int64_t ldy, const float* pos,
+                 int64_t pos_rows, int64_t rows, int64_t heads_rot, int64_t heads_copy, int64_t hd,
+                 const mpx_rope_plan* plan, mpx_dtype dt, void* stream);
+
+/* Backward: dX from dY, the turn by the opposite angle (the copied heads'
+ * cotangents are copied).  Arguments as mpx_rope_fwd, with dY in X's place. */
+int mpx_rope_bwd(const void* dY, int64_t ldy, void* dX, int64_t ldx, const float* pos,
+                 int64_t pos_rows, int64_t rows, int64_t heads_rot, int64_t heads_copy, int64_t hd,
+                 const mpx_rope_plan* plan, mpx_dtype dt, void* stream);
+
 /* Fused multi-head self-attention core (MPX §2.1 half products with float32
  * accumulation; §3.2 softmax and its backward in full precision), one pass
  * each way:
@@ -341,6 +432,53 @@ size_t mpx_loss_workspace(int64_t n);
 int mpx_cross_entropy(const void* Z, int64_t ldz, const int32_t* labels, int64_t B,
                       int64_t C, const mpx_scale_state* d_state, float* d_loss, void* dZ,
                       mpx_dtype dt, void* workspace, size_t ws_bytes, void* stream);
+
+/* Log probabilities of given tokens, with the distribution's entropy and its
+ * top alternatives, one pass over the logits Z [rows, V] (row stride ldz >= V)
+ * in float32 (MPX §3.2), per row r:
+ *   stats[r] = (m, ln S),  m = max_j z_j,  S = sum_j e^(z_j - m)  (m + ln S is
+ *       the logsumexp; apart, they stay exact where m is large);
+ *   logp = (z[targets[r]] - m) - ln S;
+ *   entropy = ln S - sum_j e^(z_j - m) (z_j - m) / S;
+ *   top_logp[r, i], top_idx[r, i]: the k largest log probabilities in falling
+ *   order and their columns, equal ones by the lower column.
+ * targets (int32 [rows]): a negative one means that the row has no target (logp
+ * 0, and no gradient from g_logp below), one of V or more gives NaN (never an
+ * out-of-range read).  Any of logp (with targets), entropy, stats ([rows, 2])
+ * and the pair top_logp / top_idx (with k >= 1) may be NULL, not all; all are
+ * float32 but top_idx (int32).  0 <= k <= MPX_LOGPROB_MAX_K, k <= V < 2^31; rows >= 1.
+ * Logits of -inf (masked ones) have probability 0 and add nothing; a row of
+ * nothing else has stats (-inf, 0), logp and top_logp -inf, entropy 0 and
+ * top_idx 0 .. k-1.  A NaN or +inf logit makes the row's float results NaN
+ * (top_idx then lists NaN before +inf before the rest).  The padding columns V .. ldz-1
+ * are never read.  Results do not depend on what else runs (no atomics).
+ * workspace: mpx_logprob_workspace(rows, V, k) bytes (device; may be NULL when
+ * that is 0), not shared by calls that overlap.  dt: MPX_F16, MPX_BF16 or
+ * MPX_F32; pointers aligned to their element. */
+#define MPX_LOGPROB_MAX_K 16
+int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t rows, int64_t V,
+                    int32_t k, float* logp, float* entropy, float* stats, float* top_logp,
+                    int32_t* top_idx, mpx_dtype dt, void* workspace, size_t ws_bytes, void* stream);
+size_t mpx_logprob_workspace(int64_t rows, int64_t V, int32_t k);
+
+/* The gradient of the calls' results at the logits, for any upstream
+ * cotangents (float32; each nullable, not all): g_logp [rows] (with targets),
+ * g_entropy [rows] (with entropy), g_top [rows, k] (with top_idx):
+ *   dZ_j = half(scale * (g_logp ([j == target] - p_j)
+ *               - g_entropy p_j (ln p_j + entropy)
+ *               + sum_i g_top_i ([j == top_idx_i] - p_j))),  p_j = e^((z_j - m) - ln S),
+ * scale = d_state->scale (d_state NULL: 1).  stats, entropy and top_idx are
+ * the forward's.  dZ [rows, V] with row stride ldo >= V; dZ == Z with ldo == ldz
+ * writes the gradient over the logits, any other overlap is not allowed.
+ * Padding columns are left as they are.  Masked logits get a gradient of 0, and
+ * so does every logit of a row of nothing but masked ones; a row whose stats
+ * are NaN gets NaN.  A target of V or more gives a NaN row, a top_idx outside
+ * [0, V) is NaN likewise. */
+int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t rows, int64_t V,
+                    int32_t k, const float* stats, const float* entropy, const int32_t* top_idx,
+                    const float* g_logp, const float* g_entropy, const float* g_top,
+                    const mpx_scale_state* d_state, void* dZ, int64_t ldo, mpx_dtype dt,
+                    void* stream);
 
 /* Workspace (bytes) of mpx_classifier_head for B rows of width d: the row
  * losses and one pair of float32 gamma / beta partial rows per 4 rows,

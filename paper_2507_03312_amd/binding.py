@@ -17,6 +17,9 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmpx.so"
 
 MPX_F32, MPX_F16, MPX_BF16 = 0, 1, 2
 MPX_ACT_NONE, MPX_ACT_GELU_TANH = 0, 1
+MPX_ACT8_GROUP = 32        # rows of a column that share a checkpoint's scale
+MPX_ROPE_MAX_AXES = 4
+MPX_LOGPROB_MAX_K = 16
 DTYPES = {"f32": MPX_F32, "f16": MPX_F16, "bf16": MPX_BF16}
 
 
@@ -32,6 +35,24 @@ class ScaleState(C.Structure):
 class AdamWHP(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
                 ("eps", C.c_double), ("weight_decay", C.c_double)]
+
+
+class RopePlan(C.Structure):
+    """``mpx_rope_plan``: ``RopePlan([16, 24, 24])`` turns 16, 24 and 24 pairs of
+    each head by a token's three positions."""
+    _fields_ = [("axes", C.c_int32), ("pairs", C.c_int32 * 4), ("base", C.c_double * 4),
+                ("interleaved", C.c_int32)]
+
+    def __init__(self, pairs, base=10000.0, interleaved=False):
+        """base: one for every axis, or a sequence of one per axis."""
+        pairs = list(pairs)
+        if not 1 <= len(pairs) <= MPX_ROPE_MAX_AXES:
+            raise ValueError(f"1 to {MPX_ROPE_MAX_AXES} axes")
+        bases = [float(base)] * len(pairs) if isinstance(base, (int, float)) else list(base)
+        if len(bases) != len(pairs):
+            raise ValueError("one base, or one per axis")
+        super().__init__(len(pairs), (C.c_int32 * 4)(*pairs), (C.c_double * 4)(*bases),
+                         int(bool(interleaved)))
 
 
 def _load():
@@ -65,6 +86,12 @@ _SIGS = {
     "mpx_gemm_batched": (C.c_int, [I32, I32, I64, I64, I64, I64, I64, P, I64, I64, I64, P, I64,
                                    I64, I64, P, I64, I64, I64, I32, P]),
     "mpx_gemm_set_config": (C.c_int, [I32]),
+    "mpx_act8_pack": (C.c_int, [P, I64, P, P, I64, I64, I32, P]),
+    "mpx_act8_unpack": (C.c_int, [P, P, P, I64, I64, I64, I32, P]),
+    "mpx_linear_bwd_act8": (C.c_int, [P, P, P, P, P, P, I32, P, P, P, I64, I64, I64, I32, P, SZ, P, P]),
+    "mpx_linear_bwd_act8_workspace": (SZ, [I64, I64, I64]),
+    "mpx_rope_fwd": (C.c_int, [P, I64, P, I64, P, I64, I64, I64, I64, I64, C.POINTER(RopePlan), I32, P]),
+    "mpx_rope_bwd": (C.c_int, [P, I64, P, I64, P, I64, I64, I64, I64, I64, C.POINTER(RopePlan), I32, P]),
     "mpx_attention_fwd": (C.c_int, [P, P, P, I64, I64, I64, I64, I32, P]),
     "mpx_attention_bwd": (C.c_int, [P, P, P, P, I64, I64, I64, I64, I32, P, SZ, P]),
     "mpx_attention_bwd_workspace": (SZ, [I64, I64, I64, I64]),
@@ -77,6 +104,9 @@ _SIGS = {
     "mpx_loss_workspace": (SZ, [I64]),
     "mpx_cross_entropy": (C.c_int, [P, I64, P, I64, I64, P, P, P, I32, P, SZ, P]),
     "mpx_mse": (C.c_int, [P, P, I64, P, P, P, I32, P, SZ, P]),
+    "mpx_logprob_fwd": (C.c_int, [P, I64, P, I64, I64, I32, P, P, P, P, P, I32, P, SZ, P]),
+    "mpx_logprob_workspace": (SZ, [I64, I64, I32]),
+    "mpx_logprob_bwd": (C.c_int, [P, I64, P, I64, I64, I32, P, P, P, P, P, P, P, P, I64, I32, P]),
     "mpx_classifier_head_workspace": (SZ, [I64, I64]),
     "mpx_classifier_head": (C.c_int, [P, I64, P, P, P, P, P, I64, I64, I64, P, P, P, P, P, I64, P, P,
                                       I32, P, SZ, P, P]),
@@ -175,6 +205,11 @@ mpx_linear_bwd_noalloc = _call("mpx_linear_bwd_noalloc")
 MPX_LINEAR_BWD_NOALLOC_SCRATCH = 64 << 20   # bytes (include/mpx.h)
 mpx_gemm_batched = _call("mpx_gemm_batched")
 mpx_gemm_set_config = _call("mpx_gemm_set_config")
+mpx_act8_pack = _call("mpx_act8_pack")
+mpx_act8_unpack = _call("mpx_act8_unpack")
+mpx_linear_bwd_act8 = _call("mpx_linear_bwd_act8")
+mpx_rope_fwd = _call("mpx_rope_fwd")
+mpx_rope_bwd = _call("mpx_rope_bwd")
 mpx_attention_fwd = _call("mpx_attention_fwd")
 mpx_attention_bwd = _call("mpx_attention_bwd")
 mpx_layernorm_fwd = _call("mpx_layernorm_fwd")
@@ -184,6 +219,8 @@ mpx_softmax_fwd = _call("mpx_softmax_fwd")
 mpx_softmax_bwd = _call("mpx_softmax_bwd")
 mpx_cross_entropy = _call("mpx_cross_entropy")
 mpx_mse = _call("mpx_mse")
+mpx_logprob_fwd = _call("mpx_logprob_fwd")
+mpx_logprob_bwd = _call("mpx_logprob_bwd")
 mpx_classifier_head = _call("mpx_classifier_head")
 mpx_patchify_cast = _call("mpx_patchify_cast")
 mpx_embed_assemble = _call("mpx_embed_assemble")
@@ -194,6 +231,14 @@ mpx_zero = _call("mpx_zero")
 
 def mpx_linear_bwd_workspace(M: int, N: int, K: int) -> int:
     return int(lib.mpx_linear_bwd_workspace(M, N, K))
+
+
+def mpx_linear_bwd_act8_workspace(M: int, N: int, K: int) -> int:
+    return int(lib.mpx_linear_bwd_act8_workspace(M, N, K))
+
+
+def mpx_logprob_workspace(rows: int, V: int, k: int) -> int:
+    return int(lib.mpx_logprob_workspace(rows, V, k))
 
 
 def mpx_attention_bwd_workspace(B: int, T: int, H: int, hd: int) -> int:

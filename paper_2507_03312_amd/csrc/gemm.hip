@@ -5,6 +5,7 @@
 // float32 calls (full-precision training) go to the kernels of gemm_f32.hip.
 #include <mutex>
 
+#include "act8.h"
 #include "gemm_f32.h"
 #include "gemm_kernels.h"
 
@@ -308,6 +309,55 @@ extern "C" int mpx_linear_bwd(const void* X, const void* W, const void* dY, cons
   clear_error();
   return linear_bwd("mpx_linear_bwd", X, W, dY, Xpre, x_act, dX, dW, db, M, N, K, dt, workspace,
                     ws_bytes, d_nonfinite, stream);
+}
+
+// ------------------------------------------------ activations in 8 bits --
+
+// Workspace: the products' own, then the activations in half, [M, K].
+static size_t act8_values_offset(int64_t M, int64_t N, int64_t K) {
+  return (mpx_linear_bwd_workspace(M, N, K) + 255) / 256 * 256;
+}
+
+extern "C" size_t mpx_linear_bwd_act8_workspace(int64_t M, int64_t N, int64_t K) {
+  if (M < 1 || N < 1 || K < 1) return 0;
+  return act8_values_offset(M, N, K) + (size_t)M * K * sizeof(uint16_t);
+}
+
+extern "C" int mpx_linear_bwd_act8(const uint8_t* Xc, const uint8_t* Xs, const void* W, const void* dY,
+                                   const uint8_t* Pc, const uint8_t* Ps, int32_t x_act, void* dX,
+                                   void* dW, void* db, int64_t M, int64_t N, int64_t K, mpx_dtype dt,
+                                   void* workspace, size_t ws_bytes, int32_t* d_nonfinite,
+                                   void* stream) {
+  clear_error();
+  const char* fn = "mpx_linear_bwd_act8";
+  MPX_REQUIRE_FN(dY, "NULL dY");
+  MPX_REQUIRE_FN(dX || dW || db, "nothing to compute: dX, dW and db are all NULL");
+  MPX_REQUIRE_FN(!dX || W, "W is required for dX");
+  MPX_REQUIRE_FN(!dW || (Xc && Xs), "Xc and Xs are required for dW");
+  MPX_REQUIRE_FN(M >= 1 && N >= 1 && K >= 1, "M, N, K must be >= 1");
+  MPX_REQUIRE_FN(is_half(dt), "dt must be MPX_F16 or MPX_BF16");
+  MPX_REQUIRE_FN(x_act == MPX_ACT_NONE || x_act == MPX_ACT_GELU_TANH, "unknown activation");
+  const bool gelu = dX && x_act == MPX_ACT_GELU_TANH;
+  MPX_REQUIRE_FN(!gelu || (Pc && Ps), "Pc and Ps are required with x_act");
+  if (dW || db || gelu) {
+    const size_t need = mpx_linear_bwd_act8_workspace(M, N, K);
+    if (ws_bytes < need || !workspace) {
+      set_error(std::string(fn) + ": workspace of " + std::to_string(need) + " bytes required");
+      return MPX_ERR_WORKSPACE;
+    }
+  }
+  const size_t values = act8_values_offset(M, N, K);
+  uint16_t* H = (uint16_t*)((char*)workspace + values);
+  if (dX) {
+    if (gelu) MPX_HIP(launch_act8_unpack(Pc, Ps, H, K, M, K, dt, (hipStream_t)stream));
+    const int rc = linear_bwd(fn, nullptr, W, dY, gelu ? H : nullptr, x_act, dX, nullptr, nullptr, M, N, K,
+                              dt, nullptr, 0, nullptr, stream);
+    if (rc != MPX_OK) return rc;
+  }
+  if (!dW && !db) return MPX_OK;
+  if (dW) MPX_HIP(launch_act8_unpack(Xc, Xs, H, K, M, K, dt, (hipStream_t)stream));
+  return linear_bwd(fn, dW ? H : nullptr, nullptr, dY, nullptr, MPX_ACT_NONE, nullptr, dW, db, M, N, K, dt,
+                    workspace, values, d_nonfinite, stream);
 }
 
 // ------------------------------------------- the variant that allocates nothing --

@@ -1,0 +1,187 @@
+"""Rotary positions with several axes on the GPU against the float64 oracle."""
+import numpy as np
+import pytest
+
+from oracle import rotary
+from oracle.numfmt import round_to
+from tests.gpu_util import HAVE_GPU, assert_within, ulp
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not HAVE_GPU, reason="no GPU")]
+
+if HAVE_GPU:
+    import torch
+    from paper_2507_03312_amd import binding as mx
+    HALF = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+FMTS = ["f16", "bf16", "f32"]
+
+
+def _s():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _positions(rng, n, axes, far):
+    pos = rng.integers(0, far, (n, axes)).astype(np.float32)
+    pos[0] = 0.0
+    if far > 100:
+        pos[-1] = far
+    return pos
+
+
+def _bound(x, ref, pairs, interleaved, rot, hd, fmt):
+    """Half a step of the output, and float32 terms of the turn: the reduced
+    angle is rounded to 2^-25 turns (2e-7 rad), sine and cosine to 2^-22, and the
+    two products and the sum to 2^-24 each: together below 2^-20 (|x0| + |x1|)."""
+    m = np.abs(x.reshape(len(x), -1, hd))
+    size = np.zeros_like(m)
+    for _, _, c0, c1 in rotary.pair_columns(pairs, interleaved):
+        size[:, :rot, c0] = size[:, :rot, c1] = m[:, :rot, c0] + m[:, :rot, c1]
+    # an error that moves the value over a rounding border costs at most itself
+    # beyond the half step
+    return 0.5 * ulp(ref, fmt) * (1 + 2.0 ** -10) + 2.0 ** -20 * size.reshape(x.shape)
+
+
+def _call(back, x, y, pos, rows, rot, copy, hd, plan, fmt, ldx, ldy, stream=None):
+    f = mx.mpx_rope_bwd if back else mx.mpx_rope_fwd
+    f(x.data_ptr(), ldx, y.data_ptr(), ldy, pos.data_ptr(), len(pos), rows, rot, copy, hd, plan,
+      mx.DTYPES[fmt], _s() if stream is None else stream)
+
+
+CASES = [
+    # rows, pos_rows, rot, copy, hd, pairs, far
+    (1, 1, 1, 0, 2, [1], 5),
+    (1, 1, 40, 8, 128, [16, 24, 24], 1 << 24),
+    (3, 3, 2, 1, 64, [16, 16], 14),
+    (16, 16, 40, 8, 128, [16, 24, 24], 1000000),
+    (197 * 2, 197, 24, 12, 64, [16, 16], 14),
+    (65 * 3, 65, 5, 3, 80, [20, 20], 9),
+    (77, 7, 3, 0, 96, [8, 40], 4000),
+    (50, 50, 4, 2, 64, [11, 4, 1, 16], 2000000),
+    (50, 25, 4, 2, 64, [3, 4], 100),            # values behind the sections
+    (33, 11, 7, 5, 10, [1, 1, 1, 1], 50),
+    (20, 20, 2, 1, 512, [256], 300),
+    (9, 9, 3, 1, 256, [4, 4, 4], 300),
+    (1030, 1030, 12, 4, 64, [8, 12, 12], 256),
+    (4097, 4097, 2, 1, 32, [8, 8], 64),
+]
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "interleaved"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(v).replace(" ", "") for v in c))
+def test_rope(fmt, interleaved, case):
+    """Both directions, out of place and in place, dense and strided; the
+    columns past the heads and the rows behind the last stay as they were."""
+    rows, pos_rows, rot, copy, hd, pairs, far = case
+    rng = np.random.default_rng(rows + hd)
+    base = [10000.0, 100.0, 37.5, 2.0][:len(pairs)]
+    width = (rot + copy) * hd
+    x = round_to(rng.normal(0, 1, (rows, width)), fmt)
+    pos = _positions(rng, pos_rows, len(pairs), far)
+    plan = mx.RopePlan(pairs, base, interleaved)
+    tp = torch.from_numpy(pos).cuda()
+    for back in (False, True):
+        ref64 = rotary.turn(x, pos, pairs, base, interleaved, rot, hd, back)
+        ref = round_to(ref64, fmt)
+        outs = []
+        for pad, off in ((0, 0), (5, 1)):
+            ld = width + pad
+            buf = torch.full((off + (rows + 1) * ld,), -7.0, dtype=HALF[fmt], device="cuda")
+            xt = buf[off:].view(rows + 1, ld)
+            xt[:rows, :width] = torch.from_numpy(x).to(HALF[fmt]).cuda()
+            out = torch.full((rows + 1, width + 3), -7.0, dtype=HALF[fmt], device="cuda")
+            _call(back, xt, out, tp, rows, rot, copy, hd, plan, fmt, ld, width + 3)
+            assert (out[rows:] == -7.0).all() and (out[:, width:] == -7.0).all()
+            outs.append(out[:rows, :width])
+            before = xt.clone()
+            _call(back, xt, xt, tp, rows, rot, copy, hd, plan, fmt, ld, ld)
+            assert torch.equal(xt[:rows, rot * hd:], before[:rows, rot * hd:])
+            assert torch.equal(xt[rows:], before[rows:]) and (buf[:off] == -7.0).all()
+            outs.append(xt[:rows, :width])
+        for o in outs[1:]:
+            assert torch.equal(o, outs[0])
+        got = outs[0].float().cpu().numpy()
+        # the whole error against the unrounded value
+        assert np.all(np.abs(got - ref64) <= _bound(x, ref64, pairs, interleaved, rot, hd, fmt))
+        still = np.all(pos == 0, axis=1)[np.arange(rows) % pos_rows]
+        assert np.array_equal(got[still], x[still])
+        assert np.array_equal(got[:, rot * hd:], x[:, rot * hd:])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_backward_is_the_gradient_by_differences(fmt):
+    """<g, turn(x + h d) - turn(x - h d)> / 2h against <bwd(g), d>, in the kernel's
+    own outputs.  Both sides sum 3 * 4 * 32 = 384 products, each output off by at
+    most half a step (2^-8, 2^-11, 2^-24 of about |v| <= 8) plus 2^-20 |v|."""
+    rows, rot, hd, pairs = 3, 4, 32, [6, 10]
+    rng = np.random.default_rng(1)
+    plan = mx.RopePlan(pairs)
+    pos = torch.from_numpy(_positions(rng, rows, 2, 30)).cuda()
+    g, d = (round_to(rng.normal(0, 1, (rows, rot * hd)), fmt) for _ in range(2))
+    tt = lambda a: torch.from_numpy(a).to(HALF[fmt]).cuda()
+    # the turn is linear: any h works, h = 1 at x = 0 wastes nothing
+    yd, dg = torch.empty_like(tt(d)), torch.empty_like(tt(g))
+    _call(False, tt(d), yd, pos, rows, rot, 0, hd, plan, fmt, rot * hd, rot * hd)
+    _call(True, tt(g), dg, pos, rows, rot, 0, hd, plan, fmt, rot * hd, rot * hd)
+    left = (yd.double().cpu().numpy() * g).sum()
+    right = (dg.double().cpu().numpy() * d).sum()
+    step = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}[fmt] + 2.0 ** -20
+    bound = step * (np.abs(yd.double().cpu().numpy() * g).sum() + np.abs(dg.double().cpu().numpy() * d).sum())
+    # the float32 terms go by both values of a pair, at most twice the turned one's norm here
+    assert abs(left - right) <= 2.0 * bound
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_not_finite_positions_and_values(fmt):
+    """A position that is not finite makes its axis's values NaN and no others;
+    a value that is not finite reaches its own pair only."""
+    plan = mx.RopePlan([4, 4])
+    x = torch.ones(4, 2 * 16, dtype=HALF[fmt], device="cuda")
+    x[3, 1] = float("inf")
+    pos = torch.tensor([[1.0, 2.0], [float("inf"), 2.0], [1.0, float("nan")], [3.0, 1.0]], device="cuda")
+    y = torch.empty_like(x)
+    _call(False, x, y, pos, 4, 2, 0, 16, plan, fmt, 32, 32)
+    n = torch.isfinite(y).cpu().numpy().reshape(4, 2, 16)
+    assert n[0].all() and not n[1, :, :8].any() and n[1, :, 8:].all()
+    assert n[2, :, :8].all() and not n[2, :, 8:].any()
+    bad = np.ones((2, 16), bool)
+    bad[0, [1, 5]] = False
+    assert np.array_equal(n[3], bad)
+
+
+def test_side_stream_and_graph():
+    rows, rot, copy, hd = 130, 6, 3, 64
+    plan = mx.RopePlan([16, 16])
+    x = torch.zeros(rows, (rot + copy) * hd, dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros(rows, 2, device="cuda")
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    ld = x.shape[1]
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        _call(False, x, y, pos, rows, rot, copy, hd, plan, "bf16", ld, ld)
+    side = torch.cuda.Stream()
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        pos.copy_(torch.randint(0, 50, pos.shape, device="cuda").float())
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            _call(False, x, z, pos, rows, rot, copy, hd, plan, "bf16", ld, ld, side.cuda_stream)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, z), i
+
+
+def test_long_strides_pass_32_bits():
+    """Rows 2^27 + 3 elements apart: the last row's offset is past 2^31 bytes."""
+    rows, ld, hd = 20, (1 << 27) + 3, 64
+    buf = torch.zeros(rows * ld, dtype=torch.bfloat16, device="cuda")
+    plan = mx.RopePlan([16, 16])
+    x = torch.randn(rows, 2 * hd, device="cuda").bfloat16()
+    pos = torch.arange(2 * rows, device="cuda", dtype=torch.float32).view(rows, 2)
+    want = torch.empty_like(x)
+    _call(False, x, want, pos, rows, 1, 1, hd, plan, "bf16", 2 * hd, 2 * hd)
+    big = buf.view(rows, ld)
+    big[:, :2 * hd] = x
+    _call(False, big, big, pos, rows, 1, 1, hd, plan, "bf16", ld, ld)
+    assert torch.equal(big[:, :2 * hd], want)
