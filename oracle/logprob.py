@@ -66,5 +66,5 @@ def backward(z, targets, stats, entropy, top_idx, g_logp, g_entropy, g_top, scal
             d = d - ge * term
             total = total + np.abs(ge) * np.where(p > 0, p * (np.abs(np.where(p > 0, lp, 0.0)) + np.abs(H)), 0.0)
         d = np.where((z == -np.inf) | empty[:, None], 0.0, d)
-        d = np.where(np.isnan(stats).any(axis=1)[:, None], np.nan, d)
+        d = np.where((np.isnan(stats).any(axis=1) | np.isnan(up))[:, None], np.nan, d)
     return scale * d, abs(scale) * total

@@ -2,6 +2,7 @@
 // gradient at the logits (mpx_logprob_fwd, mpx_logprob_bwd).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <initializer_list>
 
 #include "common.h"
@@ -17,87 +18,346 @@ __device__ __forceinline__ float logit(const typename LogitOf<DT>::type* z) {
   else return h2f<DT>(*z);
 }
 
-// Order of the alternatives as unsigned keys: by value (-0 as 0, NaN above
-// all), then by the lower column.
-__device__ __forceinline__ uint64_t rank_key(float v, uint32_t col) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);
-  const uint32_t o = v != v ? 0xFFFFFFFFu : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return ((uint64_t)o << 32) | (uint32_t)~col;
+// 16 bytes of a row at any alignment of its elements (global accesses need none
+// on gfx950), and the VE logits in them.
+typedef uint32_t lp_u32x4 __attribute__((ext_vector_type(4)));
+typedef lp_u32x4 lp_u32x4_any __attribute__((aligned(2)));
+template <int DT> constexpr int kVec = DT == MPX_F32 ? 4 : 8;
+
+template <int DT>
+__device__ __forceinline__ void lp_unpack(lp_u32x4 u, float (&x)[kVec<DT>]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (DT == MPX_F32) {
+      x[j] = __builtin_bit_cast(float, (uint32_t)u[j]);
+    } else {
+      x[2 * j] = h2f<DT>((uint16_t)(u[j] & 0xFFFFu));
+      x[2 * j + 1] = h2f<DT>((uint16_t)(u[j] >> 16));
+    }
+  }
 }
-__device__ __forceinline__ float rank_value(uint64_t key) {
-  const uint32_t o = (uint32_t)(key >> 32);
+
+// The first n (0 .. VE - 1) of a lane's logits one by one, the rest masked.
+template <int DT>
+__device__ __forceinline__ void lp_load_tail(const typename LogitOf<DT>::type* z, int n, float (&x)[kVec<DT>]) {
+#pragma unroll
+  for (int e = 0; e < kVec<DT>; ++e) x[e] = e < n ? logit<DT>(z + e) : -INFINITY;
+}
+
+// Order of the alternatives as unsigned integers: by value, -0 as 0, NaN above
+// all.  0 is below every logit and marks an empty place.
+__device__ __forceinline__ uint32_t rank_of(float v) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);
+  return v != v ? 0xFFFFFFFFu : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float rank_value(uint32_t o) {
   return __builtin_bit_cast(float, o == 0xFFFFFFFFu ? 0x7FC00000u : (o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o);
 }
+
+constexpr float kLog2e = 1.4426950408889634f;
+// differences below -200 are taken as -200: their exponential is 0 in float32,
+// and a product with it stays 0 (0 * -inf would not)
+constexpr float kFar = -200.0f;
+__device__ __forceinline__ float lp_exp(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+// Sum S of e^(z - m) and W of e^(z - m) (z - m) over some logits, m their
+// largest.  Two of them are joined by moving both to the larger m: with
+// f = e^(m - m'), S' = f S and W' = f (W + (m - m') S).
+struct Moments {
+  float m, s, w;
+  __device__ __forceinline__ void move(float to) {
+    const float del = m == -INFINITY ? kFar : fmaxf(m - to, kFar);  // -inf: S = W = 0 (or NaN)
+    const float f = lp_exp(del);
+    w = f * __builtin_fmaf(del, s, w);
+    s *= f;
+    m = to;
+  }
+};
+
+// One wave's pass over a row: per lane the moments about `ref` (moved only when
+// a logit exceeds it by 8, so nearly never after the first vectors; the sums are
+// float32 and e^8 of them costs no accuracy), the largest logit, and over the
+// wave the k best logits: lane i < k holds the i-th best one's rank and column.
+// Columns are taken in rising order, so equal logits keep the order they come
+// in, and once k are held only a strictly greater logit changes the list.
+template <int DT, bool ENT, bool TOP>
+struct RowScan {
+  static constexpr int VE = kVec<DT>;
+  float ref = -INFINITY, mx = -INFINITY, s = 0.0f, w = 0.0f;
+  uint32_t list_o = 0, list_c = 0;
+  uint32_t thr_o = 0;            // rank to exceed
+  float thr_f = NAN;             // its value; NaN: not all k places are taken (or NaN is the k-th best)
+  int k, lane;
+
+  __device__ __forceinline__ RowScan(int k_, int lane_) : k(k_), lane(lane_) {}
+
+  __device__ __forceinline__ void insert(uint32_t o, uint32_t c) {
+    const int pos = __builtin_popcountll(__builtin_amdgcn_ballot_w64(list_o >= o));
+    const uint32_t po = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)list_o, 0x138, 0xF, 0xF, false);  // lane - 1
+    const uint32_t pc = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)list_c, 0x138, 0xF, 0xF, false);
+    list_o = lane < pos ? list_o : lane == pos ? o : po;
+    list_c = lane < pos ? list_c : lane == pos ? c : pc;
+    thr_o = max(thr_o, (uint32_t)__builtin_amdgcn_readlane((int)list_o, k - 1));
+  }
+  // N ranks per lane (0: none), in rising order of columns over lanes and places
+  template <int N>
+  __device__ __forceinline__ void offer(const uint32_t (&o)[N], const uint32_t (&c)[N]) {
+    uint32_t om = o[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) om = max(om, o[e]);
+    uint64_t mask = __builtin_amdgcn_ballot_w64(om > thr_o);
+    while (mask) {
+      const int l = __builtin_ctzll(mask);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const uint32_t oe = (uint32_t)__builtin_amdgcn_readlane((int)o[e], l);
+        if (oe > thr_o) insert(oe, (uint32_t)__builtin_amdgcn_readlane((int)c[e], l));
+      }
+      mask = __builtin_amdgcn_ballot_w64(om > thr_o) & (~1ull << l);
+    }
+    const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)list_o, k - 1);
+    thr_f = kth ? rank_value(kth) : NAN;
+  }
+  // The k-th largest of the lanes' own largest logits is not above the k-th
+  // largest of all: only what reaches it is offered from the first vectors.
+  __device__ __forceinline__ void first_bound(uint32_t om) {
+    uint32_t t = 0;
+    for (int i = 0; i < k; ++i) {
+      t = wave_reduce(om, [](uint32_t a, uint32_t b) { return max(a, b); });
+      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(om == t));
+      if (lane == l) om = 0;
+    }
+    thr_o = t ? t - 1 : 0;
+  }
+
+  // a lane's VE logits from column col on; n of them exist, the others are -inf
+  __device__ __forceinline__ void add(const float (&x)[VE], uint32_t col, int n, bool first) {
+    float vm = x[0];
+#pragma unroll
+    for (int e = 1; e < VE; ++e) vm = fmaxf(vm, x[e]);
+    if (__builtin_amdgcn_ballot_w64(vm > ref + 8.0f)) {
+      if (vm > ref + 8.0f) {
+        Moments a{ref, s, w};
+        a.move(vm);
+        ref = a.m;
+        s = a.s;
+        w = a.w;
+      }
+    }
+    const float at = ref == -INFINITY ? 0.0f : ref;
+    float es = 0.0f;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float d = x[e] - at, ex = lp_exp(d);
+      es += ex;
+      if constexpr (ENT) w = __builtin_fmaf(ex, fmaxf(d, kFar), w);
+    }
+    s += es;
+    mx = fmaxf(mx, vm);
+    if constexpr (TOP) {
+      if (__builtin_amdgcn_ballot_w64(!(vm <= thr_f) || es != es) || first) {
+        uint32_t o[VE], c[VE], om = 0;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          o[e] = e < n ? rank_of(x[e]) : 0;
+          c[e] = col + e;
+          om = max(om, o[e]);
+        }
+        if (first) first_bound(om);
+        offer(o, c);
+      }
+    }
+  }
+
+  // columns [c0, c1) of the row z, this wave's chunks of 64 VE of them (every
+  // `waves`-th, from the wave-th on)
+  __device__ __forceinline__ void scan(const typename LogitOf<DT>::type* z, int64_t c0, int64_t c1, int wave,
+                                       int waves) {
+    constexpr int CH = 64 * VE, U = 4;  // U loads in flight
+    const int chunks = (int)((c1 - c0) / CH), rest = (int)((c1 - c0) % CH);
+    const typename LogitOf<DT>::type* p = z + c0 + lane * VE;
+    bool first = true;
+    for (int i = wave; i < chunks; i += U * waves) {
+      lp_u32x4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        v[u] = *reinterpret_cast<const lp_u32x4_any*>(p + (int64_t)min(i + u * waves, chunks - 1) * CH);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i + u * waves >= chunks) break;
+        float x[VE];
+        lp_unpack<DT>(v[u], x);
+        add(x, (uint32_t)(c0 + (int64_t)(i + u * waves) * CH + lane * VE), VE, first);
+        first = false;
+      }
+    }
+    if (rest && wave == chunks % waves) {
+      const int n = min(max(rest - lane * VE, 0), VE);
+      const int64_t at = c0 + (int64_t)chunks * CH + lane * VE;
+      float x[VE];
+      if (n == VE) lp_unpack<DT>(*reinterpret_cast<const lp_u32x4_any*>(z + at), x);
+      else lp_load_tail<DT>(z + at, n, x);
+      add(x, (uint32_t)at, n, first);
+    }
+  }
+  // the wave's moments about its largest logit, the same on every lane
+  __device__ __forceinline__ Moments moments() const {
+    const float m = wave_max(mx), to = m == -INFINITY ? 0.0f : m;
+    Moments a{ref, s, w};
+    a.move(to);
+    return {m, wave_sum(a.s), wave_sum(a.w)};
+  }
+};
 
 struct LogprobOut {
   float *logp, *entropy, *stats, *top_logp;
   int32_t* top_idx;
 };
 
-// One workgroup per row.
+// Partial results of a row's splits: moments, then k ranks and columns.
+struct LogprobParts {
+  float* moments;  // [rows * splits][3]
+  uint32_t* list;  // [rows * splits][k][2]
+};
+
+// A row's results from its moments (uniform over the wave) and its sorted list
+// (lane i: the i-th best).
 template <int DT>
-__global__ __launch_bounds__(256) void logprob_fwd_kernel(const void* Z, int64_t ldz,
-                                                          const int32_t* targets, int64_t V, int k,
-                                                          LogprobOut out) {
-  typedef typename LogitOf<DT>::type T;
-  __shared__ float fred[4];
-  __shared__ uint64_t kred[4];
-  const int64_t r = blockIdx.x;
-  const T* z = (const T*)Z + r * ldz;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float m = -INFINITY;
-  for (int64_t j = threadIdx.x; j < V; j += 256) m = fmaxf(m, logit<DT>(z + j));
-  m = wave_max(m);
-  if (lane == 0) fred[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(fred[0], fred[1]), fmaxf(fred[2], fred[3]));
-  if (m == -INFINITY) m = 0.0f;  // nothing but masked logits (or NaN)
-  __syncthreads();
-  float s = 0.0f, w = 0.0f;
-  for (int64_t j = threadIdx.x; j < V; j += 256) {
-    const float d = logit<DT>(z + j) - m, e = expf(d);
-    s += e;
-    if (e > 0.0f) w = __builtin_fmaf(e, d, w);
-  }
-  s = wave_sum(s);
-  w = wave_sum(w);
-  if (lane == 0) fred[wave] = s;
-  __syncthreads();
-  s = (fred[0] + fred[1]) + (fred[2] + fred[3]);
-  __syncthreads();
-  if (lane == 0) fred[wave] = w;
-  __syncthreads();
-  w = (fred[0] + fred[1]) + (fred[2] + fred[3]);
-  const bool empty = s == 0.0f;
-  const float ln = logf(s);
-  if (threadIdx.x == 0) {
+__device__ __forceinline__ void lp_results(const typename LogitOf<DT>::type* z, int64_t r, int64_t V, int k,
+                                           int lane, Moments a, uint32_t o, uint32_t c, const int32_t* targets,
+                                           const LogprobOut& out) {
+  const bool empty = a.s == 0.0f;
+  const float m = empty ? 0.0f : a.m, ln = logf(a.s);
+  if (lane == 0) {
     if (out.stats) {
-      out.stats[2 * r] = empty ? -INFINITY : s != s ? NAN : m;
+      out.stats[2 * r] = empty ? -INFINITY : a.s != a.s ? NAN : m;
       out.stats[2 * r + 1] = empty ? 0.0f : ln;
     }
-    if (out.entropy) out.entropy[r] = empty ? 0.0f : ln - w / s;
+    if (out.entropy) out.entropy[r] = empty ? 0.0f : ln - a.w / a.s;
     if (out.logp) {
       const int32_t t = targets[r];
       out.logp[r] = t < 0 ? 0.0f : t >= V ? NAN : empty ? -INFINITY : (logit<DT>(z + t) - m) - ln;
     }
   }
-  uint64_t last = ~0ull;
-  for (int i = 0; i < k; ++i) {
-    uint64_t best = 0;
-    for (int64_t j = threadIdx.x; j < V; j += 256) {
-      const uint64_t key = rank_key(logit<DT>(z + j), (uint32_t)j);
-      if (key < last || i == 0) best = max(best, key);
+  if (lane < k) {
+    out.top_idx[r * k + lane] = (int32_t)c;
+    out.top_logp[r * k + lane] = empty ? -INFINITY : (rank_value(o) - m) - ln;
+  }
+}
+
+// WAVES == 1: one wave per row, four rows per workgroup.  WAVES == 4: a
+// workgroup per row, or per split of seg columns of it, whose partial results
+// logprob_join_kernel joins.
+template <int DT, int WAVES, bool ENT, bool TOP>
+__global__ __launch_bounds__(256) void logprob_fwd_kernel(const void* Z, int64_t ldz,
+                                                          const int32_t* targets, int64_t rows, int64_t V,
+                                                          int k, int splits, int64_t seg, LogprobOut out,
+                                                          LogprobParts parts) {
+  typedef typename LogitOf<DT>::type T;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowScan<DT, ENT, TOP> scan(k, lane);
+  if constexpr (WAVES == 1) {
+    const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+    if (r >= rows) return;
+    const T* z = (const T*)Z + r * ldz;
+    scan.scan(z, 0, V, 0, 1);
+    lp_results<DT>(z, r, V, k, lane, scan.moments(), scan.list_o, scan.list_c, targets, out);
+  } else {
+    __shared__ float mom[4][3];
+    __shared__ uint32_t lists[2][64];
+    const int64_t r = blockIdx.x / splits, sp = blockIdx.x % splits;
+    const T* z = (const T*)Z + r * ldz;
+    scan.scan(z, sp * seg, min(V, (sp + 1) * seg), wave, 4);
+    const Moments a = scan.moments();
+    if (lane == 0) {
+      mom[wave][0] = a.m;
+      mom[wave][1] = a.s;
+      mom[wave][2] = a.w;
     }
-    for (int o = 32; o >= 1; o >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, o));
+    if (TOP && lane < k) {
+      lists[0][wave * k + lane] = scan.list_o;
+      // empty places after all others, each in a place of its own
+      lists[1][wave * k + lane] = scan.list_o ? scan.list_c : 0xFFFFFFFFu - (wave * 16 + lane);
+    }
     __syncthreads();
-    if (lane == 0) kred[wave] = best;
-    __syncthreads();
-    last = max(max(kred[0], kred[1]), max(kred[2], kred[3]));
-    if (threadIdx.x == 0) {
-      out.top_idx[r * k + i] = (int32_t)~(uint32_t)last;
-      out.top_logp[r * k + i] = empty ? -INFINITY : (rank_value(last) - m) - ln;
+    if (wave != 0) return;
+    const float m = fmaxf(fmaxf(mom[0][0], mom[1][0]), fmaxf(mom[2][0], mom[3][0]));
+    Moments all{m, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      Moments b{mom[i][0], mom[i][1], mom[i][2]};
+      b.move(m == -INFINITY ? 0.0f : m);
+      all.s += b.s;
+      all.w += b.w;
+    }
+    uint32_t o = 0, c = 0;
+    if constexpr (TOP) {  // the four lists in order of rank, then column
+      const int n = 4 * k;
+      const uint32_t oi = lane < n ? lists[0][lane] : 0, ci = lane < n ? lists[1][lane] : 0;
+      int better = 0;
+      for (int j = 0; j < n; ++j) {
+        const uint32_t oj = (uint32_t)__builtin_amdgcn_readlane((int)oi, j);
+        const uint32_t cj = (uint32_t)__builtin_amdgcn_readlane((int)ci, j);
+        better += oj > oi || (oj == oi && cj < ci) ? 1 : 0;
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (lane < n && better < k) {
+        lists[0][better] = oi;
+        lists[1][better] = ci;
+      }
+      __builtin_amdgcn_wave_barrier();
+      o = lane < k ? lists[0][lane] : 0;
+      c = lane < k ? lists[1][lane] : 0;
+    }
+    if (splits == 1) {
+      lp_results<DT>(z, r, V, k, lane, all, o, c, targets, out);
+      return;
+    }
+    if (lane == 0) {
+      float* p = parts.moments + (int64_t)blockIdx.x * 3;
+      p[0] = all.m;
+      p[1] = all.s;
+      p[2] = all.w;
+    }
+    if (TOP && lane < k) {
+      uint32_t* p = parts.list + ((int64_t)blockIdx.x * k + lane) * 2;
+      p[0] = o;
+      p[1] = c;
     }
   }
+}
+
+// One wave per row: the splits' moments (up to 64, one per lane) and lists.
+// The lists come in rising order of their columns' ranges, equal logits of one
+// list in rising order of columns, so the order they are offered in keeps the
+// lower column first.
+template <int DT, bool TOP>
+__global__ __launch_bounds__(256) void logprob_join_kernel(const void* Z, int64_t ldz, const int32_t* targets,
+                                                           int64_t rows, int64_t V, int k, int splits,
+                                                           LogprobOut out, LogprobParts parts) {
+  typedef typename LogitOf<DT>::type T;
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (r >= rows) return;
+  Moments a{-INFINITY, 0.0f, 0.0f};
+  if (lane < splits) {
+    const float* p = parts.moments + (r * splits + lane) * 3;
+    a = {p[0], p[1], p[2]};
+  }
+  const float m = wave_max(a.m);
+  a.move(m == -INFINITY ? 0.0f : m);
+  const Moments all{m, wave_sum(a.s), wave_sum(a.w)};
+  RowScan<DT, false, TOP> best(k, lane);
+  if constexpr (TOP) {
+    const uint32_t* p = parts.list + r * splits * k * 2;
+    const int n = splits * k;
+    for (int i = 0; i < n; i += 64) {
+      uint32_t o[1] = {i + lane < n ? p[2 * (i + lane)] : 0}, c[1] = {i + lane < n ? p[2 * (i + lane) + 1] : 0};
+      best.offer(o, c);
+    }
+  }
+  lp_results<DT>((const T*)Z + r * ldz, r, V, k, lane, all, best.list_o, best.list_c, targets, out);
 }
 
 struct LogprobGrad {
@@ -106,40 +366,107 @@ struct LogprobGrad {
   const mpx_scale_state* state;
 };
 
+// A wave's part of a row: up to U vectors per lane, all loaded before the first
+// store.  With t = (z - m) - ln S and p = e^t the gradient is
+//   p (c0 + c1 t),  c0 = -scale (sum of the upstream cotangents + g_H H),
+//   c1 = -scale g_H,
+// plus scale g at the target's and the alternatives' own columns: lane i <= k
+// holds one of those columns and its cotangent, and a chunk that holds none of
+// them, which one comparison tells, goes without.
 template <int DT>
-__global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t ldz, int64_t V, int k,
-                                                          LogprobGrad g, void* dZ, int64_t ldo,
-                                                          int64_t col_blocks) {
+__global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t ldz, int64_t rows, int64_t V,
+                                                          int k, LogprobGrad g, void* dZ, int64_t ldo,
+                                                          int64_t row_waves) {
   typedef typename LogitOf<DT>::type T;
-  const int64_t r = blockIdx.x / col_blocks;
-  const int64_t j = (blockIdx.x % col_blocks) * 256 + threadIdx.x;
-  if (j >= V) return;
-  const float scale = g.state ? g.state->scale : 1.0f;
-  const float m = g.stats[2 * r], ln = g.stats[2 * r + 1];
-  const bool empty = m == -INFINITY;
-  const int32_t t = g.g_logp ? g.targets[r] : -1;
-  float up = 0.0f, own = 0.0f;  // cotangents of all log probabilities, and of column j's
-  if (t >= 0) {
-    const float gl = g.g_logp[r];
-    up += t < V ? gl : NAN;
-    if (t == j) own += gl;
+  constexpr int VE = kVec<DT>, CH = 64 * VE, U = 4;
+  const int lane = threadIdx.x & 63;
+  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = task / row_waves;
+  if (r >= rows) return;
+  const int64_t c0 = (task % row_waves) * (U * CH);
+  const T* z = (const T*)Z + r * ldz + c0;
+  T* o = (T*)dZ + r * ldo + c0;
+  const int64_t left = V - c0;  // >= 1
+  float x[U][VE];
+  lp_u32x4 v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = u * CH + lane * VE;
+    if (at + VE <= left) v[u] = *reinterpret_cast<const lp_u32x4_any*>(z + at);
+    else lp_load_tail<DT>(z + at, (int)max<int64_t>(left - at, 0), x[u]);
   }
-  if (g.g_top) {
-    for (int i = 0; i < k; ++i) {
-      const float gt = g.g_top[r * k + i];
-      const int32_t c = g.top_idx[r * k + i];
-      up += c >= 0 && c < V ? gt : NAN;
-      if (c == j) own += gt;
+  const float scale = g.state ? g.state->scale : 1.0f;
+  const float ms = g.stats[2 * r], ln = g.stats[2 * r + 1], m = ms == -INFINITY ? 0.0f : ms;
+  int64_t mine = -1;  // lane's special column and its cotangent
+  float own = 0.0f;
+  if (lane < k && g.g_top) {
+    mine = g.top_idx[r * k + lane];
+    own = g.g_top[r * k + lane];
+    if (mine < 0 || mine >= V) own = NAN;
+  } else if (lane == k && g.g_logp) {
+    mine = g.targets[r];
+    own = mine < 0 ? 0.0f : mine < V ? g.g_logp[r] : NAN;
+  }
+  const float up = wave_sum(own);
+  const float ge = g.g_entropy ? g.g_entropy[r] : 0.0f, H = g.g_entropy ? g.entropy[r] : 0.0f;
+  const float nan = ln != ln ? NAN : 0.0f;
+  const float k1 = -scale * ge, k0 = __builtin_fmaf(k1, H, -scale * up) + nan;
+  own *= scale;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = u * CH + lane * VE;
+    if (u * CH >= left) break;
+    const int n = (int)min<int64_t>(max<int64_t>(left - at, 0), VE);
+    if (n == VE) lp_unpack<DT>(v[u], x[u]);
+    float d[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float t = fmaxf((x[u][e] - m) - ln, kFar);
+      d[e] = lp_exp(t) * __builtin_fmaf(k1, t, k0);
+    }
+    uint64_t mask = __builtin_amdgcn_ballot_w64(mine - c0 >= u * CH && mine - c0 < (u + 1) * CH);
+    while (mask) {
+      const int l = __builtin_ctzll(mask);
+      mask &= mask - 1;
+      const int off = __builtin_amdgcn_readlane((int)(mine - c0), l);
+      const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, own), l));
+#pragma unroll
+      for (int e = 0; e < VE; ++e)
+        if (at + e == off && x[u][e] != -INFINITY) d[e] += add;
+    }
+    if (n == VE) {
+      lp_u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == MPX_F32) w[j] = __builtin_bit_cast(uint32_t, d[j]);
+        else w[j] = f2h<DT>(d[2 * j]) | ((uint32_t)f2h<DT>(d[2 * j + 1]) << 16);
+      }
+      *reinterpret_cast<lp_u32x4_any*>(o + at) = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        if (e < n) {
+          if constexpr (DT == MPX_F32) o[at + e] = d[e];
+          else o[at + e] = f2h<DT>(d[e]);
+        }
+      }
     }
   }
-  const float z = logit<DT>((const T*)Z + r * ldz + j);
-  const float lp = (z - m) - ln, p = expf(lp);
-  float d = own - p * up;
-  if (g.g_entropy && p > 0.0f) d -= g.g_entropy[r] * p * (lp + g.entropy[r]);
-  if (empty || z == -INFINITY) d = ln != ln ? NAN : 0.0f;
-  T* o = (T*)dZ + r * ldo + j;
-  if constexpr (DT == MPX_F32) *o = scale * d;
-  else *o = f2h<DT>(scale * d);
+}
+
+// Rows of up to kWaveRow logits take one wave each; longer ones a workgroup, or
+// several: columns are split until there are about 1024 workgroups, into parts
+// of at least kLeastSplit columns, at most 64.
+constexpr int64_t kWaveRow = 2048, kLeastSplit = 4096;
+struct LogprobPlan {
+  int splits;
+  int64_t seg;
+};
+static LogprobPlan logprob_plan(int64_t rows, int64_t V) {
+  if (V <= kWaveRow) return {1, V};
+  const int64_t want = std::min<int64_t>({cdiv(1024, rows), cdiv(V, kLeastSplit), 64});
+  const int64_t seg = cdiv(cdiv(V, want), kLeastSplit) * kLeastSplit;
+  return {(int)cdiv(V, seg), seg};
 }
 
 }  // namespace mpx
@@ -160,10 +487,9 @@ static bool aligned4(std::initializer_list<const void*> ps) {
   } while (0)
 
 extern "C" size_t mpx_logprob_workspace(int64_t rows, int64_t V, int32_t k) {
-  (void)rows;
-  (void)V;
-  (void)k;
-  return 0;
+  if (rows < 1 || V < 1 || k < 0 || k > MPX_LOGPROB_MAX_K) return 0;
+  const int splits = logprob_plan(rows, V).splits;
+  return splits == 1 ? 0 : (size_t)rows * splits * (3 * sizeof(float) + 2 * k * sizeof(uint32_t));
 }
 
 extern "C" int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t rows,
@@ -171,8 +497,6 @@ extern "C" int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* target
                                float* top_logp, int32_t* top_idx, mpx_dtype dt, void* workspace,
                                size_t ws_bytes, void* stream) {
   clear_error();
-  (void)workspace;
-  (void)ws_bytes;
   MPX_REQUIRE(Z, "NULL logits");
   MPX_REQUIRE(is_half(dt) || dt == MPX_F32, "dt must be MPX_F16, MPX_BF16 or MPX_F32");
   MPX_REQUIRE(rows >= 1 && V >= 1 && V <= INT32_MAX && rows <= ((int64_t)1 << 23), "bad sizes");
@@ -183,12 +507,39 @@ extern "C" int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* target
   MPX_REQUIRE(!logp || targets, "logp needs targets");
   MPX_REQUIRE(logp || entropy || stats || k > 0, "nothing to compute");
   MPX_REQUIRE(reinterpret_cast<uintptr_t>(Z) % (dt == MPX_F32 ? 4 : 2) == 0, "misaligned logits");
-  MPX_REQUIRE(aligned4({targets, logp, entropy, stats, top_logp, top_idx}), "misaligned operand");
+  MPX_REQUIRE(aligned4({targets, logp, entropy, stats, top_logp, top_idx, workspace}), "misaligned operand");
+  const size_t need = mpx_logprob_workspace(rows, V, k);
+  if (need && (!workspace || ws_bytes < need)) {
+    set_error("mpx_logprob_fwd: workspace of " + std::to_string(need) + " bytes required");
+    return MPX_ERR_WORKSPACE;
+  }
+  const LogprobPlan plan = logprob_plan(rows, V);
   const LogprobOut out = {logp, entropy, stats, top_logp, top_idx};
-#define MPX_LP(DTv) \
-  logprob_fwd_kernel<DTv><<<(unsigned)rows, 256, 0, (hipStream_t)stream>>>(Z, ldz, targets, V, k, out)
+  const LogprobParts parts = {(float*)workspace, (uint32_t*)workspace + rows * plan.splits * 3};
+  hipStream_t s = (hipStream_t)stream;
+  const unsigned waves4 = (unsigned)cdiv(rows, 4), blocks = (unsigned)(rows * plan.splits);
+#define MPX_LP_FWD(DTv, ENTv, TOPv)                                                                      \
+  do {                                                                                                   \
+    if (V <= kWaveRow)                                                                                   \
+      logprob_fwd_kernel<DTv, 1, ENTv, TOPv>                                                             \
+          <<<waves4, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, plan.seg, out, parts);       \
+    else                                                                                                 \
+      logprob_fwd_kernel<DTv, 4, ENTv, TOPv>                                                             \
+          <<<blocks, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, plan.seg, out, parts);       \
+    if (plan.splits > 1)                                                                                 \
+      logprob_join_kernel<DTv, TOPv>                                                                     \
+          <<<waves4, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, out, parts);                 \
+  } while (0)
+#define MPX_LP(DTv)                              \
+  do {                                           \
+    if (entropy && k) MPX_LP_FWD(DTv, true, true);   \
+    else if (entropy) MPX_LP_FWD(DTv, true, false);  \
+    else if (k) MPX_LP_FWD(DTv, false, true);        \
+    else MPX_LP_FWD(DTv, false, false);              \
+  } while (0)
   MPX_BY_TYPE(dt, MPX_LP);
 #undef MPX_LP
+#undef MPX_LP_FWD
   MPX_LAUNCHED();
   return MPX_OK;
 }
@@ -214,11 +565,12 @@ extern "C" int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* target
   MPX_REQUIRE(aligned4({targets, stats, entropy, top_idx, g_logp, g_entropy, g_top, d_state}),
               "misaligned operand");
   const LogprobGrad g = {targets, top_idx, stats, entropy, g_logp, g_entropy, g_top, d_state};
-  const int64_t cb = cdiv(V, 256);
-  MPX_REQUIRE(rows <= ((int64_t)1 << 23) / cb, "rows * V too large for one call");
-#define MPX_LP(DTv)                                                                                \
-  logprob_bwd_kernel<DTv><<<(unsigned)(rows * cb), 256, 0, (hipStream_t)stream>>>(Z, ldz, V, k, g, dZ, \
-                                                                                  ldo, cb)
+  // tasks of up to 4 vectors per lane, four to a workgroup (2^32 work-items)
+  const int64_t row_waves = cdiv(V, 4 * 64 * (dt == MPX_F32 ? 4 : 8));
+  MPX_REQUIRE(rows <= ((int64_t)1 << 25) / row_waves, "rows * V too large for one call");
+  const unsigned blocks = (unsigned)cdiv(rows * row_waves, 4);
+#define MPX_LP(DTv)                                                                                   \
+  logprob_bwd_kernel<DTv><<<blocks, 256, 0, (hipStream_t)stream>>>(Z, ldz, rows, V, k, g, dZ, ldo, row_waves)
   MPX_BY_TYPE(dt, MPX_LP);
 #undef MPX_LP
   MPX_LAUNCHED();
