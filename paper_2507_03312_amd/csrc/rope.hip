@@ -1,6 +1,7 @@
 // Rotary positions with several axes (mpx_rope_fwd, mpx_rope_bwd).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "common.h"
@@ -8,67 +9,169 @@
 namespace mpx {
 
 constexpr int kRopeMaxHd = 512;
+constexpr int kRopeTable = 1024;  // turns (cosine, sine) that a workgroup holds in LDS
 
-// The turn of every pair of a head, in turns per unit of position, and where
-// its two values lie.
 struct RopeArgs {
-  double rev[kRopeMaxHd / 2];
   const void* X;
   void* Y;
   const float* pos;
-  int64_t ldx, ldy, pos_rows, rows, heads_rot, heads_copy;
+  int64_t ldx, ldy;
+  uint32_t pos_rows, rows, heads_rot, copy;  // copy: values copied behind the turned heads
   int32_t hd, axes, npairs, interleaved, back, in_place;
+  // a workgroup's rows, and the threads that share a row's heads: thread
+  // (slot, chunk) takes heads slot % head_slots, + head_slots, ... of row
+  // slot / head_slots, with the pairs of `chunk` of each
+  int32_t wg_rows, head_slots, chunks;
   int32_t first_pair[MPX_ROPE_MAX_AXES + 1];  // axis a owns pairs [first_pair[a], first_pair[a + 1])
+  double step[MPX_ROPE_MAX_AXES];             // log2(base) / pairs
 };
 
 template <int DT> struct RopeValue { typedef uint16_t type; };
 template <> struct RopeValue<MPX_F32> { typedef float type; };
-template <int DT>
-__device__ __forceinline__ float rope_load(const typename RopeValue<DT>::type* p) {
-  if constexpr (DT == MPX_F32) return *p;
-  else return h2f<DT>(*p);
-}
-template <int DT>
-__device__ __forceinline__ void rope_store(typename RopeValue<DT>::type* p, float v) {
-  if constexpr (DT == MPX_F32) *p = v;
-  else *p = f2h<DT>(v);
-}
 
-// One workgroup per row: a thread takes one pair (or one value that is not
-// turned) of every head in turn.
-template <int DT>
+// N values at any alignment of theirs (global accesses need no more on gfx950)
+template <int DT, int N> struct RopeVec {
+  typedef typename RopeValue<DT>::type T;
+  T v[N];
+  __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
+  __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, v, sizeof(v)); }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (DT == MPX_F32) return v[i];
+    else return h2f<DT>(v[i]);
+  }
+  __device__ __forceinline__ void set(int i, float f) {
+    if constexpr (DT == MPX_F32) v[i] = f;
+    else v[i] = f2h<DT>(f);
+  }
+};
+
+// Bound by HBM (every value read and written once).  The turns are as many as
+// rows x pairs, far fewer than the values, but dear (float64 angles): a
+// workgroup makes each of its rows' once, into LDS, while the copied heads
+// stream; every thread then keeps the turns of its VW pairs in registers and goes
+// through the heads, two vectors of VW values from each, four heads in flight.
+// VW pairs lie in two runs of VW values (halves), or in one of 2 VW
+// (interleaved).  Values behind the sections count as pairs that are not turned;
+// a head of odd length has one more (VW == 1 then).
+template <int DT, int VW, bool INTER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   typedef typename RopeValue<DT>::type T;
-  const int64_t r = blockIdx.x;
-  const T* x = (const T*)a.X + r * a.ldx;
-  T* y = (T*)a.Y + r * a.ldy;
-  const float* pos = a.pos + (r % a.pos_rows) * a.axes;
-  const int rest = a.hd - 2 * a.npairs;
-  for (int i = threadIdx.x; i < a.npairs + rest; i += 256) {
-    if (i < a.npairs) {
-      int ax = 0;
-      while (i >= a.first_pair[ax + 1]) ++ax;
-      const int n = a.first_pair[ax + 1] - a.first_pair[ax], j = i - a.first_pair[ax];
-      const int o = 2 * a.first_pair[ax];
-      const int i0 = o + (a.interleaved ? 2 * j : j), i1 = o + (a.interleaved ? 2 * j + 1 : n + j);
-      double t = (double)pos[ax] * a.rev[i];
-      t -= rint(t);
-      float s, c;
-      sincospif(2.0f * (float)t, &s, &c);
-      if (a.back) s = -s;
-      for (int64_t h = 0; h < a.heads_rot; ++h) {
-        const float x0 = rope_load<DT>(x + h * a.hd + i0), x1 = rope_load<DT>(x + h * a.hd + i1);
-        rope_store<DT>(y + h * a.hd + i0, __builtin_fmaf(x0, c, -(x1 * s)));
-        rope_store<DT>(y + h * a.hd + i1, __builtin_fmaf(x1, c, x0 * s));
-      }
-    } else if (!a.in_place) {
-      const int v = a.npairs + i;  // values behind the pairs
-      for (int64_t h = 0; h < a.heads_rot; ++h) y[h * a.hd + v] = x[h * a.hd + v];
+  __shared__ float2 turns[kRopeTable];
+  const uint32_t row0 = blockIdx.x * a.wg_rows;
+  const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
+  T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
+  const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
+
+  if (!a.in_place && a.copy) {
+    constexpr uint32_t VE = 16 / sizeof(T);
+    const int64_t w0 = (int64_t)a.heads_rot * a.hd;
+    const uint32_t nv = a.copy / VE, rest = a.copy % VE;
+    for (uint32_t i = threadIdx.x; i < nrows * nv; i += 256) {
+      const uint32_t r = i / nv, c = (i % nv) * VE;
+      RopeVec<DT, VE> v;
+      v.load(X + r * a.ldx + w0 + c);
+      v.store(Y + r * a.ldy + w0 + c);
+    }
+    for (uint32_t i = threadIdx.x; i < nrows * rest; i += 256) {
+      const int64_t r = i / rest, c = w0 + nv * VE + i % rest;
+      Y[r * a.ldy + c] = X[r * a.ldx + c];
     }
   }
-  if (a.in_place) return;
-  const int64_t w0 = a.heads_rot * a.hd, w1 = w0 + a.heads_copy * a.hd;
-  for (int64_t v = w0 + threadIdx.x; v < w1; v += 256) y[v] = x[v];
+  for (uint32_t i = threadIdx.x; i < nrows * a.npairs; i += 256) {
+    const uint32_t r = i / a.npairs, p = i % a.npairs;
+    int ax = 0;
+#pragma unroll
+    for (int k = 1; k < MPX_ROPE_MAX_AXES; ++k) ax += (int)p >= a.first_pair[k] ? 1 : 0;
+    const double turn = exp2(-(double)((int)p - a.first_pair[ax]) * a.step[ax]) * 0.15915494309189533577;
+    double t = (double)a.pos[(int64_t)((row0 + r) % a.pos_rows) * a.axes + ax] * turn;
+    t -= rint(t);  // exact: what is left is at most half a turn
+    float s, c;
+    sincospif(2.0f * (float)t, &s, &c);
+    turns[i] = make_float2(c, a.back ? -s : s);
+  }
+  __syncthreads();
+
+  const uint32_t chunk = threadIdx.x % a.chunks, slot = threadIdx.x / a.chunks;
+  const uint32_t r = slot / a.head_slots, h0 = slot % a.head_slots;
+  if (r >= nrows) return;
+  const int p0 = chunk * VW;  // the thread's first pair
+  const bool turned = p0 < a.npairs;
+  float c[VW], s[VW];
+  int at0, at1;  // its two runs of values
+  if constexpr (INTER) {
+    at0 = 2 * p0;
+    at1 = at0 + VW;
+  } else {
+    // sections: the axes', then what is not turned
+    int first = 0, n = a.hd / 2 - a.npairs;
+#pragma unroll
+    for (int k = 0; k < MPX_ROPE_MAX_AXES; ++k) {
+      if (p0 >= a.first_pair[k]) {
+        first = a.first_pair[k];
+        n = a.first_pair[k + 1] - first;
+      }
+    }
+    if (!turned) {
+      first = a.npairs;
+      n = a.hd / 2 - a.npairs;
+    }
+    at0 = 2 * first + (p0 - first);
+    at1 = at0 + n;
+  }
+#pragma unroll
+  for (int i = 0; i < VW; ++i) {
+    const float2 t = turned ? turns[r * a.npairs + p0 + i] : make_float2(1.0f, 0.0f);
+    c[i] = t.x;
+    s[i] = t.y;
+  }
+  const T* x = X + r * a.ldx;
+  T* y = Y + r * a.ldy;
+  constexpr int U = 4;
+  for (uint32_t h = h0; h < a.heads_rot; h += U * a.head_slots) {
+    RopeVec<DT, VW> v0[U], v1[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const T* p = x + (int64_t)min(h + u * a.head_slots, a.heads_rot - 1) * a.hd;
+      v0[u].load(p + at0);
+      v1[u].load(p + at1);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (h + u * a.head_slots >= a.heads_rot) break;
+      T* p = y + (int64_t)(h + u * a.head_slots) * a.hd;
+      if (turned) {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          if constexpr (INTER && VW > 1) {  // pair i at values 2 i and 2 i + 1 of both runs together
+            RopeVec<DT, VW>& v = 2 * i < VW ? v0[u] : v1[u];
+            const int j = (2 * i) % VW;
+            const float x0 = v.get(j), x1 = v.get(j + 1);
+            v.set(j, __builtin_fmaf(x0, c[i], -(x1 * s[i])));
+            v.set(j + 1, __builtin_fmaf(x1, c[i], x0 * s[i]));
+          } else {
+            const float x0 = v0[u].get(i), x1 = v1[u].get(i);
+            v0[u].set(i, __builtin_fmaf(x0, c[i], -(x1 * s[i])));
+            v1[u].set(i, __builtin_fmaf(x1, c[i], x0 * s[i]));
+          }
+        }
+      }
+      if (turned || !a.in_place) {
+        v0[u].store(p + at0);
+        v1[u].store(p + at1);
+      }
+    }
+  }
+  if constexpr (VW == 1) {
+    if ((a.hd & 1) && chunk == 0 && !a.in_place)
+      for (uint32_t h = h0; h < a.heads_rot; h += a.head_slots)
+        y[(int64_t)h * a.hd + a.hd - 1] = x[(int64_t)h * a.hd + a.hd - 1];
+  }
+}
+
+template <int DT, int VW>
+static void launch_rope(const RopeArgs& a, unsigned blocks, hipStream_t s) {
+  if (a.interleaved) rope_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
+  else rope_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
 }
 
 static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, int64_t ldy,
@@ -99,41 +202,65 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
                  "pointers must be aligned to their element");
   RopeArgs a{};
   int64_t n = 0;
+  // pairs of one vector: a power of two that divides every section, also that of
+  // the values that are not turned, of at most 16 bytes a run
+  int vw = hd % 2 ? 1 : dt == MPX_F32 ? 4 : 8;
   for (int ax = 0; ax < plan->axes; ++ax) {
     const int64_t p = plan->pairs[ax];
     const double base = plan->base[ax];
     MPX_REQUIRE_FN(p >= 1 && 2 * (n + p) <= hd, "pairs must be >= 1 and 2 * their sum <= hd");
     MPX_REQUIRE_FN(std::isfinite(base) && base > 1.0, "base must be finite and > 1");
-    for (int64_t i = 0; i < p; ++i)
-      a.rev[n + i] = std::pow(base, -(double)i / (double)p) / 6.283185307179586476925286766559;
+    a.step[ax] = std::log2(base) / (double)p;
     a.first_pair[ax] = (int32_t)n;
     n += p;
+    while (!plan->interleaved && p % vw) vw /= 2;
   }
+  while (n % vw || (hd / 2 - n) % vw) vw /= 2;
   for (int ax = plan->axes; ax <= MPX_ROPE_MAX_AXES; ++ax) a.first_pair[ax] = (int32_t)n;
-  MPX_REQUIRE_FN(rows < ((int64_t)1 << 24), "at most 2^24 - 1 rows in one call");
-#undef MPX_REQUIRE_FN
   a.X = X;
   a.Y = Y;
   a.pos = pos;
   a.ldx = ldx;
   a.ldy = ldy;
-  a.pos_rows = pos_rows;
-  a.rows = rows;
-  a.heads_rot = heads_rot;
-  a.heads_copy = heads_copy;
+  a.heads_rot = (uint32_t)heads_rot;
+  a.copy = (uint32_t)(heads_copy * hd);
   a.hd = (int32_t)hd;
   a.axes = plan->axes;
   a.npairs = (int32_t)n;
   a.interleaved = plan->interleaved;
   a.back = back ? 1 : 0;
   a.in_place = X == Y ? 1 : 0;
+  a.chunks = (int32_t)(hd / 2) / vw;
+  // Rows of a workgroup: about four heads to a thread where the rows suffice for
+  // 1024 workgroups, never more turns than the table holds.
+  const int64_t slots = 256 / a.chunks;
+  int64_t wg_rows = std::min<int64_t>({4 * slots / heads_rot, slots, kRopeTable / n, rows / 1024});
+  wg_rows = std::max<int64_t>(wg_rows, 1);
+  a.wg_rows = (int32_t)wg_rows;
+  a.head_slots = (int32_t)(slots / wg_rows);
+  const int64_t blocks = cdiv(rows, wg_rows);
+  MPX_REQUIRE_FN(rows <= INT32_MAX && blocks < ((int64_t)1 << 24), "too many rows for one call");
+#undef MPX_REQUIRE_FN
+  a.rows = (uint32_t)rows;
+  a.pos_rows = (uint32_t)pos_rows;
   hipStream_t s = (hipStream_t)stream;
-  const unsigned blocks = (unsigned)rows;
-  switch (dt) {
-    case MPX_F16: rope_kernel<MPX_F16><<<blocks, 256, 0, s>>>(a); break;
-    case MPX_BF16: rope_kernel<MPX_BF16><<<blocks, 256, 0, s>>>(a); break;
-    default: rope_kernel<MPX_F32><<<blocks, 256, 0, s>>>(a);
+#define MPX_ROPE(DTv)                                                    \
+  do {                                                                   \
+    if (vw == 4) launch_rope<DTv, 4>(a, (unsigned)blocks, s);            \
+    else if (vw == 2) launch_rope<DTv, 2>(a, (unsigned)blocks, s);       \
+    else launch_rope<DTv, 1>(a, (unsigned)blocks, s);                    \
+  } while (0)
+  if (dt == MPX_F32) {
+    MPX_ROPE(MPX_F32);
+  } else if (vw == 8) {
+    if (dt == MPX_F16) launch_rope<MPX_F16, 8>(a, (unsigned)blocks, s);
+    else launch_rope<MPX_BF16, 8>(a, (unsigned)blocks, s);
+  } else if (dt == MPX_F16) {
+    MPX_ROPE(MPX_F16);
+  } else {
+    MPX_ROPE(MPX_BF16);
   }
+#undef MPX_ROPE
   MPX_LAUNCHED();
   return MPX_OK;
 }
