@@ -292,10 +292,11 @@ int mpx_act8_unpack(const uint8_t* codes, const uint8_t* scales, void* Y, int64_
  *   dW = half(dY^T X);  db = half(sum_m dY[m,:]).
  * Shapes, subsets (dX, dW, db may be NULL, not all), d_nonfinite and errors as
  * mpx_linear_bwd; Xc and Xs are needed for dW only, Pc and Ps for dX through
- * GELU only.  dt == MPX_F16 or MPX_BF16.  Whatever overlaps needs its own
- * workspace (device, mpx_linear_bwd_act8_workspace(M, N, K) bytes when dW or
- * db is requested or x_act is set for dX, else it may be NULL).  That size
- * never falls as M grows. */
+ * GELU only.  dt == MPX_F16 or MPX_BF16; codes and scales at any address.  Whatever
+ * overlaps needs its own workspace (device, mpx_linear_bwd_act8_workspace(M, N,
+ * K) bytes when dW or db is requested, else it may be NULL).  That size never
+ * falls as M grows; the activations are widened on their way into the matrix
+ * cores, never in memory. */
 int mpx_linear_bwd_act8(const uint8_t* Xc, const uint8_t* Xs, const void* W, const void* dY,
                         const uint8_t* Pc, const uint8_t* Ps, int32_t x_act, void* dX, void* dW,
                         void* db, int64_t M, int64_t N, int64_t K, mpx_dtype dt, void* workspace,

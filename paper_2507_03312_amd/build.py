@@ -19,6 +19,7 @@ LIB = os.path.join(PKG, "libmpx.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 SOURCES = ["gemm_f16.hip", "gemm_bf16.hip", "gemm_staged_f16.hip", "gemm_staged_bf16.hip",
            "gemm_wide_f16.hip", "gemm_wide_bf16.hip", "support.hip", "attention.hip", "sweep.hip",
+           "gemm_act8_f16.hip", "gemm_act8_bf16.hip",
            "gemm.hip", "gemm_f32.hip", "support_f32.hip", "act8.hip", "rope.hip", "logprob.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

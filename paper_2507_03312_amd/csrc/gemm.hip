@@ -5,7 +5,6 @@
 // float32 calls (full-precision training) go to the kernels of gemm_f32.hip.
 #include <mutex>
 
-#include "act8.h"
 #include "gemm_f32.h"
 #include "gemm_kernels.h"
 
@@ -17,6 +16,10 @@ static hipError_t gemm_dispatch(mpx_dtype dt, const GemmArgs& g, bool ak, bool b
                                 hipStream_t s, bool* db_fused = nullptr) {
   return dt == MPX_F16 ? run_gemm_f16(g, ak, bk, nbatch, s, db_fused)
                        : run_gemm_bf16(g, ak, bk, nbatch, s, db_fused);
+}
+
+static hipError_t gemm_dispatch_act8(mpx_dtype dt, const GemmArgs& g, hipStream_t s, bool* db_fused) {
+  return dt == MPX_F16 ? run_gemm_act8_f16(g, s, db_fused) : run_gemm_act8_bf16(g, s, db_fused);
 }
 
 static GemmArgs base_args() {
@@ -165,8 +168,15 @@ extern "C" size_t mpx_linear_bwd_workspace(int64_t M, int64_t N, int64_t K) {
   return std::max(ws, colsum_workspace(M, N)) + 256;
 }
 
-// Shared body of mpx_linear_bwd and mpx_linear_bwd_noalloc (`fn` names the
-// entry point in error messages).
+// The layer's kept activations as 8-bit checkpoints: its input and, behind GELU,
+// the input's pre-activation.
+struct Act8Inputs {
+  const uint8_t *Xc, *Xs, *Pc, *Ps;
+};
+
+// Shared body of mpx_linear_bwd, mpx_linear_bwd_noalloc and mpx_linear_bwd_act8
+// (`fn` names the entry point in error messages; a8 set: X and Xpre are those
+// checkpoints, and a half type).
 #define MPX_REQUIRE_FN(cond, msg)                          \
   do {                                                     \
     if (!(cond)) {                                         \
@@ -178,15 +188,19 @@ extern "C" size_t mpx_linear_bwd_workspace(int64_t M, int64_t N, int64_t K) {
 static int linear_bwd(const char* fn, const void* X, const void* W, const void* dY, const void* Xpre,
                       int32_t x_act, void* dX, void* dW, void* db, int64_t M, int64_t N, int64_t K,
                       mpx_dtype dt, void* workspace, size_t ws_bytes, int32_t* d_nonfinite,
-                      void* stream) {
+                      void* stream, const Act8Inputs* a8 = nullptr) {
   MPX_REQUIRE_FN(dY, "NULL dY");
   MPX_REQUIRE_FN(dX || dW || db, "nothing to compute: dX, dW and db are all NULL");
   MPX_REQUIRE_FN(!dX || W, "W is required for dX");
-  MPX_REQUIRE_FN(!dW || X, "X is required for dW");
+  MPX_REQUIRE_FN(!dW || a8 || X, "X is required for dW");
+  MPX_REQUIRE_FN(!dW || !a8 || (a8->Xc && a8->Xs), "Xc and Xs are required for dW");
   MPX_REQUIRE_FN(M >= 1 && N >= 1 && K >= 1, "M, N, K must be >= 1");
+  MPX_REQUIRE_FN(!a8 || is_half(dt), "dt must be MPX_F16 or MPX_BF16");
   MPX_REQUIRE_FN(is_half(dt) || dt == MPX_F32, "dt must be MPX_F16, MPX_BF16 or MPX_F32");
   MPX_REQUIRE_FN(x_act == MPX_ACT_NONE || x_act == MPX_ACT_GELU_TANH, "unknown activation");
-  MPX_REQUIRE_FN(x_act == MPX_ACT_NONE || !dX || Xpre, "Xpre is required with x_act");
+  MPX_REQUIRE_FN(x_act == MPX_ACT_NONE || !dX || a8 || Xpre, "Xpre is required with x_act");
+  MPX_REQUIRE_FN(x_act == MPX_ACT_NONE || !dX || !a8 || (a8->Pc && a8->Ps),
+                 "Pc and Ps are required with x_act");
   MPX_REQUIRE_FN(dt != MPX_F32 || !d_nonfinite, "d_nonfinite is counted for half gradients only");
   if (dW || db) {  // only the weight and bias gradients use the workspace
     // a bias-only call needs just the column partials
@@ -243,7 +257,12 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
     g.C = (uint16_t*)dX;
     g.M = M; g.N = K; g.K = N;
     g.lda = N; g.ldb = K; g.ldc = K;
-    g.dact = x_act ? (const uint16_t*)Xpre : nullptr;
+    if (a8) {
+      g.dact8 = x_act ? a8->Pc : nullptr;
+      g.dact8_scale = x_act ? a8->Ps : nullptr;
+    } else {
+      g.dact = x_act ? (const uint16_t*)Xpre : nullptr;
+    }
     MPX_HIP(gemm_dispatch(dt, g, true, false, 1, s));
   }
   // dW[N,K] = dY^T X: A(m=n, k=m_tok) = dY[m_tok*N + n] (mn-major), B(n=k', k=m_tok) = X[m_tok*K + k']
@@ -259,15 +278,22 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
     g.lda = N; g.ldb = K; g.ldc = K;
     g.nonfinite = d_nonfinite;
     g.db = (uint16_t*)db;
+    if (a8) {
+      g.b8 = a8->Xc;
+      g.b8_scale = a8->Xs;
+    }
+    auto product = [&] {
+      return a8 ? gemm_dispatch_act8(dt, g, s, &db_fused) : gemm_dispatch(dt, g, false, false, 1, s, &db_fused);
+    };
     int sp;
     int64_t ks;
-    split_plan(N, K, M, dma_ok(g, operands_aligned(g), false, false) ? kHalfCost : kHalfStagedCost, sp, ks);
+    split_plan(N, K, M, !a8 && dma_ok(g, operands_aligned(g), false, false) ? kHalfCost : kHalfStagedCost, sp, ks);
     if (sp > 1) {
       g.splits = sp;
       g.k_split = ks;
       g.ws = (float*)workspace;
       g.dbp = db ? (float*)((char*)workspace + db_partials_offset(sp, N, K)) : nullptr;
-      MPX_HIP(gemm_dispatch(dt, g, false, false, 1, s, &db_fused));
+      MPX_HIP(product());
       // the GEMM wrote splits x (K / 128 tile columns) bias partials per row
       const int64_t MN = N * K, nrows = db_fused ? N : 0;
       const int dbparts = (int)(db_partials_count(sp, N, K) / N);
@@ -288,7 +314,7 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
 #undef MPX_SKR
       MPX_LAUNCHED();
     } else {
-      MPX_HIP(gemm_dispatch(dt, g, false, false, 1, s, &db_fused));
+      MPX_HIP(product());
     }
   }
   if (db && !db_fused) {
@@ -311,16 +337,8 @@ extern "C" int mpx_linear_bwd(const void* X, const void* W, const void* dY, cons
                     ws_bytes, d_nonfinite, stream);
 }
 
-// ------------------------------------------------ activations in 8 bits --
-
-// Workspace: the products' own, then the activations in half, [M, K].
-static size_t act8_values_offset(int64_t M, int64_t N, int64_t K) {
-  return (mpx_linear_bwd_workspace(M, N, K) + 255) / 256 * 256;
-}
-
 extern "C" size_t mpx_linear_bwd_act8_workspace(int64_t M, int64_t N, int64_t K) {
-  if (M < 1 || N < 1 || K < 1) return 0;
-  return act8_values_offset(M, N, K) + (size_t)M * K * sizeof(uint16_t);
+  return mpx_linear_bwd_workspace(M, N, K);
 }
 
 extern "C" int mpx_linear_bwd_act8(const uint8_t* Xc, const uint8_t* Xs, const void* W, const void* dY,
@@ -329,35 +347,9 @@ extern "C" int mpx_linear_bwd_act8(const uint8_t* Xc, const uint8_t* Xs, const v
                                    void* workspace, size_t ws_bytes, int32_t* d_nonfinite,
                                    void* stream) {
   clear_error();
-  const char* fn = "mpx_linear_bwd_act8";
-  MPX_REQUIRE_FN(dY, "NULL dY");
-  MPX_REQUIRE_FN(dX || dW || db, "nothing to compute: dX, dW and db are all NULL");
-  MPX_REQUIRE_FN(!dX || W, "W is required for dX");
-  MPX_REQUIRE_FN(!dW || (Xc && Xs), "Xc and Xs are required for dW");
-  MPX_REQUIRE_FN(M >= 1 && N >= 1 && K >= 1, "M, N, K must be >= 1");
-  MPX_REQUIRE_FN(is_half(dt), "dt must be MPX_F16 or MPX_BF16");
-  MPX_REQUIRE_FN(x_act == MPX_ACT_NONE || x_act == MPX_ACT_GELU_TANH, "unknown activation");
-  const bool gelu = dX && x_act == MPX_ACT_GELU_TANH;
-  MPX_REQUIRE_FN(!gelu || (Pc && Ps), "Pc and Ps are required with x_act");
-  if (dW || db || gelu) {
-    const size_t need = mpx_linear_bwd_act8_workspace(M, N, K);
-    if (ws_bytes < need || !workspace) {
-      set_error(std::string(fn) + ": workspace of " + std::to_string(need) + " bytes required");
-      return MPX_ERR_WORKSPACE;
-    }
-  }
-  const size_t values = act8_values_offset(M, N, K);
-  uint16_t* H = (uint16_t*)((char*)workspace + values);
-  if (dX) {
-    if (gelu) MPX_HIP(launch_act8_unpack(Pc, Ps, H, K, M, K, dt, (hipStream_t)stream));
-    const int rc = linear_bwd(fn, nullptr, W, dY, gelu ? H : nullptr, x_act, dX, nullptr, nullptr, M, N, K,
-                              dt, nullptr, 0, nullptr, stream);
-    if (rc != MPX_OK) return rc;
-  }
-  if (!dW && !db) return MPX_OK;
-  if (dW) MPX_HIP(launch_act8_unpack(Xc, Xs, H, K, M, K, dt, (hipStream_t)stream));
-  return linear_bwd(fn, dW ? H : nullptr, nullptr, dY, nullptr, MPX_ACT_NONE, nullptr, dW, db, M, N, K, dt,
-                    workspace, values, d_nonfinite, stream);
+  const Act8Inputs a8 = {Xc, Xs, Pc, Ps};
+  return linear_bwd("mpx_linear_bwd_act8", nullptr, W, dY, nullptr, x_act, dX, dW, db, M, N, K, dt,
+                    workspace, ws_bytes, d_nonfinite, stream, &a8);
 }
 
 // ------------------------------------------- the variant that allocates nothing --

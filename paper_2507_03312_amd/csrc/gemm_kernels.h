@@ -61,16 +61,41 @@ struct GemmArgs {
   // reduction adds.
   uint16_t* db;
   float* dbp;
+  // 8-bit checkpoints (codes, and biased scale exponents per 32 rows of a column,
+  // both dense): in dact's place, of the output's shape; in B's place, with rows
+  // of ldb
+  const uint8_t *dact8, *dact8_scale, *b8, *b8_scale;
 };
 
 // Epilogue operations compiled into a kernel (a mask of these bits);
 // EPI_GENERIC takes them from the call's arguments, the same arithmetic step
 // for step.
-enum : int { EPI_BIAS = 1, EPI_GELU = 2, EPI_DACT = 4, EPI_RESID = 8, EPI_GENERIC = -1 };
+// EPI_DACT8 is EPI_DACT with the pre-activations from an 8-bit checkpoint: the
+// same values, hence the same results.
+enum : int { EPI_BIAS = 1, EPI_GELU = 2, EPI_DACT = 4, EPI_RESID = 8, EPI_DACT8 = 16, EPI_GENERIC = -1 };
 
 // 16 bytes at any 2-byte aligned address (one instruction: global accesses
 // need no alignment on gfx950)
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
+// 8 bytes (codes or scales of 8 columns of a checkpoint) at any address
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+
+// Value c (0..7) of 8 packed codes, and its scale: a code's value times its
+// scale is exactly a half value.
+__device__ __forceinline__ float act8_scale(u32x2 s, int c) {
+  return __builtin_bit_cast(float, ((s[c / 4] >> (8 * (c & 3))) & 0xFFu) << 23);
+}
+__device__ __forceinline__ float act8_value(u32x2 q, u32x2 s, int c) {
+  const uint32_t w = q[c / 4];
+  float v;
+  switch (c & 3) {  // the byte must be a constant
+    case 0: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 0); break;
+    case 1: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 1); break;
+    case 2: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 2); break;
+    default: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+  }
+  return v * act8_scale(s, c);
+}
 
 // Epilogue through LDS, for the transposed accumulator layout.  Step 1
 // (accumulator layout: lane = one row, runs of 4 consecutive columns):
@@ -112,6 +137,7 @@ __device__ __forceinline__ void gemm_epilogue_lds(const GemmArgs& g, const f32x1
   const bool do_dact = E == EPI_GENERIC ? g.dact != nullptr : (E & EPI_DACT) != 0;
   const bool do_res = E == EPI_GENERIC ? g.resid != nullptr : (E & EPI_RESID) != 0;
   const bool do_count = E == EPI_GENERIC && g.nonfinite != nullptr;
+  constexpr bool kDact8 = E != EPI_GENERIC && (E & EPI_DACT8) != 0;
   auto unpack = [](u32x2 w, float (&f)[4]) {
     f[0] = h2f<DT>((uint16_t)(w.x & 0xFFFFu));
     f[1] = h2f<DT>((uint16_t)(w.x >> 16));
@@ -200,6 +226,24 @@ __device__ __forceinline__ void gemm_epilogue_lds(const GemmArgs& g, const f32x1
       }
     }
   }
+  // the same of an 8-bit checkpoint: codes of every step, scales of every 32 rows
+  u32x2 op8[kDact8 ? STEPS : 1], sc8[kDact8 ? TM : 1];
+  if constexpr (kDact8) {
+    if (!EDGE || nv >= 8) {  // uniform
+      const uint8_t* src = g.dact8 + (mw * ldc + nw);
+      const uint8_t* scl = g.dact8_scale + ((mw / MPX_ACT8_GROUP) * ldc + nw);
+      const int c0 = EDGE ? min(c8, nv - 8) : c8;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) {
+        const int row = lane / LPR + RPT * t;
+        op8[t] = *reinterpret_cast<const u32x2_any*>(src + ((EDGE ? min(row, mv - 1) : row) * (int64_t)ldc + c0));
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+        sc8[i] = *reinterpret_cast<const u32x2_any*>(
+            scl + ((EDGE ? min(i, (mv - 1) / MPX_ACT8_GROUP) : i) * (int64_t)ldc + c0));
+    }
+  }
   asm volatile("" ::: "memory");  // the lanes' writes to LDS come before the wave's reads
   auto operand8 = [&](int t, const uint16_t* p, uint16_t (&h)[8]) {
     if (kOp && nc == 8) h8(op[kOp ? t : 0], h);
@@ -250,6 +294,22 @@ __device__ __forceinline__ void gemm_epilogue_lds(const GemmArgs& g, const f32x1
       operand8(t, dact + off, da);
 #pragma unroll
       for (int c = 0; c < 8; ++c) h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(h2f<DT>(da[c])));
+    }
+    if constexpr (kDact8) {
+      if (nc == 8) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(act8_value(op8[t], sc8[t * RPT / 32], c)));
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          if (c < nc) {
+            const int64_t at = (mw + row) * ldc + nw + c8 + c, sat = ((mw + row) / MPX_ACT8_GROUP) * ldc + nw + c8 + c;
+            const u32x2 q = {g.dact8[at], 0u}, s = {g.dact8_scale[sat], 0u};
+            h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(act8_value(q, s, 0)));
+          }
+        }
+      }
     }
     if (do_res) {
       uint16_t rv[8];
@@ -485,6 +545,93 @@ struct StagedOperand {
   }
 };
 
+// StagedOperand's mn-major form for an operand in 8 bits (codes [k][outputs]
+// with one scale byte per 32 k of an output): 8 codes and their 8 scales per
+// vector, widened to the half values on their way into LDS, where the tile lies
+// as the half operand's would.  A lane's vectors lie 16 or 32 k rows apart, so
+// two scale vectors serve a k tile of 64.
+template <int DT, int ROWS, int NWAVES, bool ANY>
+struct StagedAct8 {
+  static constexpr int BLOCKS = ROWS / 8, Q = BLOCKS / NWAVES;
+  static_assert(BLOCKS % NWAVES == 0, "blocks do not split evenly over the waves");
+  static constexpr int CH = ROWS / 8;
+  static constexpr int RSTEP = 64 / CH * NWAVES;
+  static_assert(32 % RSTEP == 0, "a vector's k rows do not tell its group");
+  u32x2 v[2][Q], sv[2][2];
+  uint32_t off[Q], soff;
+  int64_t ld;
+  int c8, r0, rv;
+  int krem[2];
+
+  __device__ __forceinline__ void init(int64_t ld_, int64_t left, int wave, int lane) {
+    ld = ld_;
+    rv = (int)min<int64_t>(left, 1 << 20);
+    r0 = 64 / CH * wave + lane / CH;
+    c8 = 8 * dma_chunk<ROWS, false>(r0, lane % CH);
+    soff = (uint32_t)max(min(c8, rv - 8), 0);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) off[q] = (uint32_t)((r0 + RSTEP * q) * ld) + soff;
+  }
+  // tile: its first code; stile: the first scale of its first group; kr:
+  // reduction values from there on (>= 1); past: as StagedOperand's
+  template <int P>
+  __device__ __forceinline__ void load(const uint8_t* tile, const uint8_t* stile, int kr, bool past) {
+    krem[P] = kr;
+    if constexpr (ANY) {
+      const int last = past ? 0 : rv - 1, last_row = past ? 0 : kr - 1;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const uint8_t* row = tile + (int64_t)min(r0 + RSTEP * q, last_row) * ld;
+        v[P][q] = u32x2{0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[P][q][e / 4] |= (uint32_t)row[min(c8 + e, last)] << (8 * (e & 3));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint8_t* row = stile + min(i, last_row / MPX_ACT8_GROUP) * ld;
+        sv[P][i] = u32x2{0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sv[P][i][e / 4] |= (uint32_t)row[min(c8 + e, last)] << (8 * (e & 3));
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        uint32_t o = off[q];
+        if (kr < 64) o -= (uint32_t)(max(0, r0 + RSTEP * q - (kr - 1)) * ld);  // uniform: the last k tile
+        if (past) o = (uint32_t)__builtin_amdgcn_readfirstlane((int)o);
+        v[P][q] = *reinterpret_cast<const u32x2_any*>(tile + o);
+      }
+      uint32_t so = soff;
+      if (past) so = (uint32_t)__builtin_amdgcn_readfirstlane((int)so);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        sv[P][i] = *reinterpret_cast<const u32x2_any*>(stile + (min(i, (kr - 1) / MPX_ACT8_GROUP) * ld + so));
+    }
+  }
+  template <int P>
+  __device__ __forceinline__ void store(uint8_t* lds, int wave, int lane) {
+    const bool whole = rv >= ROWS;
+    const int sh = c8 - min(c8, rv - 8);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const u32x2 s = sv[P][RSTEP * q / 32];
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = f2h<DT>(act8_value(v[P][q], s, 2 * e)) | ((uint32_t)f2h<DT>(act8_value(v[P][q], s, 2 * e + 1)) << 16);
+      if constexpr (ANY) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c8 + e >= rv) x[e / 2] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      } else {
+        if (!whole) x = StagedOperand<ROWS, false, NWAVES, false>::shr_halves(x, sh);
+      }
+      if (r0 + RSTEP * q >= krem[P]) x = u32x4{0u, 0u, 0u, 0u};
+      *reinterpret_cast<u32x4*>(lds + 1024 * (wave + NWAVES * q) + 16 * lane) = x;
+    }
+  }
+};
+
 // Per-lane LDS byte offsets of the MFMA fragments of one operand, for a
 // wave whose rows start at w0 within the tile (relative to the tile base).
 template <int ROWS, bool KMAJ, int T>
@@ -566,8 +713,9 @@ __device__ __forceinline__ float frag_sum8(const uint4& f) {
 // stage and the loads of tile kt + 3 are issued ahead of the MFMAs of tile kt,
 // so a load has two k tiles to land.  (One-value loads served these operands
 // before: 8415 x 768 x 588 in bf16 forward / dX / dW took 89 / 145 / 157 us.)
+// B8: operand B is an 8-bit checkpoint (register-staged kernels only).
 template <int DT, int BM, int BN, int WM, int WN, int OCC, bool AK, bool BKM, int E, bool DBS = false,
-          int STG = 0>
+          int STG = 0, bool B8 = false>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64)
 __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void gemm_tile_kernel(GemmArgs g) {
@@ -611,7 +759,10 @@ void gemm_tile_kernel(GemmArgs g) {
   const uint16_t* Ab = g.A + offA + (AK ? m0 * g.lda + kbeg : kbeg * g.lda + m0);
   const uint16_t* Bb = g.B + offB + (BKM ? n0 * g.ldb + kbeg : kbeg * g.ldb + n0);
   std::conditional_t<STG != 0, StagedOperand<BM, AK, NWAVES, STG == 2>, DmaOperand<BM, AK, NWAVES>> da;
-  std::conditional_t<STG != 0, StagedOperand<BN, BKM, NWAVES, STG == 2>, DmaOperand<BN, BKM, NWAVES>> db;
+  static_assert(!B8 || (STG != 0 && !BKM), "an 8-bit operand is staged, mn-major");
+  std::conditional_t<B8, StagedAct8<DT, BN, NWAVES, STG == 2>,
+                     std::conditional_t<STG != 0, StagedOperand<BN, BKM, NWAVES, STG == 2>,
+                                        DmaOperand<BN, BKM, NWAVES>>> db;
   if constexpr (STG != 0) {
     da.init(g.lda, g.M - m0, wave, lane);
     db.init(g.ldb, g.N - n0, wave, lane);
@@ -643,7 +794,10 @@ void gemm_tile_kernel(GemmArgs g) {
       kt = min(kt, nk - 1);
       const int krem = (int)min<int64_t>(kend - kbeg - 64 * (int64_t)kt, 1 << 20);
       da.template load<par>(Ab + (int64_t)kt * (AK ? 64 : 64 * g.lda), krem, past);
-      db.template load<par>(Bb + (int64_t)kt * (BKM ? 64 : 64 * g.ldb), krem, past);
+      if constexpr (B8)
+        db.template load<par>(g.b8 + ((kbeg + 64 * (int64_t)kt) * g.ldb + n0),
+                              g.b8_scale + ((kbeg + 64 * (int64_t)kt) / MPX_ACT8_GROUP * g.ldb + n0), krem, past);
+      else db.template load<par>(Bb + (int64_t)kt * (BKM ? 64 : 64 * g.ldb), krem, past);
     } else {
       const uint32_t st = lds0 + (uint32_t)((kt & 1) * STAGE);
       da.issue(reinterpret_cast<const uint16_t*>(reinterpret_cast<const uint8_t*>(Ab) + kt * da.step), st, wave);
@@ -891,7 +1045,7 @@ static int epilogue_mask(const GemmArgs& g) {
   if (g.splits > 1) return 0;
   if (g.nonfinite) return EPI_GENERIC;
   return (g.bias ? EPI_BIAS : 0) | (g.act == MPX_ACT_GELU_TANH ? EPI_GELU : 0) |
-         (g.dact ? EPI_DACT : 0) | (g.resid ? EPI_RESID : 0);
+         (g.dact ? EPI_DACT : 0) | (g.resid ? EPI_RESID : 0) | (g.dact8 ? EPI_DACT8 : 0);
 }
 
 // Whole-tile epilogue preconditions that do not depend on the tile: output,
@@ -928,6 +1082,7 @@ static bool full_epilogue_ok(const GemmArgs& g, int bm) {
       switch (e) {                                                           \
         case 0: MPX_K(true, false, 0, false); break;                         \
         case EPI_DACT: MPX_K(true, false, EPI_DACT, false); break;           \
+        case EPI_DACT8: MPX_K(true, false, EPI_DACT8, false); break;         \
         default: MPX_K(true, false, EPI_GENERIC, false);                     \
       }                                                                      \
     } else if constexpr (ALL_LAYOUTS) {                                      \
@@ -1055,7 +1210,7 @@ static int choose_tiles(const GemmArgs& g, int64_t nbatch) {
       {5, 128, 192, 2, {0.77, 0.83, 0}, {1.86, 4.49}},
       {3, 256, 256, 1, {1.08, 0, 0}, {7.36, 14.1}},
   };
-  const int second = g.pre || g.dact || g.resid ? 1 : 0;
+  const int second = g.pre || g.dact || g.dact8 || g.resid ? 1 : 0;
   const double nk = (double)(g.K / 64);
   int best = 7;
   double least = 0.0;
@@ -1141,7 +1296,7 @@ __global__ __launch_bounds__(256) void gemm_small_kernel(GemmArgs g, bool ak, bo
 }
 
 static bool small_ok(const GemmArgs& g, int64_t nbatch) {
-  return nbatch == 1 && g.splits == 1 && !g.pre && !g.dact && g.act == MPX_ACT_NONE &&
+  return nbatch == 1 && g.splits == 1 && !g.pre && !g.dact && !g.dact8 && g.act == MPX_ACT_NONE &&
          g.M * g.N <= ((int64_t)1 << 22);
 }
 
@@ -1185,6 +1340,46 @@ static hipError_t run_gemm(GemmArgs g, bool ak, bool bk, int64_t nbatch, hipStre
     default: return hipErrorInvalidValue;
   }
 }
+
+// C = A^T B of a weight gradient whose B is an 8-bit checkpoint (g.b8), register
+// staged: 64 x 64 or 128 x 128 tiles by choose_config's rule for such operands.
+template <int DT>
+static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused) {
+  const int64_t lim = ((int64_t)1 << 31) - 4096;
+  const bool any = g.M < 8 || g.N < 8 || g.lda * 256 >= lim || g.ldb * 64 >= lim;
+  const int64_t t64 = ((g.M + 63) / 64) * ((g.N + 63) / 64);
+  const bool small = any || g.M <= 64 || g.N <= 64 || (g.splits == 1 && t64 <= 512);
+  *db_fused = g.db && (!small || g.splits == 1);  // split partials are laid out for 128-wide tile columns
+  if (!*db_fused) {
+    g.db = nullptr;
+    g.dbp = nullptr;
+  }
+  const int b = small ? 64 : 128;
+  const dim3 grid((unsigned)(((g.M + b - 1) / b) * ((g.N + b - 1) / b)), (unsigned)g.splits);
+  g.full_epi = full_epilogue_ok(g, b) ? 1 : 0;
+#define MPX_K8(B, W, Ev, DBv, STGv) \
+  gemm_tile_kernel<DT, B, B, W, W, 2, false, false, Ev, DBv, STGv, true><<<grid, 256, 0, s>>>(g)
+#define MPX_K8_EPI(B, W, STGv)                                       \
+  do {                                                               \
+    const bool plain = epilogue_mask(g) == 0;                        \
+    if (g.db) {                                                      \
+      if (plain) MPX_K8(B, W, 0, true, STGv);                        \
+      else MPX_K8(B, W, EPI_GENERIC, true, STGv);                    \
+    } else {                                                         \
+      if (plain) MPX_K8(B, W, 0, false, STGv);                       \
+      else MPX_K8(B, W, EPI_GENERIC, false, STGv);                   \
+    }                                                                \
+  } while (0)
+  if (any) MPX_K8_EPI(64, 32, 2);
+  else if (small) MPX_K8_EPI(64, 32, 1);
+  else MPX_K8_EPI(128, 64, 1);
+#undef MPX_K8_EPI
+#undef MPX_K8
+  return hipGetLastError();
+}
+
+hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused);
+hipError_t run_gemm_act8_bf16(const GemmArgs& g, hipStream_t s, bool* db_fused);
 
 hipError_t run_gemm_f16(const GemmArgs& g, bool ak, bool bk, int64_t nbatch, hipStream_t s,
                         bool* db_fused = nullptr);
