@@ -18,8 +18,10 @@ static hipError_t gemm_dispatch(mpx_dtype dt, const GemmArgs& g, bool ak, bool b
                        : run_gemm_bf16(g, ak, bk, nbatch, s, db_fused);
 }
 
-static hipError_t gemm_dispatch_act8(mpx_dtype dt, const GemmArgs& g, hipStream_t s, bool* db_fused) {
-  return dt == MPX_F16 ? run_gemm_act8_f16(g, s, db_fused) : run_gemm_act8_bf16(g, s, db_fused);
+static hipError_t gemm_dispatch_act8(mpx_dtype dt, const GemmArgs& g, hipStream_t s, bool* db_fused,
+                                     int* db_width) {
+  return dt == MPX_F16 ? run_gemm_act8_f16(g, s, db_fused, db_width)
+                       : run_gemm_act8_bf16(g, s, db_fused, db_width);
 }
 
 static GemmArgs base_args() {
@@ -282,21 +284,23 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
       g.b8 = a8->Xc;
       g.b8_scale = a8->Xs;
     }
+    int db_width = 128;  // columns of dW that share a split's bias partials
     auto product = [&] {
-      return a8 ? gemm_dispatch_act8(dt, g, s, &db_fused) : gemm_dispatch(dt, g, false, false, 1, s, &db_fused);
+      return a8 ? gemm_dispatch_act8(dt, g, s, &db_fused, &db_width) : gemm_dispatch(dt, g, false, false, 1, s, &db_fused);
     };
     int sp;
     int64_t ks;
-    split_plan(N, K, M, !a8 && dma_ok(g, operands_aligned(g), false, false) ? kHalfCost : kHalfStagedCost, sp, ks);
+    const bool direct = a8 ? act8_dma_ok(g) : dma_ok(g, operands_aligned(g), false, false);
+    split_plan(N, K, M, direct ? kHalfCost : kHalfStagedCost, sp, ks);
     if (sp > 1) {
       g.splits = sp;
       g.k_split = ks;
       g.ws = (float*)workspace;
       g.dbp = db ? (float*)((char*)workspace + db_partials_offset(sp, N, K)) : nullptr;
       MPX_HIP(product());
-      // the GEMM wrote splits x (K / 128 tile columns) bias partials per row
+      // the GEMM wrote splits x (K / db_width tile columns) bias partials per row
       const int64_t MN = N * K, nrows = db_fused ? N : 0;
-      const int dbparts = (int)(db_partials_count(sp, N, K) / N);
+      const int dbparts = sp * (int)((K + db_width - 1) / db_width);
       // 4 outputs per thread wherever the rows allow (from 4 splits on only, as
       // before, the ViT-B step measured 1.5% slower: its MLP gradients have 3)
       const bool vec = splitk_reduce_vec(g.ws, MN, (const uint16_t*)dW);

@@ -1,10 +1,10 @@
-// Weight gradients from 8-bit checkpoints for float16 (see gemm_kernels.h).
-#include "gemm_kernels.h"
+// Weight gradients from 8-bit checkpoints for float16 (see gemm_act8.h).
+#include "gemm_act8.h"
 
 namespace mpx {
 
-hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused) {
-  return run_gemm_act8<MPX_F16>(g, s, db_fused);
+hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused, int* db_width) {
+  return run_gemm_act8<MPX_F16>(g, s, db_fused, db_width);
 }
 
 }  // namespace mpx

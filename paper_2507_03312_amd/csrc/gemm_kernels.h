@@ -1179,6 +1179,14 @@ static bool dma_ok(const GemmArgs& g, bool vec, bool ak, bool bk) {
   return spanA < lim && spanB < lim;
 }
 
+// What the direct copies of an 8-bit B (gemm_act8.h) need: 16-byte aligned operands, rows of whole 16-byte chunks,
+// 32-bit lane offsets.
+static bool act8_dma_ok(const GemmArgs& g) {
+  auto al16 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
+  const int64_t lim = (int64_t)1 << 31;
+  return al16(g.A) && al16(g.b8) && g.lda % 8 == 0 && g.ldb % 16 == 0 && g.lda * 128 < lim && g.ldb * 64 < lim;
+}
+
 static bool small_ok(const GemmArgs& g, int64_t nbatch);
 
 // Direct-to-LDS tiles for a k-major A, by estimated time.  A chip of 256 CUs
@@ -1341,45 +1349,8 @@ static hipError_t run_gemm(GemmArgs g, bool ak, bool bk, int64_t nbatch, hipStre
   }
 }
 
-// C = A^T B of a weight gradient whose B is an 8-bit checkpoint (g.b8), register
-// staged: 64 x 64 or 128 x 128 tiles by choose_config's rule for such operands.
-template <int DT>
-static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused) {
-  const int64_t lim = ((int64_t)1 << 31) - 4096;
-  const bool any = g.M < 8 || g.N < 8 || g.lda * 256 >= lim || g.ldb * 64 >= lim;
-  const int64_t t64 = ((g.M + 63) / 64) * ((g.N + 63) / 64);
-  const bool small = any || g.M <= 64 || g.N <= 64 || (g.splits == 1 && t64 <= 512);
-  *db_fused = g.db && (!small || g.splits == 1);  // split partials are laid out for 128-wide tile columns
-  if (!*db_fused) {
-    g.db = nullptr;
-    g.dbp = nullptr;
-  }
-  const int b = small ? 64 : 128;
-  const dim3 grid((unsigned)(((g.M + b - 1) / b) * ((g.N + b - 1) / b)), (unsigned)g.splits);
-  g.full_epi = full_epilogue_ok(g, b) ? 1 : 0;
-#define MPX_K8(B, W, Ev, DBv, STGv) \
-  gemm_tile_kernel<DT, B, B, W, W, 2, false, false, Ev, DBv, STGv, true><<<grid, 256, 0, s>>>(g)
-#define MPX_K8_EPI(B, W, STGv)                                       \
-  do {                                                               \
-    const bool plain = epilogue_mask(g) == 0;                        \
-    if (g.db) {                                                      \
-      if (plain) MPX_K8(B, W, 0, true, STGv);                        \
-      else MPX_K8(B, W, EPI_GENERIC, true, STGv);                    \
-    } else {                                                         \
-      if (plain) MPX_K8(B, W, 0, false, STGv);                       \
-      else MPX_K8(B, W, EPI_GENERIC, false, STGv);                   \
-    }                                                                \
-  } while (0)
-  if (any) MPX_K8_EPI(64, 32, 2);
-  else if (small) MPX_K8_EPI(64, 32, 1);
-  else MPX_K8_EPI(128, 64, 1);
-#undef MPX_K8_EPI
-#undef MPX_K8
-  return hipGetLastError();
-}
-
-hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused);
-hipError_t run_gemm_act8_bf16(const GemmArgs& g, hipStream_t s, bool* db_fused);
+hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused, int* db_width);
+hipError_t run_gemm_act8_bf16(const GemmArgs& g, hipStream_t s, bool* db_fused, int* db_width);
 
 hipError_t run_gemm_f16(const GemmArgs& g, bool ak, bool bk, int64_t nbatch, hipStream_t s,
                         bool* db_fused = nullptr);
