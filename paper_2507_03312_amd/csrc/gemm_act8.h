@@ -40,6 +40,17 @@ struct Act8Dma {
   }
 };
 
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 4 bytes per lane from base + off (bytes) into LDS at lds + 4 * lane
+__device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(lds)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 typedef int act8_v2i __attribute__((ext_vector_type(2)));
 
 // 8 codes of one output (ds_read_b64_tr_b8 transposes bytes across 16 lanes: lane
@@ -70,8 +81,10 @@ __device__ __forceinline__ uint4 act8_widen(u32x2 q, float s) {
 // ahead of its last k step) with B in 8 bits: B takes half the LDS and copies,
 // its fragments one transposing read each instead of two, and are widened in
 // registers by the instruction that takes a scale: a lane's 8 codes are 8 rows of
-// one column, so one group.  The scales (2 groups x TN columns per lane and k
-// tile) are loaded a whole k tile ahead.
+// one column, so one group.  A k tile's scales (2 groups of BN columns) come with
+// its copies, by one wave, and from LDS into registers (loaded by each lane for its
+// own columns they cost as many memory instructions as the codes: 65536 x 1024 x
+// 1024 bf16 192 us, 180 without any).
 //
 // Any reduction length: in the last k tile, rows behind the matrix read its last
 // row again, and A's are then zeroed in LDS by the wave that copied them (a code
@@ -83,11 +96,12 @@ void gemm_act8_kernel(GemmArgs g) {
   constexpr int NWAVES = (BM / WM) * (BN / WN);
   constexpr int TM = WM / 32, TN = WN / 32;
   constexpr int A_BYTES = BM * 64 * 2, B_BYTES = BN * 64;
-  constexpr int STAGE = A_BYTES + B_BYTES;
+  constexpr int STAGE = A_BYTES + B_BYTES, SCALES = 2 * BN;
+  static_assert(SCALES % 256 == 0, "whole copies of scales");
   constexpr int kReads = 2 * TM + TN;
   constexpr int EC = WN < 64 ? WN : 64;
   constexpr int EPI = NWAVES * WM * (EC + 4) * 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE > EPI ? 2 * STAGE : EPI];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * (STAGE + SCALES) > EPI ? 2 * (STAGE + SCALES) : EPI];
   const uint32_t lds0 = lds_u32(smem);
 
   const int tid = threadIdx.x;
@@ -111,10 +125,27 @@ void gemm_act8_kernel(GemmArgs g) {
   da.init(g.lda, (int)min<int64_t>(BM, g.M - m0), wave, lane);
   db.init(g.ldb, (int)min<int64_t>(BN, g.N - n0), wave, lane);
 
+  // scales of k tile kt: 2 groups of BN columns, in LDS behind both stages
+  const uint8_t* Sb = g.b8_scale + kbeg / MPX_ACT8_GROUP * g.ldb + n0;
+  const int groups = (int)((kend - kbeg + MPX_ACT8_GROUP - 1) / MPX_ACT8_GROUP);
+  const int scols = (int)min<int64_t>(BN, g.N - n0);
+  auto issue_scales = [&](int kt) {
+    const uint64_t p = reinterpret_cast<uint64_t>(Sb + (int64_t)2 * kt * g.ldb);
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+    const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+#pragma unroll
+    for (int q = 0; q < SCALES / 256; ++q) {
+      const int at = 256 * q + 4 * lane, c = at % BN;
+      const int gr = min(at / BN, groups - 1 - 2 * kt);
+      dma4(reinterpret_cast<const void*>(lo | (hi << 32)), (uint32_t)(gr * g.ldb + (c < scols ? c : 0)),
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + 2 * STAGE + (kt & 1) * SCALES + 256 * q)));
+    }
+  };
   auto issue = [&](int kt) {
     const uint32_t st = lds0 + (uint32_t)((kt & 1) * STAGE);
     const uint16_t* a = reinterpret_cast<const uint16_t*>(reinterpret_cast<const uint8_t*>(Ab) + kt * da.step);
     const uint8_t* b = Bb + (int64_t)kt * 64 * g.ldb;
+    if (wave == 0) issue_scales(kt);
     if (kt + 1 < nk || krest == 64) {  // uniform
       da.issue(a, st, wave);
       db.issue(b, st + A_BYTES, wave);
@@ -145,31 +176,6 @@ void gemm_act8_kernel(GemmArgs g) {
       if (kr >= krest) *reinterpret_cast<u32x4*>(st + 1024 * (wave + NWAVES * q) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
     }
   };
-  // scales of k tile kt: 2 groups of the lane's TN columns
-  const uint8_t* sbase = g.b8_scale + kbeg / MPX_ACT8_GROUP * g.ldb;
-  const int groups = (int)((kend - kbeg + MPX_ACT8_GROUP - 1) / MPX_ACT8_GROUP);
-  int64_t scol[TN];
-#pragma unroll
-  for (int j = 0; j < TN; ++j) scol[j] = min(n0 + wn0 + 32 * j + (lane & 31), g.N - 1);
-  uint32_t sraw[2][TN];
-  float sc[2][TN];
-  auto load_scales = [&](int kt) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sraw[i][j] = sbase[min(2 * kt + i, groups - 1) * g.ldb + scol[j]];
-  };
-  auto take_scales = [&] {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        // (the loads are older than the copies just waited for)
-        asm volatile("" : "+v"(sraw[i][j]));
-        sc[i][j] = __builtin_bit_cast(float, sraw[i][j] << 23);
-      }
-  };
-  load_scales(0);
   issue(0);
   if (nk > 1) issue(1);
 
@@ -200,12 +206,21 @@ void gemm_act8_kernel(GemmArgs g) {
 #pragma unroll
   for (int i = 0; i < TM; ++i) dbs[i] = 0.0f;
 
+  float sc[2][TN];
+  auto take_scales = [&](int kt) {
+    const uint8_t* s = smem + 2 * STAGE + (kt & 1) * SCALES + wn0 + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sc[i][j] = __builtin_bit_cast(float, (uint32_t)s[i * BN + 32 * j] << 23);
+  };
+
   constexpr int L = (DmaOperand<BM, false, NWAVES>::Q + Act8Dma<BN, NWAVES>::Q);
-  if (nk > 1) wait_vmcnt<L>();
+  if (nk > 1) wait_vmcnt<L>();  // the first wave has its scales' copies too: it waits for the second tile's
   else wait_vmcnt<0>();
-  take_scales();
   landed(0);
   __syncthreads();
+  take_scales(0);
 
   constexpr std::integral_constant<int, 0> I0{};
   constexpr std::integral_constant<int, 1> I1{};
@@ -241,7 +256,6 @@ void gemm_act8_kernel(GemmArgs g) {
     const uint32_t sn = lds0 + (uint32_t)(((kt + 1) & 1) * STAGE);
     const bool db_now = dbw && kt == db_next;
     if (db_now) db_next += db_cols;
-    load_scales(min(kt + 1, nk - 1));
     read(I1, I1, sa);
     multiply(I0, db_now);
     widen(I1, I1);
@@ -251,11 +265,11 @@ void gemm_act8_kernel(GemmArgs g) {
     read(I1, I3, sa);
     multiply(I0, db_now);
     widen(I1, I3);
-    wait_vmcnt<0>();  // k tile kt + 1 and its scales
-    take_scales();
     if (kt + 1 < nk) {
+      wait_vmcnt<0>();  // k tile kt + 1 has landed
       landed(kt + 1);
       __syncthreads();
+      take_scales(kt + 1);
       if (kt + 2 < nk) issue(kt + 2);
       read(I0, I0, sn);
     }
