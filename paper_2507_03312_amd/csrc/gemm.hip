@@ -18,10 +18,9 @@ static hipError_t gemm_dispatch(mpx_dtype dt, const GemmArgs& g, bool ak, bool b
                        : run_gemm_bf16(g, ak, bk, nbatch, s, db_fused);
 }
 
-static hipError_t gemm_dispatch_act8(mpx_dtype dt, const GemmArgs& g, hipStream_t s, bool* db_fused,
-                                     int* db_width) {
-  return dt == MPX_F16 ? run_gemm_act8_f16(g, s, db_fused, db_width)
-                       : run_gemm_act8_bf16(g, s, db_fused, db_width);
+static hipError_t gemm_dispatch_act8(mpx_dtype dt, const GemmArgs& g, hipStream_t s, bool* db_fused) {
+  return dt == MPX_F16 ? run_gemm_act8_f16(g, s, db_fused)
+                       : run_gemm_act8_bf16(g, s, db_fused);
 }
 
 static GemmArgs base_args() {
@@ -97,6 +96,43 @@ static void split_plan(int64_t N, int64_t K, int64_t Mr, SplitCost c, int& sp, i
   sp = choose_splits(N, K, Mr, c);
   k_split = ((Mr + sp - 1) / sp + 63) / 64 * 64;
   sp = (int)((Mr + k_split - 1) / k_split);
+}
+
+// Tile height and splits of a weight gradient from an 8-bit checkpoint with
+// direct copies: 64 x 128 tiles, four workgroups per CU, or 128 x 128 ones, two, by
+// estimated time.  A round of o workgroups per CU takes its k tiles x k_us[o - 1]
+// plus tile_us; partials cost 2.5 us per million outputs and split (what they cost
+// beside other work; alone less).  Constants of least loss on 70% of 158 measured
+// gradients (100 to 60000 rows, 128 to 3200 outputs a side, every height and
+// split count timed): on the others the choice is 0.3% slower than the fastest,
+// 64-high tiles alone at least 1.6%, 128-high ones 14%.  Examples (us, 64 / 128
+// high, each with its best split count): 1000 x 768 x 768 13 / 18, 2100 x 640 x 512
+// 16 / 20, 16640 x 384 x 1536 38 / 38, 12608 x 2304 x 768 83 / 69.
+static void act8_plan(int64_t N, int64_t K, int64_t Mr, int& rows, int& sp, int64_t& k_split) {
+  struct Cost {
+    int rows, per_cu;
+    double k_us[4], tile_us;
+  };
+  static const Cost costs[] = {{64, 4, {0.67, 0.72, 0.80, 1.32}, 2.6}, {128, 2, {0.72, 0.80, 0, 0}, 2.9}};
+  const int64_t most = most_splits(N, K, Mr);
+  double least = 0.0;
+  for (const Cost& c : costs) {
+    const int64_t tiles = cdiv(N, c.rows) * cdiv(K, 128), slots = 256 * c.per_cu;
+    for (int64_t s = 1; s <= most; ++s) {
+      const double nk = (double)cdiv(Mr, 64 * s);
+      const int64_t full = tiles * s / slots, last = cdiv(tiles * s % slots, 256);
+      const double t = (double)full * (nk * c.k_us[c.per_cu - 1] + c.tile_us) +
+                       (last ? nk * c.k_us[last - 1] + c.tile_us : 0.0) +
+                       (s > 1 ? 0.34 + 2.5e-6 * (double)(s * N * K) : 0.0);
+      if (least == 0.0 || t < least) {
+        least = t;
+        rows = c.rows;
+        sp = (int)s;
+      }
+    }
+  }
+  k_split = cdiv(cdiv(Mr, sp), 64) * 64;
+  sp = (int)cdiv(Mr, k_split);
 }
 
 static GemmF32Args f32_args() {
@@ -284,23 +320,25 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
       g.b8 = a8->Xc;
       g.b8_scale = a8->Xs;
     }
-    int db_width = 128;  // columns of dW that share a split's bias partials
     auto product = [&] {
-      return a8 ? gemm_dispatch_act8(dt, g, s, &db_fused, &db_width) : gemm_dispatch(dt, g, false, false, 1, s, &db_fused);
+      return a8 ? gemm_dispatch_act8(dt, g, s, &db_fused) : gemm_dispatch(dt, g, false, false, 1, s, &db_fused);
     };
     int sp;
     int64_t ks;
-    const bool direct = a8 ? act8_dma_ok(g) : dma_ok(g, operands_aligned(g), false, false);
-    split_plan(N, K, M, direct ? kHalfCost : kHalfStagedCost, sp, ks);
+    if (a8 && act8_dma_ok(g))
+      act8_plan(N, K, M, g.act8_rows, sp, ks);
+    else
+      split_plan(N, K, M, !a8 && dma_ok(g, operands_aligned(g), false, false) ? kHalfCost : kHalfStagedCost, sp,
+                 ks);
     if (sp > 1) {
       g.splits = sp;
       g.k_split = ks;
       g.ws = (float*)workspace;
       g.dbp = db ? (float*)((char*)workspace + db_partials_offset(sp, N, K)) : nullptr;
       MPX_HIP(product());
-      // the GEMM wrote splits x (K / db_width tile columns) bias partials per row
+      // the GEMM wrote splits x (K / 128 tile columns) bias partials per row
       const int64_t MN = N * K, nrows = db_fused ? N : 0;
-      const int dbparts = sp * (int)((K + db_width - 1) / db_width);
+      const int dbparts = (int)(db_partials_count(sp, N, K) / N);
       // 4 outputs per thread wherever the rows allow (from 4 splits on only, as
       // before, the ViT-B step measured 1.5% slower: its MLP gradients have 3)
       const bool vec = splitk_reduce_vec(g.ws, MN, (const uint16_t*)dW);

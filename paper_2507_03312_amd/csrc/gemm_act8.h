@@ -7,25 +7,21 @@
 
 namespace mpx {
 
-// Codes [64 k][BN] of one stage, 16-byte chunks permuted so that the 8 rows x 2
+// Codes [64 k][128] of one stage, 16-byte chunks permuted so that the 8 rows x 2
 // chunks which 32 lanes of a transposing read touch lie in 16 different 16-byte
-// columns of the 256 bytes of banks.
-template <int BN>
-__device__ __forceinline__ int act8_chunk(int r, int c) {
-  static_assert(BN == 128 || BN == 256, "rows of half or all banks");
-  return BN == 128 ? c ^ (2 * ((r >> 1) & 3)) : c ^ (2 * (r & 7));
-}
+// columns of the 256 bytes of banks (a row spans half of them).
+__device__ __forceinline__ int act8_chunk(int r, int c) { return c ^ (2 * ((r >> 1) & 3)); }
 
-template <int BN, int NWAVES>
+template <int NWAVES>
 struct Act8Dma {
-  static constexpr int CH = BN / 16, Q = BN / 16 / NWAVES;
-  static_assert(BN / 16 % NWAVES == 0, "copies do not split evenly over the waves");
+  static constexpr int CH = 8, Q = 8 / NWAVES;
+  static_assert(8 % NWAVES == 0, "copies do not split evenly over the waves");
   uint32_t off[Q];
   // rv: outputs (a multiple of 16) of the matrix from the tile's first on; ld: bytes
   __device__ __forceinline__ void init(int64_t ld, int rv, int wave, int lane) {
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const int at = 64 * (wave + NWAVES * q) + lane, kr = at / CH, c = act8_chunk<BN>(kr, at % CH);
+      const int at = 64 * (wave + NWAVES * q) + lane, kr = at / CH, c = act8_chunk(kr, at % CH);
       off[q] = (uint32_t)(kr * ld + (16 * c < rv ? 16 * c : 0));
     }
   }
@@ -91,13 +87,13 @@ __device__ __forceinline__ uint4 act8_widen(u32x2 q, float s) {
 // of that row can be NaN only where its column's sum is NaN anyway).
 template <int DT, int BM, int BN, int WM, int WN, int E, bool DBS>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64)
-__attribute__((amdgpu_waves_per_eu(2, 2)))
+__attribute__((amdgpu_waves_per_eu(BM == 64 ? 4 : 2, BM == 64 ? 4 : 2)))
 void gemm_act8_kernel(GemmArgs g) {
   constexpr int NWAVES = (BM / WM) * (BN / WN);
   constexpr int TM = WM / 32, TN = WN / 32;
   constexpr int A_BYTES = BM * 64 * 2, B_BYTES = BN * 64;
   constexpr int STAGE = A_BYTES + B_BYTES, SCALES = 2 * BN;
-  static_assert(SCALES % 256 == 0, "whole copies of scales");
+  static_assert(BN == 128, "act8_chunk, and one copy of scales");
   constexpr int kReads = 2 * TM + TN;
   constexpr int EC = WN < 64 ? WN : 64;
   constexpr int EPI = NWAVES * WM * (EC + 4) * 2;
@@ -121,7 +117,7 @@ void gemm_act8_kernel(GemmArgs g) {
   const uint16_t* Ab = g.A + kbeg * g.lda + m0;
   const uint8_t* Bb = g.b8 + kbeg * g.ldb + n0;
   DmaOperand<BM, false, NWAVES> da;
-  Act8Dma<BN, NWAVES> db;
+  Act8Dma<NWAVES> db;
   da.init(g.lda, (int)min<int64_t>(BM, g.M - m0), wave, lane);
   db.init(g.ldb, (int)min<int64_t>(BN, g.N - n0), wave, lane);
 
@@ -133,13 +129,9 @@ void gemm_act8_kernel(GemmArgs g) {
     const uint64_t p = reinterpret_cast<uint64_t>(Sb + (int64_t)2 * kt * g.ldb);
     const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
     const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
-#pragma unroll
-    for (int q = 0; q < SCALES / 256; ++q) {
-      const int at = 256 * q + 4 * lane, c = at % BN;
-      const int gr = min(at / BN, groups - 1 - 2 * kt);
-      dma4(reinterpret_cast<const void*>(lo | (hi << 32)), (uint32_t)(gr * g.ldb + (c < scols ? c : 0)),
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + 2 * STAGE + (kt & 1) * SCALES + 256 * q)));
-    }
+    const int c = 4 * lane % BN, gr = min(4 * lane / BN, groups - 1 - 2 * kt);
+    dma4(reinterpret_cast<const void*>(lo | (hi << 32)), (uint32_t)(gr * g.ldb + (c < scols ? c : 0)),
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + 2 * STAGE + (kt & 1) * SCALES)));
   };
   auto issue = [&](int kt) {
     const uint32_t st = lds0 + (uint32_t)((kt & 1) * STAGE);
@@ -188,7 +180,7 @@ void gemm_act8_kernel(GemmArgs g) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int c = (wn0 + 32 * j) / 16 + (gq & 1);
-      fb[j] = (uint32_t)(kr * BN + act8_chunk<BN>(kr, c) * 16 + 8 * (i & 1));
+      fb[j] = (uint32_t)(kr * BN + act8_chunk(kr, c) * 16 + 8 * (i & 1));
     }
   }
   f32x16 acc[TM][TN];
@@ -215,7 +207,7 @@ void gemm_act8_kernel(GemmArgs g) {
       for (int j = 0; j < TN; ++j) sc[i][j] = __builtin_bit_cast(float, (uint32_t)s[i * BN + 32 * j] << 23);
   };
 
-  constexpr int L = (DmaOperand<BM, false, NWAVES>::Q + Act8Dma<BN, NWAVES>::Q);
+  constexpr int L = (DmaOperand<BM, false, NWAVES>::Q + Act8Dma<NWAVES>::Q);
   if (nk > 1) wait_vmcnt<L>();  // the first wave has its scales' copies too: it waits for the second tile's
   else wait_vmcnt<0>();
   landed(0);
@@ -316,64 +308,46 @@ void gemm_act8_kernel(GemmArgs g) {
   });
 }
 
-template <int DT, int BN>
-static void launch_act8_tiles(const GemmArgs& g, hipStream_t s) {
-  const dim3 grid((unsigned)(((g.M + 127) / 128) * ((g.N + BN - 1) / BN)), (unsigned)g.splits);
-  const bool plain = epilogue_mask(g) == 0;
-#define MPX_K8(Ev, DBv) gemm_act8_kernel<DT, 128, BN, 64, BN / 2, Ev, DBv><<<grid, 256, 0, s>>>(g)
-  if (g.db) {
-    if (plain) MPX_K8(0, true);
-    else MPX_K8(EPI_GENERIC, true);
-  } else {
-    if (plain) MPX_K8(0, false);
-    else MPX_K8(EPI_GENERIC, false);
-  }
-#undef MPX_K8
-}
-
 // C = A^T B of a weight gradient whose B is an 8-bit checkpoint (g.b8): direct
-// tiles where the operands allow, else register-staged ones of 64 x 64 or 128 x 128
-// by choose_config's rule for such operands.  *db_width: columns of C that share
-// a split's bias partials.
+// tiles of g.act8_rows x 128 (chosen with the splits, act8_plan), or, where that is
+// 0, register-staged ones of 64 x 64 or 128 x 128 by choose_config's rule for such
+// operands.
 template <int DT>
-static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused, int* db_width) {
+static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused) {
   const int64_t lim = ((int64_t)1 << 31) - 4096;
   const bool any = g.M < 8 || g.N < 8 || g.lda * 256 >= lim || g.ldb * 64 >= lim;
-  const bool direct = act8_dma_ok(g);
   const int64_t t64 = ((g.M + 63) / 64) * ((g.N + 63) / 64);
-  const bool small = any || g.M <= 64 || g.N <= 64 || (g.splits == 1 && t64 <= 512);
+  const bool small = !g.act8_rows && (any || g.M <= 64 || g.N <= 64 || (g.splits == 1 && t64 <= 512));
   *db_fused = g.db && (!small || g.splits == 1);  // split partials are laid out for 128-wide tile columns
   if (!*db_fused) {
     g.db = nullptr;
     g.dbp = nullptr;
   }
-  *db_width = 128;
-  if (direct && !small) {
-    g.full_epi = full_epilogue_ok(g, 128) ? 1 : 0;
-    launch_act8_tiles<DT, 128>(g, s);
-    return hipGetLastError();
-  }
-  const int b = small ? 64 : 128;
-  const dim3 grid((unsigned)(((g.M + b - 1) / b) * ((g.N + b - 1) / b)), (unsigned)g.splits);
-  g.full_epi = full_epilogue_ok(g, b) ? 1 : 0;
-#define MPX_K8(B, W, Ev, DBv, STGv) \
+  const int bm = g.act8_rows ? g.act8_rows : small ? 64 : 128, bn = small ? 64 : 128;
+  const dim3 grid((unsigned)(((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn)), (unsigned)g.splits);
+  g.full_epi = full_epilogue_ok(g, bm) ? 1 : 0;
+#define MPX_K8_STAGED(B, W, STGv, Ev, DBv) \
   gemm_tile_kernel<DT, B, B, W, W, 2, false, false, Ev, DBv, STGv, true><<<grid, 256, 0, s>>>(g)
-#define MPX_K8_EPI(B, W, STGv)                                       \
-  do {                                                               \
-    const bool plain = epilogue_mask(g) == 0;                        \
-    if (g.db) {                                                      \
-      if (plain) MPX_K8(B, W, 0, true, STGv);                        \
-      else MPX_K8(B, W, EPI_GENERIC, true, STGv);                    \
-    } else {                                                         \
-      if (plain) MPX_K8(B, W, 0, false, STGv);                       \
-      else MPX_K8(B, W, EPI_GENERIC, false, STGv);                   \
-    }                                                                \
+#define MPX_K8_DIRECT(B, W, STGv, Ev, DBv) gemm_act8_kernel<DT, B, 128, W, 64, Ev, DBv><<<grid, 256, 0, s>>>(g)
+#define MPX_K8_EPI(KERNEL, B, W, STGv)                     \
+  do {                                                     \
+    const bool plain = epilogue_mask(g) == 0;              \
+    if (g.db) {                                            \
+      if (plain) KERNEL(B, W, STGv, 0, true);              \
+      else KERNEL(B, W, STGv, EPI_GENERIC, true);          \
+    } else {                                               \
+      if (plain) KERNEL(B, W, STGv, 0, false);             \
+      else KERNEL(B, W, STGv, EPI_GENERIC, false);         \
+    }                                                      \
   } while (0)
-  if (any) MPX_K8_EPI(64, 32, 2);
-  else if (small) MPX_K8_EPI(64, 32, 1);
-  else MPX_K8_EPI(128, 64, 1);
+  if (g.act8_rows == 64) MPX_K8_EPI(MPX_K8_DIRECT, 64, 32, 0);
+  else if (g.act8_rows) MPX_K8_EPI(MPX_K8_DIRECT, 128, 64, 0);
+  else if (any) MPX_K8_EPI(MPX_K8_STAGED, 64, 32, 2);
+  else if (small) MPX_K8_EPI(MPX_K8_STAGED, 64, 32, 1);
+  else MPX_K8_EPI(MPX_K8_STAGED, 128, 64, 1);
 #undef MPX_K8_EPI
-#undef MPX_K8
+#undef MPX_K8_DIRECT
+#undef MPX_K8_STAGED
   return hipGetLastError();
 }
 

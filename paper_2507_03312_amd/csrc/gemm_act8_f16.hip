@@ -3,8 +3,8 @@
 
 namespace mpx {
 
-hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused, int* db_width) {
-  return run_gemm_act8<MPX_F16>(g, s, db_fused, db_width);
+hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused) {
+  return run_gemm_act8<MPX_F16>(g, s, db_fused);
 }
 
 }  // namespace mpx

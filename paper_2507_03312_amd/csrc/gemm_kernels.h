@@ -65,6 +65,7 @@ struct GemmArgs {
   // both dense): in dact's place, of the output's shape; in B's place, with rows
   // of ldb
   const uint8_t *dact8, *dact8_scale, *b8, *b8_scale;
+  int32_t act8_rows;  // tile height of the direct kernels of an 8-bit B; 0: staged
 };
 
 // Epilogue operations compiled into a kernel (a mask of these bits);
@@ -1349,8 +1350,8 @@ static hipError_t run_gemm(GemmArgs g, bool ak, bool bk, int64_t nbatch, hipStre
   }
 }
 
-hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused, int* db_width);
-hipError_t run_gemm_act8_bf16(const GemmArgs& g, hipStream_t s, bool* db_fused, int* db_width);
+hipError_t run_gemm_act8_f16(const GemmArgs& g, hipStream_t s, bool* db_fused);
+hipError_t run_gemm_act8_bf16(const GemmArgs& g, hipStream_t s, bool* db_fused);
 
 hipError_t run_gemm_f16(const GemmArgs& g, bool ak, bool bk, int64_t nbatch, hipStream_t s,
                         bool* db_fused = nullptr);

@@ -130,7 +130,8 @@ def _run(fmt, M, N, K, x, pre, w, dy, act, want="xwb", off=0, counter=True):
 
 SHAPES = [(1, 1, 1), (1, 64, 128), (5, 3, 9), (31, 64, 64), (33, 128, 128), (64, 512, 1024), (65, 40, 24),
           (128, 10, 384), (257, 136, 144), (1000, 96, 588), (2048, 768, 384), (2500, 200, 136),
-          (4097, 72, 264), (8320, 384, 256)]
+          (4097, 72, 264), (8320, 384, 256), (63, 64, 128), (65, 72, 144), (97, 8, 16), (2049, 64, 16),
+          (1537, 136, 400), (4099, 200, 272), (5000, 1032, 48), (2056, 2056, 1040)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
