@@ -35,6 +35,17 @@ template <int DT, int N> struct RopeVec {
   T v[N];
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
   __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, v, sizeof(v)); }
+  // the same vector of another lane
+  __device__ __forceinline__ RopeVec from_lane(int l) const {
+    constexpr int W = (sizeof(v) + 3) / 4;
+    int w[W] = {};
+    __builtin_memcpy(w, v, sizeof(v));
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = __builtin_amdgcn_ds_bpermute(4 * l, w[i]);
+    RopeVec o;
+    __builtin_memcpy(o.v, w, sizeof(v));
+    return o;
+  }
   __device__ __forceinline__ float get(int i) const {
     if constexpr (DT == MPX_F32) return v[i];
     else return h2f<DT>(v[i]);
@@ -45,24 +56,14 @@ template <int DT, int N> struct RopeVec {
   }
 };
 
-// Bound by HBM (every value read and written once).  The turns are as many as
-// rows x pairs, far fewer than the values, but dear (float64 angles): a
-// workgroup makes each of its rows' once, into LDS, while the copied heads
-// stream; every thread then keeps the turns of its VW pairs in registers and goes
-// through the heads, two vectors of VW values from each, four heads in flight.
-// VW pairs lie in two runs of VW values (halves), or in one of 2 VW
-// (interleaved).  Values behind the sections count as pairs that are not turned;
-// a head of odd length has one more (VW == 1 then).
-template <int DT, int VW, bool INTER>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+// What both kernels begin with: the copied heads of the workgroup's rows (COPY),
+// and their turns into LDS.
+template <int DT, bool COPY>
+__device__ __forceinline__ void rope_copies_and_turns(const RopeArgs& a, const typename RopeValue<DT>::type* X,
+                                                      typename RopeValue<DT>::type* Y, uint32_t row0,
+                                                      uint32_t nrows, float2* turns) {
   typedef typename RopeValue<DT>::type T;
-  __shared__ float2 turns[kRopeTable];
-  const uint32_t row0 = blockIdx.x * a.wg_rows;
-  const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
-  T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
-  const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
-
-  if (!a.in_place && a.copy) {
+  if (COPY && !a.in_place && a.copy) {
     constexpr uint32_t VE = 16 / sizeof(T);
     const int64_t w0 = (int64_t)a.heads_rot * a.hd;
     const uint32_t nv = a.copy / VE, rest = a.copy % VE;
@@ -90,6 +91,109 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     turns[i] = make_float2(c, a.back ? -s : s);
   }
   __syncthreads();
+}
+
+// Bound by HBM (every value read and written once).  The turns are as many as
+// rows x pairs, far fewer than the values, but dear (float64 angles): a
+// workgroup makes each of its rows' once, into LDS, while the copied heads
+// stream; every thread then keeps the turns of its VW values in registers and goes
+// through the heads, one run of VW values from each, four heads in flight.  A
+// value's partner lies in the same run (interleaved) or comes from the lane that
+// has it (halves): y = x c + partner s, s negative in a section's first half.
+// Values behind the sections count as pairs that are not turned.  The lanes of a
+// head lie in one wave (a.chunks <= 64 runs).
+template <int DT, int VW, bool INTER>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  typedef typename RopeValue<DT>::type T;
+  __shared__ float2 turns[kRopeTable];
+  const uint32_t row0 = blockIdx.x * a.wg_rows;
+  const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
+  T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
+  const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
+  // runs of 16 bytes also serve the copied heads, like turned ones (a loop of
+  // their own: 12608 x 36 heads of 64 bf16 28.6 us)
+  constexpr bool kWide = VW * sizeof(T) == 16;
+  rope_copies_and_turns<DT, !kWide>(a, X, Y, row0, nrows, turns);
+
+  const int lane = threadIdx.x & 63;
+  const uint32_t chunk = lane % a.chunks, wave_slots = 64 / a.chunks;
+  const uint32_t slot = (threadIdx.x >> 6) * wave_slots + lane / a.chunks;
+  const uint32_t r = slot / a.head_slots, h0 = slot % a.head_slots;
+  if ((uint32_t)lane >= wave_slots * a.chunks || r >= nrows) return;  // all lanes of a head or none
+  const int v0 = chunk * VW;  // the thread's first value
+  const bool turned = v0 < 2 * a.npairs;
+  int p0 = v0 / 2, partner = lane;  // its first pair, the lane of its partners
+  bool second = false;
+  if (!INTER && turned) {
+    int first = 0, n = a.first_pair[1];
+#pragma unroll
+    for (int k = 1; k < MPX_ROPE_MAX_AXES; ++k) {
+      if (v0 >= 2 * a.first_pair[k]) {
+        first = a.first_pair[k];
+        n = a.first_pair[k + 1] - first;
+      }
+    }
+    second = v0 - 2 * first >= n;
+    p0 = v0 - first - (second ? n : 0);
+    partner = lane + (second ? -n : n) / VW;
+  }
+  constexpr int NP = INTER ? VW / 2 : VW;  // pairs the thread has a part in
+  float c[NP], s[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const float2 t = turned ? turns[r * a.npairs + p0 + i] : make_float2(1.0f, 0.0f);
+    c[i] = t.x;
+    s[i] = INTER || second ? t.y : -t.y;
+  }
+  const T* x = X + r * a.ldx + v0;
+  T* y = Y + r * a.ldy + v0;
+  const uint32_t heads = a.heads_rot + (kWide && !a.in_place ? a.copy / a.hd : 0);
+  constexpr int U = 4;
+  for (uint32_t h = h0; h < heads; h += U * a.head_slots) {
+    RopeVec<DT, VW> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u].load(x + (int64_t)min(h + u * a.head_slots, heads - 1) * a.hd);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (h + u * a.head_slots >= heads) break;
+      const bool turn = turned && (!kWide || h + u * a.head_slots < a.heads_rot);
+      T* p = y + (int64_t)(h + u * a.head_slots) * a.hd;
+      if constexpr (INTER) {
+        if (turn) {
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const float x0 = v[u].get(2 * i), x1 = v[u].get(2 * i + 1);
+            v[u].set(2 * i, __builtin_fmaf(x0, c[i], -(x1 * s[i])));
+            v[u].set(2 * i + 1, __builtin_fmaf(x1, c[i], x0 * s[i]));
+          }
+        }
+      } else {
+        const RopeVec<DT, VW> o = v[u].from_lane(partner);
+        if (turn) {
+#pragma unroll
+          for (int i = 0; i < NP; ++i) v[u].set(i, __builtin_fmaf(v[u].get(i), c[i], o.get(i) * s[i]));
+        }
+      }
+      if (turn || !a.in_place) v[u].store(p);
+    }
+  }
+}
+
+// Heads of more than 64 runs (long ones whose sections allow only short runs), or
+// of runs of one value: a thread takes both runs of VW pairs, so that nothing
+// passes between lanes (8192 rows of 36 heads of 64 bf16 in sections of 11, 4, 1
+// and 16 pairs 19.6 us; values passed one by one 23.1).  A head of odd length has
+// one value more (VW == 1 then).
+template <int DT, int VW, bool INTER>
+__global__ __launch_bounds__(256) void rope_pairs_kernel(RopeArgs a) {
+  typedef typename RopeValue<DT>::type T;
+  __shared__ float2 turns[kRopeTable];
+  const uint32_t row0 = blockIdx.x * a.wg_rows;
+  const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
+  T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
+  const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
+
+  rope_copies_and_turns<DT, true>(a, X, Y, row0, nrows, turns);
 
   const uint32_t chunk = threadIdx.x % a.chunks, slot = threadIdx.x / a.chunks;
   const uint32_t r = slot / a.head_slots, h0 = slot % a.head_slots;
@@ -169,9 +273,18 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 }
 
 template <int DT, int VW>
-static void launch_rope(const RopeArgs& a, unsigned blocks, hipStream_t s) {
-  if (a.interleaved) rope_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
-  else rope_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
+static void launch_rope(const RopeArgs& a, bool pairs, unsigned blocks, hipStream_t s) {
+  if constexpr (VW <= 4) {  // 512 values make at most 64 runs of 8
+    if (pairs) {
+      if (a.interleaved) rope_pairs_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
+      else rope_pairs_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
+      return;
+    }
+  }
+  if constexpr (VW > 1) {
+    if (a.interleaved) rope_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
+    else rope_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
+  }
 }
 
 static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, int64_t ldy,
@@ -202,9 +315,11 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
                  "pointers must be aligned to their element");
   RopeArgs a{};
   int64_t n = 0;
-  // pairs of one vector: a power of two that divides every section, also that of
-  // the values that are not turned, of at most 16 bytes a run
-  int vw = hd % 2 ? 1 : dt == MPX_F32 ? 4 : 8;
+  // Values of one run: a power of two, at most 16 bytes, that divides every
+  // section's halves (interleaved: twice the pairs), and what is not turned.
+  const bool inter = plan->interleaved != 0;
+  const int wide = dt == MPX_F32 ? 4 : 8;
+  int vw = wide, vp = hd % 2 ? 1 : wide;  // of the kernel of runs, and of pairs of runs
   for (int ax = 0; ax < plan->axes; ++ax) {
     const int64_t p = plan->pairs[ax];
     const double base = plan->base[ax];
@@ -213,9 +328,13 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
     a.step[ax] = std::log2(base) / (double)p;
     a.first_pair[ax] = (int32_t)n;
     n += p;
-    while (!plan->interleaved && p % vw) vw /= 2;
+    while (!inter && p % vw) vw /= 2;
+    while (!inter && p % vp) vp /= 2;
   }
-  while (n % vw || (hd / 2 - n) % vw) vw /= 2;
+  while (2 * n % vw || (hd - 2 * n) % vw) vw /= 2;
+  while (n % vp || (hd / 2 - n) % vp) vp /= 2;
+  const bool pairs = hd / vw > 64 || vw == 1;
+  if (pairs) vw = vp;
   for (int ax = plan->axes; ax <= MPX_ROPE_MAX_AXES; ++ax) a.first_pair[ax] = (int32_t)n;
   a.X = X;
   a.Y = Y;
@@ -230,11 +349,11 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
   a.interleaved = plan->interleaved;
   a.back = back ? 1 : 0;
   a.in_place = X == Y ? 1 : 0;
-  a.chunks = (int32_t)(hd / 2) / vw;
+  a.chunks = (int32_t)(pairs ? hd / 2 : hd) / vw;
   // Rows of a workgroup: about four heads to a thread where the rows suffice for
   // 1024 workgroups, never more turns than the table holds.
-  const int64_t slots = 256 / a.chunks;
-  int64_t wg_rows = std::min<int64_t>({4 * slots / heads_rot, slots, kRopeTable / n, rows / 1024});
+  const int64_t slots = pairs ? 256 / a.chunks : 4 * (64 / a.chunks);
+  int64_t wg_rows = std::min<int64_t>({4 * slots / (heads_rot + (a.in_place ? 0 : heads_copy)), slots, kRopeTable / n, rows / 1024});
   wg_rows = std::max<int64_t>(wg_rows, 1);
   a.wg_rows = (int32_t)wg_rows;
   a.head_slots = (int32_t)(slots / wg_rows);
@@ -246,15 +365,15 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
   hipStream_t s = (hipStream_t)stream;
 #define MPX_ROPE(DTv)                                                    \
   do {                                                                   \
-    if (vw == 4) launch_rope<DTv, 4>(a, (unsigned)blocks, s);            \
-    else if (vw == 2) launch_rope<DTv, 2>(a, (unsigned)blocks, s);       \
-    else launch_rope<DTv, 1>(a, (unsigned)blocks, s);                    \
+    if (vw == 4) launch_rope<DTv, 4>(a, pairs, (unsigned)blocks, s);     \
+    else if (vw == 2) launch_rope<DTv, 2>(a, pairs, (unsigned)blocks, s); \
+    else launch_rope<DTv, 1>(a, pairs, (unsigned)blocks, s);             \
   } while (0)
   if (dt == MPX_F32) {
     MPX_ROPE(MPX_F32);
   } else if (vw == 8) {
-    if (dt == MPX_F16) launch_rope<MPX_F16, 8>(a, (unsigned)blocks, s);
-    else launch_rope<MPX_BF16, 8>(a, (unsigned)blocks, s);
+    if (dt == MPX_F16) launch_rope<MPX_F16, 8>(a, pairs, (unsigned)blocks, s);
+    else launch_rope<MPX_BF16, 8>(a, pairs, (unsigned)blocks, s);
   } else if (dt == MPX_F16) {
     MPX_ROPE(MPX_F16);
   } else {

@@ -63,6 +63,10 @@ CASES = [
     (9, 9, 3, 1, 256, [4, 4, 4], 300),
     (1030, 1030, 12, 4, 64, [8, 12, 12], 256),
     (4097, 4097, 2, 1, 32, [8, 8], 64),
+    (20, 10, 3, 1, 130, [33, 30], 50),          # short runs of a long head
+    (1040, 1040, 3, 1, 256, [42, 42, 44], 50),
+    (2050, 2050, 2, 1, 65, [8, 8], 9),          # an odd one
+    (1030, 515, 3, 2, 24, [12], 9),
 ]
 
 
