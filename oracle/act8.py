@@ -16,7 +16,8 @@ EMAX = {"f16": 8, "bf16": 120}
 
 def exponents(x, fmt: str) -> np.ndarray:
     """Scale exponents [ceil(M / 32), K] of the matrix x [M, K]."""
-    x = np.asarray(x, np.float64)
+    with np.errstate(invalid="ignore"):      # signalling NaN inputs stay NaN
+        x = np.asarray(x, np.float64)
     M, K = x.shape
     a = np.zeros((-(-M // GROUP) * GROUP, K))
     a[:M] = np.where(np.isfinite(x), np.abs(x), 0.0)
@@ -37,10 +38,10 @@ def e4m3(y) -> np.ndarray:
 
 def pack(x, fmt: str):
     """Codes (as e4m3 values, NaN for non-finite x) and exponents of x."""
-    x = np.asarray(x, np.float64)
     e = exponents(x, fmt)
-    rows = np.repeat(e, GROUP, axis=0)[:x.shape[0]]
+    rows = np.repeat(e, GROUP, axis=0)[:np.shape(x)[0]]
     with np.errstate(invalid="ignore"):
+        x = np.asarray(x, np.float64)
         c = e4m3(np.ldexp(np.where(np.isfinite(x), x, np.nan), -rows))
     top = (rows == EMAX[fmt]) & (np.abs(c) > 240.0)
     return np.where(top, np.copysign(240.0, c), c), e

@@ -2,7 +2,6 @@
 // 32 rows of a column (the format is documented at mpx_act8_pack).
 #include <hip/hip_runtime.h>
 
-#include "act8.h"
 #include "common.h"
 #include "mfma.h"
 
@@ -244,7 +243,7 @@ static hipError_t launch_unpack(const uint8_t* codes, const uint8_t* scales, uin
   return hipGetLastError();
 }
 
-hipError_t launch_act8_unpack(const uint8_t* codes, const uint8_t* scales, uint16_t* Y, int64_t ldy,
+static hipError_t launch_act8_unpack(const uint8_t* codes, const uint8_t* scales, uint16_t* Y, int64_t ldy,
                               int64_t M, int64_t K, mpx_dtype dt, hipStream_t s) {
   return dt == MPX_F16 ? launch_unpack<MPX_F16>(codes, scales, Y, ldy, M, K, s)
                        : launch_unpack<MPX_BF16>(codes, scales, Y, ldy, M, K, s);

@@ -81,21 +81,16 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));
 // 8 bytes (codes or scales of 8 columns of a checkpoint) at any address
 typedef u32x2 u32x2_any __attribute__((aligned(1)));
 
-// Value c (0..7) of 8 packed codes, and its scale: a code's value times its
-// scale is exactly a half value.
+// Scale c (0..7) of 8 packed ones, and values c and c + 1 (c even) of 8 packed
+// codes: a code's value times its scale is exactly a half value.
 __device__ __forceinline__ float act8_scale(u32x2 s, int c) {
   return __builtin_bit_cast(float, ((s[c / 4] >> (8 * (c & 3))) & 0xFFu) << 23);
 }
-__device__ __forceinline__ float act8_value(u32x2 q, u32x2 s, int c) {
-  const uint32_t w = q[c / 4];
-  float v;
-  switch (c & 3) {  // the byte must be a constant
-    case 0: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 0); break;
-    case 1: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 1); break;
-    case 2: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 2); break;
-    default: v = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
-  }
-  return v * act8_scale(s, c);
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ f32x2 act8_values(u32x2 q, u32x2 s, int c) {
+  const f32x2 v = c & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)q[c / 4], true)
+                        : __builtin_amdgcn_cvt_pk_f32_fp8((int)q[c / 4], false);
+  return f32x2{v[0] * act8_scale(s, c), v[1] * act8_scale(s, c + 1)};
 }
 
 // Epilogue through LDS, for the transposed accumulator layout.  Step 1
@@ -299,15 +294,18 @@ __device__ __forceinline__ void gemm_epilogue_lds(const GemmArgs& g, const f32x1
     if constexpr (kDact8) {
       if (nc == 8) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-          h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(act8_value(op8[t], sc8[t * RPT / 32], c)));
+        for (int c = 0; c < 8; c += 2) {
+          const f32x2 v = act8_values(op8[t], sc8[t * RPT / 32], c);
+          h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(v[0]));
+          h[c + 1] = f2h<DT>(h2f<DT>(h[c + 1]) * gelu_tanh_grad(v[1]));
+        }
       } else {
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           if (c < nc) {
             const int64_t at = (mw + row) * ldc + nw + c8 + c, sat = ((mw + row) / MPX_ACT8_GROUP) * ldc + nw + c8 + c;
             const u32x2 q = {g.dact8[at], 0u}, s = {g.dact8_scale[sat], 0u};
-            h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(act8_value(q, s, 0)));
+            h[c] = f2h<DT>(h2f<DT>(h[c]) * gelu_tanh_grad(act8_values(q, s, 0)[0]));
           }
         }
       }
@@ -618,8 +616,10 @@ struct StagedAct8 {
       const u32x2 s = sv[P][RSTEP * q / 32];
       u32x4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        x[e] = f2h<DT>(act8_value(v[P][q], s, 2 * e)) | ((uint32_t)f2h<DT>(act8_value(v[P][q], s, 2 * e + 1)) << 16);
+      for (int e = 0; e < 4; ++e) {
+        const f32x2 f = act8_values(v[P][q], s, 2 * e);
+        x[e] = f2h<DT>(f[0]) | ((uint32_t)f2h<DT>(f[1]) << 16);
+      }
       if constexpr (ANY) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)

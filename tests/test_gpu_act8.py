@@ -131,7 +131,8 @@ def _run(fmt, M, N, K, x, pre, w, dy, act, want="xwb", off=0, counter=True):
 SHAPES = [(1, 1, 1), (1, 64, 128), (5, 3, 9), (31, 64, 64), (33, 128, 128), (64, 512, 1024), (65, 40, 24),
           (128, 10, 384), (257, 136, 144), (1000, 96, 588), (2048, 768, 384), (2500, 200, 136),
           (4097, 72, 264), (8320, 384, 256), (63, 64, 128), (65, 72, 144), (97, 8, 16), (2049, 64, 16),
-          (1537, 136, 400), (4099, 200, 272), (5000, 1032, 48), (2056, 2056, 1040)]
+          (1537, 136, 400), (4099, 200, 272), (5000, 1032, 48), (2056, 2056, 1040), (700, 2568, 2576),
+          (3300, 2056, 1040)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -251,3 +252,96 @@ def test_graph_replays_with_fresh_data(fmt):
         torch.cuda.synchronize()
         for a, b in zip(out, eager):
             assert torch.equal(a.view(torch.int16), b.view(torch.int16)), i
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("config", [1, 2, 3, 5, 7, 9])
+@pytest.mark.parametrize("mnk", [(512, 128, 768), (300, 192, 392), (65, 64, 72), (257, 128, 999)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_gelu_backward_on_every_tile(fmt, config, mnk):
+    """dX through GELU' from a checkpoint against mpx_linear_bwd on its widened
+    values, on each tile shape (whole tiles, edges, partial vectors): the same
+    roundings, so the same values up to one last place (the compiler may form
+    the float16 product in one rounding or two)."""
+    M, N, K = mnk
+    x, pre, w, dy = _problem(fmt, M, N, K, config)
+    pre[3, 5], pre[M - 1, K - 1], pre[:, 7] = 0.0, -30.0, 0.0
+    dt, h = mx.DTYPES[fmt], TORCH_HALF[fmt]
+    pc, ps = _pack(to_dev_half(pre, fmt), fmt)
+    P = torch.empty(M, K, dtype=h, device="cuda")
+    mx.mpx_act8_unpack(pc.data_ptr(), ps.data_ptr(), P.data_ptr(), K, M, K, dt, _s())
+    tw, tdy = to_dev_half(w, fmt), to_dev_half(dy, fmt)
+    a, b = (torch.full((M + 1, K), -7.0, dtype=h, device="cuda") for _ in range(2))
+    mx.mpx_gemm_set_config(config)
+    try:
+        mx.mpx_linear_bwd_act8(None, None, tw.data_ptr(), tdy.data_ptr(), pc.data_ptr(), ps.data_ptr(),
+                               mx.MPX_ACT_GELU_TANH, a.data_ptr(), None, None, M, N, K, dt, None, 0, None, _s())
+        mx.mpx_linear_bwd(None, tw.data_ptr(), tdy.data_ptr(), P.data_ptr(), mx.MPX_ACT_GELU_TANH, b.data_ptr(),
+                          None, None, M, N, K, dt, None, 0, None, _s())
+    finally:
+        mx.mpx_gemm_set_config(0)
+    assert (a[M] == -7.0).all()
+    ga, gb = to_host(a[:M]).astype(np.float64), to_host(b[:M]).astype(np.float64)
+    assert np.all(np.abs(ga - gb) <= ulp(np.maximum(np.abs(ga), np.abs(gb)), fmt))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dy_off, x_off, s_off", [(1, 0, 0), (0, 8, 0), (0, 0, 2), (8, 16, 4), (3, 5, 7)])
+def test_any_address_of_the_operands(fmt, dy_off, x_off, s_off):
+    """dY, codes and scales at addresses that the direct copies take and at others:
+    the same sums, in one of two orders."""
+    M, N, K = 1700, 136, 272
+    x, pre, w, dy = _problem(fmt, M, N, K, 5)
+    dt, h = mx.DTYPES[fmt], TORCH_HALF[fmt]
+    xc, xs = _pack(to_dev_half(x, fmt), fmt)
+    put = lambda t, off: torch.cat([torch.zeros(off, dtype=t.dtype, device="cuda"), t.reshape(-1)])
+    tdy, c, s = put(to_dev_half(dy, fmt), dy_off), put(xc, x_off), put(xs, s_off)
+    dw, db = torch.zeros(N, K, dtype=h, device="cuda"), torch.zeros(N, dtype=h, device="cuda")
+    need = mx.mpx_linear_bwd_act8_workspace(M, N, K)
+    ws = _bytes(need)
+    mx.mpx_linear_bwd_act8(c.data_ptr() + x_off, s.data_ptr() + s_off, None, tdy.data_ptr() + 2 * dy_off, None, None,
+                           0, None, dw.data_ptr(), db.data_ptr(), M, N, K, dt, ws.data_ptr(), need, None, _s())
+    xv = act8.values(*act8.pack(x, fmt))
+    _, rdw, rdb = ops.linear_bwd(Policy(fmt), xv, w, dy)
+    assert_within(to_host(dw), rdw, gemm_bound(dy.T, xv, rdw, fmt, M), "dW")
+    colb = ulp(rdb, fmt) + 2.0 * M * 2.0 ** -24 * np.abs(dy.astype(np.float64)).sum(axis=0)
+    assert_within(to_host(db), rdb, colb, "db")
+
+
+def test_offsets_past_32_bits():
+    """1,100,005 rows of 2048: codes past 2^31 bytes, halves past 2^32."""
+    M, N, K, h, dt = 1_100_005, 16, 2048, torch.bfloat16, mx.MPX_BF16
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(M, K, dtype=h, device="cuda").normal_(generator=g)
+    dy = torch.empty(M, N, dtype=h, device="cuda").normal_(generator=g)
+    w = torch.empty(N, K, dtype=h, device="cuda").normal_(generator=g)
+    c, s = torch.empty(M, K, dtype=torch.uint8, device="cuda"), torch.empty(-(-M // 32), K, dtype=torch.uint8, device="cuda")
+    mx.mpx_act8_pack(x.data_ptr(), K, c.data_ptr(), s.data_ptr(), M, K, dt, _s())
+    r0 = (M - 70) // 32 * 32   # the last groups on their own
+    ec, es = _pack(x[r0:].contiguous(), "bf16")
+    assert torch.equal(c[r0:], ec) and torch.equal(s[r0 // 32:], es)
+    y = torch.empty(M, K, dtype=h, device="cuda")
+    mx.mpx_act8_unpack(c.data_ptr(), s.data_ptr(), y.data_ptr(), K, M, K, dt, _s())
+    dx, dw, db = torch.empty(M, K, dtype=h, device="cuda"), torch.empty(N, K, dtype=h, device="cuda"), torch.empty(N, dtype=h, device="cuda")
+    need = mx.mpx_linear_bwd_act8_workspace(M, N, K)
+    ws = _bytes(need)
+    mx.mpx_linear_bwd_act8(c.data_ptr(), s.data_ptr(), w.data_ptr(), dy.data_ptr(), c.data_ptr(), s.data_ptr(),
+                           mx.MPX_ACT_GELU_TANH, dx.data_ptr(), dw.data_ptr(), db.data_ptr(), M, N, K, dt,
+                           ws.data_ptr(), need, None, _s())
+    ref, mag = torch.zeros(N, K, dtype=torch.float64, device="cuda"), torch.zeros(N, K, dtype=torch.float64, device="cuda")
+    for r in range(0, M, 1 << 17):
+        a, b = dy[r:r + (1 << 17)].double(), y[r:r + (1 << 17)].double()
+        ref += a.t() @ b
+        mag += a.abs().t() @ b.abs()
+    # two float32 summation orders of M products, one rounding
+    ref, mag = ref.cpu().numpy(), mag.cpu().numpy()
+    assert np.all(np.abs(to_host(dw) - ref) <= ulp(ref, "bf16") + 2.0 * M * 2.0 ** -24 * mag)
+    assert np.linalg.norm(to_host(dw) - ref) <= 2.0 ** -8 * np.linalg.norm(ref)
+    # the last rows of dX, and rows across 2^31 codes, alone
+    for lo in (r0, (1 << 31) // K // 32 * 32 - 64):
+        n = min(128, M - lo)
+        part = torch.empty(n, K, dtype=h, device="cuda")
+        mx.mpx_linear_bwd(None, w.data_ptr(), dy[lo:lo + n].contiguous().data_ptr(), y[lo:lo + n].contiguous().data_ptr(),
+                          mx.MPX_ACT_GELU_TANH, part.data_ptr(), None, None, n, N, K, dt, None, 0, None, _s())
+        d = (dx[lo:lo + n].double() - part.double()).abs().cpu().numpy()
+        assert np.all(d <= ulp(to_host(part), "bf16"))
