@@ -12,30 +12,6 @@ namespace mpx {
 // columns of the 256 bytes of banks (a row spans half of them).
 __device__ __forceinline__ int act8_chunk(int r, int c) { return c ^ (2 * ((r >> 1) & 3)); }
 
-template <int NWAVES>
-struct Act8Dma {
-  static constexpr int CH = 8, Q = 8 / NWAVES;
-  static_assert(8 % NWAVES == 0, "copies do not split evenly over the waves");
-  uint32_t off[Q];
-  // rv: outputs (a multiple of 16) of the matrix from the tile's first on; ld: bytes
-  __device__ __forceinline__ void init(int64_t ld, int rv, int wave, int lane) {
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const int at = 64 * (wave + NWAVES * q) + lane, kr = at / CH, c = act8_chunk(kr, at % CH);
-      off[q] = (uint32_t)(kr * ld + (16 * c < rv ? 16 * c : 0));
-    }
-  }
-  __device__ __forceinline__ void issue(const uint8_t* base, uint32_t lds, int wave) const {
-    const uint64_t p = reinterpret_cast<uint64_t>(base);
-    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
-    const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
-    const uint32_t slds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-      dma16(reinterpret_cast<const void*>(lo | (hi << 32)), off[q], slds + 1024u * (uint32_t)(wave + NWAVES * q));
-  }
-};
-
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 // 4 bytes per lane from base + off (bytes) into LDS at lds + 4 * lane
@@ -46,6 +22,42 @@ __device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t ld
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
+
+// Copies of a stage's codes, 16 bytes per lane, or 4 (NARROW) where rows are not
+// whole 16-byte chunks or start between them (8415 x 768 x 588 bf16 27 us, 38 with
+// the register-staged tiles; 12608 x 2304 x 764 68 and 108).
+template <int NWAVES, bool NARROW>
+struct Act8Dma {
+  static constexpr int Q = (NARROW ? 32 : 8) / NWAVES;
+  static_assert(8 % NWAVES == 0, "copies do not split evenly over the waves");
+  uint32_t off[Q];
+  // k row of this lane's copy q
+  __device__ __forceinline__ static int row(int q, int wave, int lane) {
+    return (wave + NWAVES * q) * (NARROW ? 2 : 8) + lane / (NARROW ? 32 : 8);
+  }
+  // rv: outputs (a multiple of 16, or 4) of the matrix from the tile's first on; ld: bytes
+  __device__ __forceinline__ void init(int64_t ld, int rv, int wave, int lane) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int kr = row(q, wave, lane);
+      const int col = NARROW ? 16 * act8_chunk(kr, lane % 32 / 4) + 4 * (lane & 3) : 16 * act8_chunk(kr, lane % 8);
+      off[q] = (uint32_t)(kr * ld + (col < rv ? col : 0));
+    }
+  }
+  __device__ __forceinline__ void issue(const uint8_t* base, uint32_t lds, int wave) const {
+    const uint64_t p = reinterpret_cast<uint64_t>(base);
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+    const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+    const uint32_t slds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if constexpr (NARROW)
+        dma4(reinterpret_cast<const void*>(lo | (hi << 32)), off[q], slds + 256u * (uint32_t)(wave + NWAVES * q));
+      else
+        dma16(reinterpret_cast<const void*>(lo | (hi << 32)), off[q], slds + 1024u * (uint32_t)(wave + NWAVES * q));
+    }
+  }
+};
 
 typedef int act8_v2i __attribute__((ext_vector_type(2)));
 
@@ -85,7 +97,7 @@ __device__ __forceinline__ uint4 act8_widen(u32x2 q, float s) {
 // Any reduction length: in the last k tile, rows behind the matrix read its last
 // row again, and A's are then zeroed in LDS by the wave that copied them (a code
 // of that row can be NaN only where its column's sum is NaN anyway).
-template <int DT, int BM, int BN, int WM, int WN, int E, bool DBS>
+template <int DT, int BM, int BN, int WM, int WN, int E, bool DBS, bool NARROW>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64)
 __attribute__((amdgpu_waves_per_eu(BM == 64 ? 4 : 2, BM == 64 ? 4 : 2)))
 void gemm_act8_kernel(GemmArgs g) {
@@ -117,7 +129,7 @@ void gemm_act8_kernel(GemmArgs g) {
   const uint16_t* Ab = g.A + kbeg * g.lda + m0;
   const uint8_t* Bb = g.b8 + kbeg * g.ldb + n0;
   DmaOperand<BM, false, NWAVES> da;
-  Act8Dma<NWAVES> db;
+  Act8Dma<NWAVES, NARROW> db;
   da.init(g.lda, (int)min<int64_t>(BM, g.M - m0), wave, lane);
   db.init(g.ldb, (int)min<int64_t>(BN, g.N - n0), wave, lane);
 
@@ -151,8 +163,7 @@ void gemm_act8_kernel(GemmArgs g) {
       }
 #pragma unroll
       for (int q = 0; q < cb.Q; ++q) {
-        const int kr = (64 * (wave + NWAVES * q) + lane) / (BN / 16);
-        cb.off[q] -= (uint32_t)(max(0, kr - (krest - 1)) * g.ldb);
+        cb.off[q] -= (uint32_t)(max(0, cb.row(q, wave, lane) - (krest - 1)) * g.ldb);
       }
       ca.issue(a, st, wave);
       cb.issue(b, st + A_BYTES, wave);
@@ -207,7 +218,7 @@ void gemm_act8_kernel(GemmArgs g) {
       for (int j = 0; j < TN; ++j) sc[i][j] = __builtin_bit_cast(float, (uint32_t)s[i * BN + 32 * j] << 23);
   };
 
-  constexpr int L = (DmaOperand<BM, false, NWAVES>::Q + Act8Dma<NWAVES>::Q);
+  constexpr int L = (DmaOperand<BM, false, NWAVES>::Q + Act8Dma<NWAVES, NARROW>::Q);
   if (nk > 1) wait_vmcnt<L>();  // the first wave has its scales' copies too: it waits for the second tile's
   else wait_vmcnt<0>();
   landed(0);
@@ -328,7 +339,8 @@ static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused) {
   g.full_epi = full_epilogue_ok(g, bm) ? 1 : 0;
 #define MPX_K8_STAGED(B, W, STGv, Ev, DBv) \
   gemm_tile_kernel<DT, B, B, W, W, 2, false, false, Ev, DBv, STGv, true><<<grid, 256, 0, s>>>(g)
-#define MPX_K8_DIRECT(B, W, STGv, Ev, DBv) gemm_act8_kernel<DT, B, 128, W, 64, Ev, DBv><<<grid, 256, 0, s>>>(g)
+#define MPX_K8_DIRECT(B, W, NARv, Ev, DBv) \
+  gemm_act8_kernel<DT, B, 128, W, 64, Ev, DBv, NARv><<<grid, 256, 0, s>>>(g)
 #define MPX_K8_EPI(KERNEL, B, W, STGv)                     \
   do {                                                     \
     const bool plain = epilogue_mask(g) == 0;              \
@@ -340,8 +352,11 @@ static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused) {
       else KERNEL(B, W, STGv, EPI_GENERIC, false);         \
     }                                                      \
   } while (0)
-  if (g.act8_rows == 64) MPX_K8_EPI(MPX_K8_DIRECT, 64, 32, 0);
-  else if (g.act8_rows) MPX_K8_EPI(MPX_K8_DIRECT, 128, 64, 0);
+  const bool narrow = g.ldb % 16 != 0 || (reinterpret_cast<uintptr_t>(g.b8) & 15u) != 0;
+  if (g.act8_rows == 64 && narrow) MPX_K8_EPI(MPX_K8_DIRECT, 64, 32, true);
+  else if (g.act8_rows == 64) MPX_K8_EPI(MPX_K8_DIRECT, 64, 32, false);
+  else if (g.act8_rows && narrow) MPX_K8_EPI(MPX_K8_DIRECT, 128, 64, true);
+  else if (g.act8_rows) MPX_K8_EPI(MPX_K8_DIRECT, 128, 64, false);
   else if (any) MPX_K8_EPI(MPX_K8_STAGED, 64, 32, 2);
   else if (small) MPX_K8_EPI(MPX_K8_STAGED, 64, 32, 1);
   else MPX_K8_EPI(MPX_K8_STAGED, 128, 64, 1);

@@ -1180,12 +1180,14 @@ static bool dma_ok(const GemmArgs& g, bool vec, bool ak, bool bk) {
   return spanA < lim && spanB < lim;
 }
 
-// What the direct copies of an 8-bit B (gemm_act8.h) need: 16-byte aligned
-// operands, rows of whole 16-byte chunks, 4-byte aligned scales, 32-bit lane offsets.
+// What the direct copies of an 8-bit B (gemm_act8.h) need: a 16-byte aligned A
+// with rows of whole 16-byte chunks, codes and scales in rows of whole 4-byte words
+// at such addresses, 32-bit lane offsets.
 static bool act8_dma_ok(const GemmArgs& g) {
-  auto al16 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
   const int64_t lim = (int64_t)1 << 31;
-  return al16(g.A) && al16(g.b8) && (reinterpret_cast<uintptr_t>(g.b8_scale) & 3u) == 0 && g.lda % 8 == 0 && g.ldb % 16 == 0 && g.lda * 128 < lim && g.ldb * 64 < lim;
+  const uintptr_t words = reinterpret_cast<uintptr_t>(g.b8) | reinterpret_cast<uintptr_t>(g.b8_scale);
+  return (reinterpret_cast<uintptr_t>(g.A) & 15u) == 0 && g.lda % 8 == 0 && (words & 3u) == 0 && g.ldb % 4 == 0 &&
+         g.lda * 128 < lim && g.ldb * 64 < lim;
 }
 
 static bool small_ok(const GemmArgs& g, int64_t nbatch);
