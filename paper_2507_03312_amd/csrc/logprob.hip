@@ -143,10 +143,13 @@ struct BestK {
   }
 };
 
-// One wave's pass over a row: per lane the moments about `ref` (moved only when
-// a logit exceeds it by 8, so nearly never after the first vectors; the sums are
-// float32 and e^8 of them costs no accuracy), the largest logit, and over the
-// wave the k best logits.
+// Bound by HBM where the logits are many and the alternatives few (4096 x 65536
+// bf16: 99 us without, 5.4 TB/s; 107 with 4, 130 with 16), by the latency of the
+// best's ordering in a few rows.
+// One wave's pass over a row: per lane the moments about `ref` (moved only when a
+// logit exceeds it by 8, so nearly never after the first vectors; the sums are
+// float32 and e^8 of them costs no accuracy), the largest logit, and over the wave
+// the k best logits.
 template <int DT, bool ENT, bool TOP>
 struct RowScan {
   static constexpr int VE = kVec<DT>;
@@ -381,8 +384,9 @@ struct LogprobGrad {
   const mpx_scale_state* state;
 };
 
-// A wave's part of a row: up to U vectors per lane, all loaded before the first
-// store.  With t = (z - m) - ln S and p = e^t the gradient is
+// Bound by HBM (one read and one write of every logit: 4096 x 65536 bf16 186 us,
+// 5.8 TB/s).  A wave's part of a row: up to U vectors per lane, all loaded before
+// the first store.  With t = (z - m) - ln S and p = e^t the gradient is
 //   p (c0 + c1 t),  c0 = -scale (sum of the upstream cotangents + g_H H),
 //   c1 = -scale g_H,
 // plus scale g at the target's and the alternatives' own columns: lane i <= k
@@ -469,19 +473,26 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t
   }
 }
 
-// Rows of up to kWaveRow logits take one wave each; longer ones a workgroup, or
-// several: columns are split until there are about 1024 workgroups, into parts
-// of at least kLeastSplit columns, at most 64.
-constexpr int64_t kWaveRow = 2048, kLeastSplit = 4096;
+// One wave per row where the rows alone fill the chip, or are so short that a
+// workgroup's join costs more than its other waves gain; else a workgroup per row
+// or, up to about 1024 workgroups, several, of at least kLeastSplit columns each and
+// at most 64.  A wave keeps its own best, so fewer waves per row also order less.
+// Measured (bf16, 4 alternatives; us, one wave / a workgroup): 64 rows x 500 4.9 /
+// 5.2, x 1000 6.1 / 5.1; 2048 x 1000 6.7 / 7.6, x 4000 13.3 / 12.0; 4096 x 4000 16 /
+// 19, x 32000 61 / 60 (with 16 75 / 82), x 65536 112 / 107; 16384 x 16000 109 / 129.
+// Splits (us; workgroups aimed at 256, 512, 1024): 64 x 131072 24.4, 19.4, 17.8; 1 x
+// 131072 in parts of at least 4096 columns 11.2, of 8192 12.8.
+constexpr int64_t kLeastSplit = 4096;
 struct LogprobPlan {
+  bool wave;
   int splits;
   int64_t seg;
 };
 static LogprobPlan logprob_plan(int64_t rows, int64_t V) {
-  if (V <= kWaveRow) return {1, V};
+  if (V <= (rows >= 4096 ? 32768 : rows >= 2048 ? 2048 : 512)) return {true, 1, V};
   const int64_t want = std::min<int64_t>({cdiv(1024, rows), cdiv(V, kLeastSplit), 64});
   const int64_t seg = cdiv(cdiv(V, want), kLeastSplit) * kLeastSplit;
-  return {(int)cdiv(V, seg), seg};
+  return {false, (int)cdiv(V, seg), seg};
 }
 
 }  // namespace mpx
@@ -535,7 +546,7 @@ extern "C" int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* target
   const unsigned waves4 = (unsigned)cdiv(rows, 4), blocks = (unsigned)(rows * plan.splits);
 #define MPX_LP_FWD(DTv, ENTv, TOPv)                                                                      \
   do {                                                                                                   \
-    if (V <= kWaveRow)                                                                                   \
+    if (plan.wave)                                                                                       \
       logprob_fwd_kernel<DTv, 1, ENTv, TOPv>                                                             \
           <<<waves4, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, plan.seg, out, parts);       \
     else                                                                                                 \

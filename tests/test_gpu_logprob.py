@@ -151,7 +151,8 @@ def _check_backward(z, t, targets, k, fmt, f, idx, which="les", scale=None, in_p
 
 SHAPES = [(1, 1, 1), (1, 2, 2), (3, 7, 7), (5, 10, 0), (4, 63, 3), (2, 64, 16), (7, 65, 16), (64, 100, 5),
           (9, 511, 2), (6, 513, 8), (256, 1000, 5), (33, 1024, 1), (5, 2049, 4), (3, 4099, 16), (2, 8192, 8),
-          (17, 10007, 6), (1, 65537, 16), (3, 131072, 8), (1, 262144, 1), (300, 5003, 4)]
+          (17, 10007, 6), (1, 65537, 16), (3, 131072, 8), (1, 262144, 1), (300, 5003, 4), (2048, 1501, 5),
+          (4097, 1031, 3)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -318,3 +319,32 @@ def test_offsets_past_32_bits():
                            f[1].data_ptr(), None, gl.data_ptr(), ge.data_ptr(), gt, st.data_ptr(),
                            out.data_ptr(), lo, mx.MPX_BF16, _s())
     assert torch.equal(t, one) and want.shape == one.shape
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("k", [0, 1, 16])
+def test_rows_do_not_depend_on_how_many_there_are(fmt, k):
+    """Thousands of rows (a wave each), hundreds (a workgroup each) and single ones
+    (several workgroups each): the same alternatives, and float results that
+    differ by their summation orders only (chains of at most V / 64 + 64 terms on
+    either side, relative to sums of positive terms)."""
+    rows, V = 4096, 20011
+    g = torch.Generator(device="cuda").manual_seed(k)
+    t = torch.empty(rows, V, device="cuda").normal_(0, 2.5, generator=g).to(HALF[fmt])
+    t[5] = float("-inf")
+    t[9, ::3] = float("-inf")
+    t[11, 77] = float("nan")
+    targets = torch.randint(0, V, (rows,), generator=g, device="cuda").int()
+    f, top, idx, _, _ = _fwd(t, targets, V, k, fmt)
+    stats = f[2:].reshape(-1)[:2 * rows].view(rows, 2)
+    tol = 2 * (V / 64 + 64 + 40) * U
+    for lo, n in ((0, 700), (3000, 700), (5, 1), (9, 4), (4095, 1), (100, 33)):
+        pf, ptop, pidx, _, _ = _fwd(t[lo:lo + n], targets[lo:lo + n], V, k, fmt)
+        assert torch.equal(pidx[:n * k], idx[lo * k:(lo + n) * k])
+        for a, b, size in ((pf[0, :n], f[0, lo:lo + n], 30.0), (pf[1, :n], f[1, lo:lo + n], 30.0),
+                           (ptop[:n * k], top[lo * k:(lo + n) * k], 30.0),
+                           (pf[2:].reshape(-1)[:2 * n].view(n, 2)[:, 1], stats[lo:lo + n, 1], 30.0)):
+            assert torch.equal(torch.isfinite(a), torch.isfinite(b))
+            ok = torch.isfinite(a)
+            assert torch.equal(a[~ok].isnan(), b[~ok].isnan())
+            assert ok.sum() == 0 or float((a[ok] - b[ok]).abs().max()) <= tol * size
