@@ -22,6 +22,20 @@ __device__ __forceinline__ float logit(const typename LogitOf<DT>::type* z) {
 // on gfx950), and the VE logits in them.
 typedef uint32_t lp_u32x4 __attribute__((ext_vector_type(4)));
 typedef lp_u32x4 lp_u32x4_any __attribute__((aligned(2)));
+// Operands past the 256 MB last-level cache stream past it (the choice is the
+// caller's, by their size: kStreamBytes).
+template <bool NT>
+__device__ __forceinline__ lp_u32x4 lp_load(const void* p) {
+  const lp_u32x4_any* q = reinterpret_cast<const lp_u32x4_any*>(p);
+  if constexpr (NT) return __builtin_nontemporal_load(q);
+  else return *q;
+}
+template <bool NT>
+__device__ __forceinline__ void lp_store(void* p, lp_u32x4 v) {
+  lp_u32x4_any* q = reinterpret_cast<lp_u32x4_any*>(p);
+  if constexpr (NT) __builtin_nontemporal_store(v, q);
+  else *q = v;
+}
 template <int DT> constexpr int kVec = DT == MPX_F32 ? 4 : 8;
 
 template <int DT>
@@ -200,6 +214,7 @@ struct RowScan {
 
   // columns [c0, c1) of the row z, this wave's chunks of 64 VE of them (every
   // `waves`-th, from the wave-th on)
+  template <bool NT>
   __device__ __forceinline__ void scan(const typename LogitOf<DT>::type* z, int64_t c0, int64_t c1, int wave,
                                        int waves) {
     constexpr int CH = 64 * VE, U = 2;  // U loads in flight per wave, eight waves a SIMD
@@ -210,7 +225,7 @@ struct RowScan {
       lp_u32x4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        v[u] = *reinterpret_cast<const lp_u32x4_any*>(p + (int64_t)min(i + u * waves, chunks - 1) * CH);
+        v[u] = lp_load<NT>(p + (int64_t)min(i + u * waves, chunks - 1) * CH);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (i + u * waves >= chunks) break;
@@ -277,7 +292,7 @@ __device__ __forceinline__ void lp_results(const typename LogitOf<DT>::type* z, 
 // WAVES == 1: one wave per row, four rows per workgroup.  WAVES == 4: a
 // workgroup per row, or per split of seg columns of it, whose partial results
 // logprob_join_kernel joins.
-template <int DT, int WAVES, bool ENT, bool TOP>
+template <int DT, int WAVES, bool ENT, bool TOP, bool NT>
 __global__ __launch_bounds__(256) void logprob_fwd_kernel(const void* Z, int64_t ldz,
                                                           const int32_t* targets, int64_t rows, int64_t V,
                                                           int k, int splits, int64_t seg, LogprobOut out,
@@ -291,14 +306,14 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(const void* Z, int64_t
     const int64_t r = (int64_t)blockIdx.x * 4 + wave;
     if (r >= rows) return;
     const T* z = (const T*)Z + r * ldz;
-    scan.scan(z, 0, V, 0, 1);
+    scan.template scan<NT>(z, 0, V, 0, 1);
     if constexpr (TOP) scan.best.order();
     lp_results<DT>(z, r, V, k, lane, scan.moments(), scan.best.buf, targets, out);
   } else {
     __shared__ float mom[4][3];
     const int64_t r = blockIdx.x / splits, sp = blockIdx.x % splits;
     const T* z = (const T*)Z + r * ldz;
-    scan.scan(z, sp * seg, min(V, (sp + 1) * seg), wave, 4);
+    scan.template scan<NT>(z, sp * seg, min(V, (sp + 1) * seg), wave, 4);
     if constexpr (TOP) scan.best.order();
     const Moments a = scan.moments();
     if (lane == 0) {
@@ -392,7 +407,7 @@ struct LogprobGrad {
 // plus scale g at the target's and the alternatives' own columns: lane i <= k
 // holds one of those columns and its cotangent, and a chunk that holds none of
 // them, which one comparison tells, goes without.
-template <int DT>
+template <int DT, bool NT>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t ldz, int64_t rows, int64_t V,
                                                           int k, LogprobGrad g, void* dZ, int64_t ldo,
                                                           int64_t row_waves) {
@@ -411,7 +426,7 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t at = u * CH + lane * VE;
-    if (at + VE <= left) v[u] = *reinterpret_cast<const lp_u32x4_any*>(z + at);
+    if (at + VE <= left) v[u] = lp_load<NT>(z + at);
     else lp_load_tail<DT>(z + at, (int)max<int64_t>(left - at, 0), x[u]);
   }
   const float scale = g.state ? g.state->scale : 1.0f;
@@ -460,7 +475,7 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t
         if constexpr (DT == MPX_F32) w[j] = __builtin_bit_cast(uint32_t, d[j]);
         else w[j] = f2h<DT>(d[2 * j]) | ((uint32_t)f2h<DT>(d[2 * j + 1]) << 16);
       }
-      *reinterpret_cast<lp_u32x4_any*>(o + at) = w;
+      lp_store<NT>(o + at, w);
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
@@ -483,6 +498,11 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(const void* Z, int64_t
 // Splits (us; workgroups aimed at 256, 512, 1024): 64 x 131072 24.4, 19.4, 17.8; 1 x
 // 131072 in parts of at least 4096 columns 11.2, of 8192 12.8.
 constexpr int64_t kLeastSplit = 4096;
+// Logits (and, backward, gradients) that together pass the last-level cache are
+// read and written around it; smaller ones may stay there for the next call
+// (4096 x 65537 bf16 gradient 218 -> 183 us, 16384 x 32000 forward 199 -> 177;
+// 1024 x 32000 forward 22.8, around the cache 23.6).
+constexpr int64_t kStreamBytes = 256 << 20;
 struct LogprobPlan {
   bool wave;
   int splits;
@@ -544,17 +564,19 @@ extern "C" int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* target
   const LogprobParts parts = {(float*)workspace, (uint32_t*)workspace + rows * plan.splits * 3};
   hipStream_t s = (hipStream_t)stream;
   const unsigned waves4 = (unsigned)cdiv(rows, 4), blocks = (unsigned)(rows * plan.splits);
-#define MPX_LP_FWD(DTv, ENTv, TOPv)                                                                      \
-  do {                                                                                                   \
-    if (plan.wave)                                                                                       \
-      logprob_fwd_kernel<DTv, 1, ENTv, TOPv>                                                             \
-          <<<waves4, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, plan.seg, out, parts);       \
-    else                                                                                                 \
-      logprob_fwd_kernel<DTv, 4, ENTv, TOPv>                                                             \
-          <<<blocks, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, plan.seg, out, parts);       \
-    if (plan.splits > 1)                                                                                 \
-      logprob_join_kernel<DTv, TOPv>                                                                     \
-          <<<waves4, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, out, parts);                 \
+  const bool nt = rows * V > kStreamBytes / (dt == MPX_F32 ? 4 : 2);
+#define MPX_LP_KERNEL(DTv, WAVESv, ENTv, TOPv, NTv, grid)  \
+  logprob_fwd_kernel<DTv, WAVESv, ENTv, TOPv, NTv>         \
+      <<<grid, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, plan.seg, out, parts)
+#define MPX_LP_FWD(DTv, ENTv, TOPv)                                                      \
+  do {                                                                                   \
+    if (plan.wave && nt) MPX_LP_KERNEL(DTv, 1, ENTv, TOPv, true, waves4);                \
+    else if (plan.wave) MPX_LP_KERNEL(DTv, 1, ENTv, TOPv, false, waves4);                \
+    else if (nt) MPX_LP_KERNEL(DTv, 4, ENTv, TOPv, true, blocks);                        \
+    else MPX_LP_KERNEL(DTv, 4, ENTv, TOPv, false, blocks);                               \
+    if (plan.splits > 1)                                                                 \
+      logprob_join_kernel<DTv, TOPv>                                                     \
+          <<<waves4, 256, 0, s>>>(Z, ldz, targets, rows, V, k, plan.splits, out, parts); \
   } while (0)
 #define MPX_LP(DTv)                              \
   do {                                           \
@@ -566,6 +588,7 @@ extern "C" int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* target
   MPX_BY_TYPE(dt, MPX_LP);
 #undef MPX_LP
 #undef MPX_LP_FWD
+#undef MPX_LP_KERNEL
   MPX_LAUNCHED();
   return MPX_OK;
 }
@@ -595,10 +618,18 @@ extern "C" int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* target
   const int64_t row_waves = cdiv(V, 4 * 64 * (dt == MPX_F32 ? 4 : 8));
   MPX_REQUIRE(rows <= ((int64_t)1 << 25) / row_waves, "rows * V too large for one call");
   const unsigned blocks = (unsigned)cdiv(rows * row_waves, 4);
-#define MPX_LP(DTv)                                                                                   \
-  logprob_bwd_kernel<DTv><<<blocks, 256, 0, (hipStream_t)stream>>>(Z, ldz, rows, V, k, g, dZ, ldo, row_waves)
+  const bool nt = 2 * rows * V > kStreamBytes / (dt == MPX_F32 ? 4 : 2);
+#define MPX_LP_KERNEL(DTv, NTv)    \
+  logprob_bwd_kernel<DTv, NTv>     \
+      <<<blocks, 256, 0, (hipStream_t)stream>>>(Z, ldz, rows, V, k, g, dZ, ldo, row_waves)
+#define MPX_LP(DTv)                            \
+  do {                                         \
+    if (nt) MPX_LP_KERNEL(DTv, true);          \
+    else MPX_LP_KERNEL(DTv, false);            \
+  } while (0)
   MPX_BY_TYPE(dt, MPX_LP);
 #undef MPX_LP
+#undef MPX_LP_KERNEL
   MPX_LAUNCHED();
   return MPX_OK;
 }

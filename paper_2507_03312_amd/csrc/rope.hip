@@ -18,6 +18,7 @@ struct RopeArgs {
   int64_t ldx, ldy;
   uint32_t pos_rows, rows, heads_rot, copy;  // copy: values copied behind the turned heads
   int32_t hd, axes, npairs, interleaved, back, in_place;
+  int32_t stream;  // more than the last-level cache holds
   // a workgroup's rows, and the threads that share a row's heads: thread
   // (slot, chunk) takes heads slot % head_slots, + head_slots, ... of row
   // slot / head_slots, with the pairs of `chunk` of each
@@ -29,12 +30,33 @@ struct RopeArgs {
 template <int DT> struct RopeValue { typedef uint16_t type; };
 template <> struct RopeValue<MPX_F32> { typedef float type; };
 
+typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
+typedef rope_u32x4 rope_u32x4_any __attribute__((aligned(2)));
+
 // N values at any alignment of theirs (global accesses need no more on gfx950)
 template <int DT, int N> struct RopeVec {
   typedef typename RopeValue<DT>::type T;
   T v[N];
-  __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
-  __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, v, sizeof(v)); }
+  // NT (16-byte vectors): around the caches
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (NT) {
+      const rope_u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const rope_u32x4_any*>(p));
+      __builtin_memcpy(v, &w, sizeof(v));
+    } else {
+      __builtin_memcpy(v, p, sizeof(v));
+    }
+  }
+  template <bool NT = false>
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (NT) {
+      rope_u32x4 w;
+      __builtin_memcpy(&w, v, sizeof(v));
+      __builtin_nontemporal_store(w, reinterpret_cast<rope_u32x4_any*>(p));
+    } else {
+      __builtin_memcpy(p, v, sizeof(v));
+    }
+  }
   // the same vector of another lane
   __device__ __forceinline__ RopeVec from_lane(int l) const {
     constexpr int W = (sizeof(v) + 3) / 4;
@@ -101,8 +123,9 @@ __device__ __forceinline__ void rope_copies_and_turns(const RopeArgs& a, const t
 // value's partner lies in the same run (interleaved) or comes from the lane that
 // has it (halves): y = x c + partner s, s negative in a section's first half.
 // Values behind the sections count as pairs that are not turned.  The lanes of a
-// head lie in one wave (a.chunks <= 64 runs).
-template <int DT, int VW, bool INTER>
+// head lie in one wave (a.chunks <= 64 runs).  12608 rows of 36 heads of 64 bf16 (116
+// MB) take 25 us, in place 16.5; 29997 of 48 heads of 128 f16 (737 MB) 119 us.
+template <int DT, int VW, bool INTER, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   typedef typename RopeValue<DT>::type T;
   __shared__ float2 turns[kRopeTable];
@@ -152,7 +175,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   for (uint32_t h = h0; h < heads; h += U * a.head_slots) {
     RopeVec<DT, VW> v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u].load(x + (int64_t)min(h + u * a.head_slots, heads - 1) * a.hd);
+    for (int u = 0; u < U; ++u) v[u].template load<NT>(x + (int64_t)min(h + u * a.head_slots, heads - 1) * a.hd);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (h + u * a.head_slots >= heads) break;
@@ -174,7 +197,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
           for (int i = 0; i < NP; ++i) v[u].set(i, __builtin_fmaf(v[u].get(i), c[i], o.get(i) * s[i]));
         }
       }
-      if (turn || !a.in_place) v[u].store(p);
+      if (turn || !a.in_place) v[u].template store<NT>(p);
     }
   }
 }
@@ -282,8 +305,16 @@ static void launch_rope(const RopeArgs& a, bool pairs, unsigned blocks, hipStrea
     }
   }
   if constexpr (VW > 1) {
-    if (a.interleaved) rope_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
-    else rope_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
+    constexpr bool kWide = VW * sizeof(typename RopeValue<DT>::type) == 16;
+    if constexpr (kWide) {
+      if (a.stream) {
+        if (a.interleaved) rope_kernel<DT, VW, true, true><<<blocks, 256, 0, s>>>(a);
+        else rope_kernel<DT, VW, false, true><<<blocks, 256, 0, s>>>(a);
+        return;
+      }
+    }
+    if (a.interleaved) rope_kernel<DT, VW, true, false><<<blocks, 256, 0, s>>>(a);
+    else rope_kernel<DT, VW, false, false><<<blocks, 256, 0, s>>>(a);
   }
 }
 
@@ -301,6 +332,7 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
   MPX_REQUIRE_FN(is_half(dt) || dt == MPX_F32, "dt must be MPX_F16, MPX_BF16 or MPX_F32");
   MPX_REQUIRE_FN(rows >= 1 && pos_rows >= 1 && rows % pos_rows == 0,
                  "rows must be a positive multiple of pos_rows");
+  MPX_REQUIRE_FN(rows <= INT32_MAX, "too many rows for one call");
   MPX_REQUIRE_FN(hd >= 2 && hd <= kRopeMaxHd, "hd must be in [2, 512]");
   const int64_t most = (int64_t)1 << 20;
   MPX_REQUIRE_FN(heads_rot >= 1 && heads_rot <= most && heads_copy >= 0 && heads_copy <= most,
@@ -349,16 +381,22 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
   a.interleaved = plan->interleaved;
   a.back = back ? 1 : 0;
   a.in_place = X == Y ? 1 : 0;
+  // Values past the 256 MB last-level cache go around it (29997 rows of 48 heads of
+  // 128 f16 129 -> 119 us, in place 117 -> 100); smaller ones may be in it, or be read
+  // from it next (16640 rows of 18 heads of 64 15.6 us, around it 18.9).
+  const double bytes = (double)rows * (double)width * (dt == MPX_F32 ? 4.0 : 2.0);
+  a.stream = (X == Y ? bytes : 2.0 * bytes) > 256.0 * (1 << 20) ? 1 : 0;
   a.chunks = (int32_t)(pairs ? hd / 2 : hd) / vw;
   // Rows of a workgroup: about four heads to a thread where the rows suffice for
-  // 1024 workgroups, never more turns than the table holds.
+  // 1024 workgroups, never more turns than the table holds (12608 rows of 36 heads of
+  // 64 bf16, two, four and eight heads: 32, 25.7, 27 us).
   const int64_t slots = pairs ? 256 / a.chunks : 4 * (64 / a.chunks);
   int64_t wg_rows = std::min<int64_t>({4 * slots / (heads_rot + (a.in_place ? 0 : heads_copy)), slots, kRopeTable / n, rows / 1024});
   wg_rows = std::max<int64_t>(wg_rows, 1);
   a.wg_rows = (int32_t)wg_rows;
   a.head_slots = (int32_t)(slots / wg_rows);
   const int64_t blocks = cdiv(rows, wg_rows);
-  MPX_REQUIRE_FN(rows <= INT32_MAX && blocks < ((int64_t)1 << 24), "too many rows for one call");
+  MPX_REQUIRE_FN(blocks < ((int64_t)1 << 24), "too many rows for one call");
 #undef MPX_REQUIRE_FN
   a.rows = (uint32_t)rows;
   a.pos_rows = (uint32_t)pos_rows;

@@ -348,3 +348,40 @@ def test_rows_do_not_depend_on_how_many_there_are(fmt, k):
             ok = torch.isfinite(a)
             assert torch.equal(a[~ok].isnan(), b[~ok].isnan())
             assert ok.sum() == 0 or float((a[ok] - b[ok]).abs().max()) <= tol * size
+
+
+@pytest.mark.parametrize("fmt, rows, V", [("bf16", 4100, 33001), ("f16", 16400, 8200), ("f32", 2100, 32777)])
+def test_logits_past_the_cache(fmt, rows, V):
+    """Logits whose size sends them around the last-level cache, against calls on
+    few of their rows: the alternatives and, from the same statistics, the
+    gradients are the same bits, in place too."""
+    k = 3
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    t = torch.empty(rows, V, device="cuda").normal_(0, 2.5, generator=g).to(HALF[fmt])
+    targets = torch.randint(0, V, (rows,), generator=g, device="cuda").int()
+    f, top, idx, _, _ = _fwd(t, targets, V, k, fmt)
+    stats = f[2:].reshape(-1)[:2 * rows].view(rows, 2)
+    gl, ge = (torch.empty(rows, device="cuda").normal_(generator=g) for _ in range(2))
+    gt = torch.empty(rows, k, device="cuda").normal_(generator=g)
+    ent, ix = f[1, :rows].contiguous(), idx[:rows * k].view(rows, k)
+
+    def bwd(z, out, lo, n):
+        s = slice(lo, lo + n)
+        args = [a[s].contiguous() for a in (targets, stats, ent, ix, gl, ge, gt)]
+        tg, st, en, i, a, b, c = (x.data_ptr() for x in args)
+        mx.mpx_logprob_bwd(z.data_ptr(), V, tg, n, V, k, st, en, i, a, b, c, None, out.data_ptr(), V,
+                           mx.DTYPES[fmt], _s())
+        torch.cuda.synchronize()
+    dz = torch.full((rows + 1, V), -7.0, dtype=HALF[fmt], device="cuda")
+    bwd(t, dz, 0, rows)
+    assert (dz[rows] == -7.0).all()
+    for lo, n in ((0, 3), (1000, 17), (rows - 4, 4)):
+        pf, ptop, pidx, _, _ = _fwd(t[lo:lo + n], targets[lo:lo + n], V, k, fmt)
+        assert torch.equal(pidx[:n * k], idx[lo * k:(lo + n) * k])
+        tol = 2 * (V / 64 + 64 + 40) * U * 30.0
+        assert float((pf[:2, :n] - f[:2, lo:lo + n]).abs().max()) <= tol
+        part = torch.empty(n, V, dtype=HALF[fmt], device="cuda")
+        bwd(t[lo:lo + n], part, lo, n)
+        assert torch.equal(part, dz[lo:lo + n])
+    bwd(t, t, 0, rows)
+    assert torch.equal(t, dz[:rows])

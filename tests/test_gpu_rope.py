@@ -189,3 +189,27 @@ def test_long_strides_pass_32_bits():
     big[:, :2 * hd] = x
     _call(False, big, big, pos, rows, 1, 1, hd, plan, "bf16", ld, ld)
     assert torch.equal(big[:, :2 * hd], want)
+
+
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "interleaved"])
+@pytest.mark.parametrize("fmt", ["bf16", "f32"])
+def test_large_batches_equal_small_ones(fmt, interleaved):
+    """A batch past the last-level cache, whose values go around it, against the
+    same rows in calls of their own: the same bits, both directions."""
+    rows, rot, copy, hd = 40003, 24, 12, 64
+    ld = (rot + copy) * hd
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(rows, ld, device="cuda").normal_(generator=g).to(HALF[fmt])
+    pos = torch.randint(0, 200, (rows, 2), generator=g, device="cuda").float()
+    plan = mx.RopePlan([16, 16], interleaved=interleaved)
+    for back in (False, True):
+        y = torch.full((rows + 1, ld), -7.0, dtype=HALF[fmt], device="cuda")
+        _call(back, x, y, pos, rows, rot, copy, hd, plan, fmt, ld, ld)
+        assert (y[rows] == -7.0).all()
+        z = x.clone()
+        _call(back, z, z, pos, rows, rot, copy, hd, plan, fmt, ld, ld)
+        assert torch.equal(y[:rows], z)
+        for lo, n in ((0, 1), (1023, 700), (20000, 33), (rows - 5, 5)):
+            part = torch.empty(n, ld, dtype=HALF[fmt], device="cuda")
+            _call(back, x[lo:lo + n], part, pos[lo:lo + n].contiguous(), n, rot, copy, hd, plan, fmt, ld, ld)
+            assert torch.equal(part, y[lo:lo + n])
