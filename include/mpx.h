@@ -12,6 +12,11 @@
  *   §3.3  DynamicLossScaling.adjust       -> mpx_scale_update
  *   §3.5  optimizer_update (skip when     -> mpx_adamw_masked
  *         gradients are not finite)
+ * Beside that path, for the same training step: activation checkpoints in 8
+ * bits and the linear backward that reads them (mpx_act8_pack,
+ * mpx_act8_unpack, mpx_linear_bwd_act8), rotary positions with several axes
+ * (mpx_rope_fwd, mpx_rope_bwd), per-token log probabilities with entropy, top
+ * alternatives and their gradient (mpx_logprob_fwd, mpx_logprob_bwd).
  *
  * Conventions shared by every call:
  *  - Pointers named d_* and every tensor pointer are DEVICE pointers; the
@@ -27,15 +32,16 @@
  *    order; results are visible to later calls on the same stream.
  *  - Full precision (MPX's use_mixed_precision switched off, the baseline of
  *    §4): mpx_linear_fwd/bwd, mpx_gemm_batched, mpx_layernorm_fwd/bwd,
- *    mpx_softmax_fwd/bwd, mpx_cross_entropy, mpx_mse, mpx_patchify_cast and
- *    mpx_embed_assemble(_bwd) also accept dt == MPX_F32: every tensor named
+ *    mpx_softmax_fwd/bwd, mpx_cross_entropy, mpx_mse, mpx_patchify_cast,
+ *    mpx_embed_assemble(_bwd), mpx_rope_fwd/bwd and mpx_logprob_fwd/bwd also accept dt == MPX_F32: every tensor named
  *    "half" in their description is then float32 and half() is the identity
  *    (d_nonfinite must be NULL).
  *  - Return value: MPX_OK (0) or a negative code; mpx_last_error() gives a
  *    message (per host thread).  Invalid arguments are detected before
  *    anything is launched.  Non-finite DATA is never an error: it is reported
  *    through the non-finite count (MPX §2.1: overflow makes the step skip).
- *  - The calls that write parameter gradients (mpx_linear_bwd's dW and db,
+ *  - The calls that write parameter gradients (mpx_linear_bwd's and
+ *    mpx_linear_bwd_act8's dW and db,
  *    mpx_layernorm_bwd's and mpx_classifier_head's dgamma and dbeta,
  *    mpx_embed_assemble_bwd's dcls and dpos) take a nullable int32 device
  *    counter d_nonfinite: when set, the number of those half results whose
@@ -452,7 +458,8 @@ int mpx_cross_entropy(const void* Z, int64_t ldz, const int32_t* labels, int64_t
  * nothing else has stats (-inf, 0), logp and top_logp -inf, entropy 0 and
  * top_idx 0 .. k-1.  A NaN or +inf logit makes the row's float results NaN
  * (top_idx then lists NaN before +inf before the rest).  The padding columns V .. ldz-1
- * are never read.  Results do not depend on what else runs (no atomics).
+ * are never read.  Results do not depend on what else runs (no atomics);
+ * the order of a row's float32 sums goes by rows and V.
  * workspace: mpx_logprob_workspace(rows, V, k) bytes (device; may be NULL when
  * that is 0), not shared by calls that overlap.  dt: MPX_F16, MPX_BF16 or
  * MPX_F32; pointers aligned to their element. */

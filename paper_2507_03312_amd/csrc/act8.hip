@@ -73,7 +73,8 @@ struct Act8Place {
   }
 };
 
-// Bound by HBM: 2 bytes in and 1 out per value.  One workgroup reads its rows
+// Bound by HBM: 2 bytes in and 1 out per value (12608 x 2304 bf16 15.4 us, 5.7 TB/s;
+// one thread per column and group 23.5 us at 12608 x 768, this 7.7).  One workgroup reads its rows
 // once, 4 vectors of 16 bytes in flight per thread, finds the groups' largest
 // magnitudes in the packed halves (as integers; a thread that sees +-inf or NaN,
 // or the largest scale, takes a slower path of its own) and through LDS across
@@ -159,6 +160,8 @@ __global__ __launch_bounds__(256) void act8_pack_kernel(const uint16_t* __restri
   }
 }
 
+// The same places the other way round (16640 x 1536 f16 15 us, 5.1 TB/s; one thread per
+// column and group 43).
 template <int DT>
 __global__ __launch_bounds__(256) void act8_unpack_kernel(const uint8_t* __restrict__ codes,
                                                           const uint8_t* __restrict__ scales,

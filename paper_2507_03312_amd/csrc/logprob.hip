@@ -158,8 +158,8 @@ struct BestK {
 };
 
 // Bound by HBM where the logits are many and the alternatives few (4096 x 65536
-// bf16: 99 us without, 5.4 TB/s; 107 with 4, 130 with 16), by the latency of the
-// best's ordering in a few rows.
+// bf16: 95 us without entropy and alternatives, 5.7 TB/s; 109 with both and 4 of them,
+// 128 with 16), by the latency of the best's ordering in a few rows.
 // One wave's pass over a row: per lane the moments about `ref` (moved only when a
 // logit exceeds it by 8, so nearly never after the first vectors; the sums are
 // float32 and e^8 of them costs no accuracy), the largest logit, and over the wave
@@ -399,8 +399,8 @@ struct LogprobGrad {
   const mpx_scale_state* state;
 };
 
-// Bound by HBM (one read and one write of every logit: 4096 x 65536 bf16 186 us,
-// 5.8 TB/s).  A wave's part of a row: up to U vectors per lane, all loaded before
+// Bound by HBM (one read and one write of every logit: 4096 x 65536 bf16 173 us,
+// 6.2 TB/s).  A wave's part of a row: up to U vectors per lane, all loaded before
 // the first store.  With t = (z - m) - ln S and p = e^t the gradient is
 //   p (c0 + c1 t),  c0 = -scale (sum of the upstream cotangents + g_H H),
 //   c1 = -scale g_H,
