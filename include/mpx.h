@@ -33,9 +33,9 @@
  *  - Full precision (MPX's use_mixed_precision switched off, the baseline of
  *    §4): mpx_linear_fwd/bwd, mpx_gemm_batched, mpx_layernorm_fwd/bwd,
  *    mpx_softmax_fwd/bwd, mpx_cross_entropy, mpx_mse, mpx_patchify_cast,
- *    mpx_embed_assemble(_bwd), mpx_rope_fwd/bwd and mpx_logprob_fwd/bwd also accept dt == MPX_F32: every tensor named
- *    "half" in their description is then float32 and half() is the identity
- *    (d_nonfinite must be NULL).
+ *    mpx_embed_assemble(_bwd), mpx_rope_fwd/bwd and mpx_logprob_fwd/bwd also
+ *    accept dt == MPX_F32: every tensor named "half" in their description is
+ *    then float32 and half() is the identity (d_nonfinite must be NULL).
  *  - Return value: MPX_OK (0) or a negative code; mpx_last_error() gives a
  *    message (per host thread).  Invalid arguments are detected before
  *    anything is launched.  Non-finite DATA is never an error: it is reported
@@ -281,7 +281,8 @@ int mpx_gemm_set_config(int32_t config);
 #define MPX_ACT8_GROUP 32
 
 /* codes, scales = checkpoint of X [M, K] half with row stride ldx (elements,
- * >= K).  M, K >= 1; any alignment. */
+ * >= K).  M, K >= 1; X at any 2-byte address, codes and scales at any.  M * K (K
+ * rounded up to a multiple of 8) up to 2^36, with K < 8 up to 2^31, K < 2^31. */
 int mpx_act8_pack(const void* X, int64_t ldx, uint8_t* codes, uint8_t* scales, int64_t M, int64_t K,
                   mpx_dtype dt, void* stream);
 
@@ -320,7 +321,8 @@ size_t mpx_linear_bwd_act8_workspace(int64_t M, int64_t N, int64_t K);
  *   y0 = x0 cos - x1 sin,  y1 = x1 cos + x0 sin.
  * Angles are taken in float64 and reduced to less than one turn before they
  * are rounded, so positions far out lose nothing; the turn is computed in
- * float32 and rounded once.  A position of 0 leaves its values as they are. */
+ * float32 and rounded once.  A position of 0 leaves finite values as they are (an
+ * infinite one or NaN reaches its partner at any position). */
 #define MPX_ROPE_MAX_AXES 4
 typedef struct {
   int32_t axes;                       /* 1 .. MPX_ROPE_MAX_AXES */
@@ -338,7 +340,8 @@ typedef struct {
  * exact up to 2^24; a position that is not finite makes its values NaN).  plan
  * is a host pointer, read during the call.  rows, heads_rot, pos_rows >= 1,
  * heads_copy >= 0, 2 <= hd <= 512, 2 * sum(pairs) <= hd.  dt: MPX_F16,
- * MPX_BF16 or MPX_F32; pointers aligned to their element. */
+ * MPX_BF16 or MPX_F32; pointers aligned to their element.  rows < 2^31, at most
+ * 2^20 heads of either kind, and 2^24 workgroups (always enough for rows < 2^24). */
 int mpx_rope_fwd(const void* X, int64_t ldx, void* Y, int64_t ldy, const float* pos,
                  int64_t pos_rows, int64_t rows, int64_t heads_rot, int64_t heads_copy, int64_t hd,
                  const mpx_rope_plan* plan, mpx_dtype dt, void* stream);
@@ -453,7 +456,7 @@ int mpx_cross_entropy(const void* Z, int64_t ldz, const int32_t* labels, int64_t
  * 0, and no gradient from g_logp below), one of V or more gives NaN (never an
  * out-of-range read).  Any of logp (with targets), entropy, stats ([rows, 2])
  * and the pair top_logp / top_idx (with k >= 1) may be NULL, not all; all are
- * float32 but top_idx (int32).  0 <= k <= MPX_LOGPROB_MAX_K, k <= V < 2^31; rows >= 1.
+ * float32 but top_idx (int32).  0 <= k <= MPX_LOGPROB_MAX_K, k <= V < 2^31; 1 <= rows <= 2^23.
  * Logits of -inf (masked ones) have probability 0 and add nothing; a row of
  * nothing else has stats (-inf, 0), logp and top_logp -inf, entropy 0 and
  * top_idx 0 .. k-1.  A NaN or +inf logit makes the row's float results NaN
@@ -481,7 +484,8 @@ size_t mpx_logprob_workspace(int64_t rows, int64_t V, int32_t k);
  * Padding columns are left as they are.  Masked logits get a gradient of 0, and
  * so does every logit of a row of nothing but masked ones; a row whose stats
  * are NaN gets NaN.  A target of V or more gives a NaN row, a top_idx outside
- * [0, V) is NaN likewise. */
+ * [0, V) is NaN likewise.  One call takes rows * ceil(V / 2048) <= 2^25 (float32:
+ * ceil(V / 1024)). */
 int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t rows, int64_t V,
                     int32_t k, const float* stats, const float* entropy, const int32_t* top_idx,
                     const float* g_logp, const float* g_entropy, const float* g_top,
