@@ -117,6 +117,9 @@ struct BestK {
       thr_f = rank_value(t - 2);  // a value below the bound's (t - 1 may be -0, which 0 does not exceed)
     }
   }
+  // Lanes read what others of their wave wrote.  LDS serves a wave in order; this
+  // keeps the compiler from moving such accesses across each other (no instruction).
+  __device__ __forceinline__ static void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
   // one key per lane (0: none)
   __device__ __forceinline__ void offer(uint64_t key) {
     const uint64_t mask = __builtin_amdgcn_ballot_w64(key > lim);
@@ -135,10 +138,8 @@ struct BestK {
     count += __builtin_popcountll(mask);
   }
   // puts the buffer in falling order, drops all but k; places without a key hold 0
-  // (Lanes read what others of their wave wrote.  LDS serves a wave in order, and
-  // indexes unknown to the compiler keep it from moving one access of buf across
-  // another; fences between them cost 4096 x 65537 bf16 12 us of 103.)
   __device__ __forceinline__ void order() {
+    in_order();
     const uint64_t a = lane < count ? buf[lane] : 0, b = 64 + lane < count ? buf[64 + lane] : 0;
     int ra = 0, rb = 0;
 #pragma unroll 4
@@ -147,9 +148,12 @@ struct BestK {
 #pragma unroll 4
       for (int j = 0; j < count; ++j) rb += buf[j] > b ? 1 : 0;
     }
+    in_order();
     if (lane < k) buf[lane] = 0;
+    in_order();
     if (a && ra < k) buf[ra] = a;
     if (b && rb < k) buf[rb] = b;
+    in_order();
     if (count >= k) {
       count = k;
       lim = max(lim, buf[k - 1]);
