@@ -557,7 +557,7 @@ struct StagedAct8 {
   static constexpr int RSTEP = 64 / CH * NWAVES;
   static_assert(32 % RSTEP == 0, "a vector's k rows do not tell its group");
   u32x2 v[2][Q], sv[2][2];
-  uint32_t off[Q], soff;
+  uint32_t off[Q], soff;  // lane offsets from 8 codes before the tile's first
   int64_t ld;
   int c8, r0, rv;
   int krem[2];
@@ -567,7 +567,7 @@ struct StagedAct8 {
     rv = (int)min<int64_t>(left, 1 << 20);
     r0 = 64 / CH * wave + lane / CH;
     c8 = 8 * dma_chunk<ROWS, false>(r0, lane % CH);
-    soff = (uint32_t)max(min(c8, rv - 8), 0);
+    soff = (uint32_t)(8 + min(c8, rv - 8));
 #pragma unroll
     for (int q = 0; q < Q; ++q) off[q] = (uint32_t)((r0 + RSTEP * q) * ld) + soff;
   }
@@ -593,18 +593,19 @@ struct StagedAct8 {
         for (int e = 0; e < 8; ++e) sv[P][i][e / 4] |= (uint32_t)row[min(c8 + e, last)] << (8 * (e & 3));
       }
     } else {
+      const uint8_t *base = tile - 8, *sbase = stile - 8;  // never accessed themselves
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         uint32_t o = off[q];
         if (kr < 64) o -= (uint32_t)(max(0, r0 + RSTEP * q - (kr - 1)) * ld);  // uniform: the last k tile
         if (past) o = (uint32_t)__builtin_amdgcn_readfirstlane((int)o);
-        v[P][q] = *reinterpret_cast<const u32x2_any*>(tile + o);
+        v[P][q] = *reinterpret_cast<const u32x2_any*>(base + o);
       }
       uint32_t so = soff;
       if (past) so = (uint32_t)__builtin_amdgcn_readfirstlane((int)so);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        sv[P][i] = *reinterpret_cast<const u32x2_any*>(stile + (min(i, (kr - 1) / MPX_ACT8_GROUP) * ld + so));
+        sv[P][i] = *reinterpret_cast<const u32x2_any*>(sbase + (min(i, (kr - 1) / MPX_ACT8_GROUP) * ld + so));
     }
   }
   template <int P>
