@@ -34,9 +34,9 @@ static GemmArgs base_args() {
 // The most splits choose_splits considers for a reduction of length K over an
 // M x N output.  It never falls as K grows, where the chosen count may (2304 x 768:
 // 4 for 7936 rows, 2 for 7952, 4 again for 12608).
-static int64_t most_splits(int64_t M, int64_t N, int64_t K) {
+static int64_t most_splits(int64_t M, int64_t N, int64_t K, int64_t most = 16, int64_t least_rows = 1024) {
   const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
-  return std::max<int64_t>(1, std::min<int64_t>({512 / tiles, 16, K / 1024}));
+  return std::max<int64_t>(1, std::min<int64_t>({512 / tiles, most, K / least_rows}));
 }
 
 // Cost of a k tile of 64 (us) with one and with two workgroups per CU, of the
@@ -47,7 +47,7 @@ static int64_t most_splits(int64_t M, int64_t N, int64_t K) {
 // (float32, staged) ran unsplit, 487 us against 319 in 2 splits, and 2298 x
 // 220 over 16955 in 7 splits, 382 against 265 in 14.
 struct SplitCost {
-  double one, two;
+  double one, two, join = 3.0, partial = 3.5e-6;
 };
 static constexpr SplitCost kHalfCost = {0.9, 1.1}, kHalfStagedCost = {1.6, 1.9};
 static constexpr SplitCost kF32Cost = {4.5, 8.0}, kF32StagedCost = {9.7, 13.5};
@@ -71,9 +71,8 @@ static constexpr SplitCost kF32Cost = {4.5, 8.0}, kF32StagedCost = {9.7, 13.5};
 // the fastest count where the operands are copied directly (0.2% with a charge of 2.3),
 // 0.7% staged.  With 0.74 and 1.07 for both it was 1.8% and 2.8%: 1088 x 3008 over 7168
 // rows unsplit 99 us, in 2 splits 73; 3072 x 1024 over 6076 (staged) 114 and 80.
-static int choose_splits(int64_t M, int64_t N, int64_t K, SplitCost c) {
+static int choose_splits(int64_t M, int64_t N, int64_t K, SplitCost c, int64_t most) {
   const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
-  const int64_t most = most_splits(M, N, K);
   int best = 1;
   double least = 0.0;
   for (int64_t s = 1; s <= most; ++s) {
@@ -81,7 +80,7 @@ static int choose_splits(int64_t M, int64_t N, int64_t K, SplitCost c) {
     const int64_t wgs = tiles * s, full = wgs / 512, last = (wgs % 512 + 255) / 256;
     const double k_tile = c.two * (double)full + (last == 2 ? c.two : last == 1 ? c.one : 0.0);
     const double t = (double)((K + 64 * s - 1) / (64 * s)) * k_tile +
-                     (s > 1 ? 3.0 + 3.5e-6 * (double)(s * M * N) : 0.0);
+                     (s > 1 ? c.join + c.partial * (double)(s * M * N) : 0.0);
     if (least == 0.0 || t < least) {
       least = t;
       best = (int)s;
@@ -92,29 +91,41 @@ static int choose_splits(int64_t M, int64_t N, int64_t K, SplitCost c) {
 
 // split-K plan of a reduction of length Mr over an N x K weight gradient:
 // sp splits of k_split rows each (a multiple of 64), every split non-empty
-static void split_plan(int64_t N, int64_t K, int64_t Mr, SplitCost c, int& sp, int64_t& k_split) {
-  sp = choose_splits(N, K, Mr, c);
+static void split_plan(int64_t N, int64_t K, int64_t Mr, SplitCost c, int64_t most, int& sp, int64_t& k_split) {
+  sp = choose_splits(N, K, Mr, c, most);
   k_split = ((Mr + sp - 1) / sp + 63) / 64 * 64;
   sp = (int)((Mr + k_split - 1) / k_split);
 }
 
-// Tile height and splits of a weight gradient from an 8-bit checkpoint with
-// direct copies: 64 x 128 tiles, four workgroups per CU, or 128 x 128 ones, two, by
-// estimated time.  A round of o workgroups per CU takes its k tiles x k_us[o - 1]
-// plus tile_us; partials cost 2.5 us per million outputs and split (what they cost
-// beside other work; alone less).  Constants of least loss on 70% of 158 measured
-// gradients (100 to 60000 rows, 128 to 3200 outputs a side, every height and
-// split count timed): on the others the choice is 0.3% slower than the fastest,
-// 64-high tiles alone at least 1.6%, 128-high ones 14%.  Examples (us, 64 / 128
-// high, each with its best split count): 1000 x 768 x 768 13 / 18, 2100 x 640 x 512
-// 16 / 20, 16640 x 384 x 1536 38 / 38, 12608 x 2304 x 768 83 / 69.
+// A weight gradient from an 8-bit checkpoint: its splits may be shorter than the
+// half operands' above (1024 rows each: 1672 x 320 x 192 unsplit 19.3 us, in 7 splits
+// 10.6), with direct copies up to 16 of at least 192 rows, register-staged, where a k
+// tile takes longer, up to 32 of at least 128 (2471 x 287 x 267 in 2 42.5, in 16 21.5).
+static int64_t act8_most_splits(int64_t N, int64_t K, int64_t Mr, bool direct) {
+  return direct ? most_splits(N, K, Mr, 16, 192) : most_splits(N, K, Mr, 32, 128);
+}
+
+// Its register-staged tiles' cost, of least loss on 153 gradients (100 to 50000 rows,
+// 61 to 3200 outputs a side, all odd): 0.5% slower than the fastest count.  An unsplit
+// one has smaller tiles, so the join's charge holds more than the join.
+static constexpr SplitCost kAct8StagedCost = {1.0, 1.35, 11.0, 2.5e-6};
+
+// With direct copies, tile height and splits: 64 x 128 tiles, four workgroups per CU,
+// or 128 x 128 ones, two, by estimated time.  A round of o workgroups per CU takes its
+// k tiles x k_us[o - 1] plus tile_us; partials cost 2.5 us per million outputs and
+// split (what they cost beside other work; alone less).  Of 275 measured gradients (100
+// to 60000 rows, 64 to 3200 outputs a side, both heights and the split counts timed)
+// the choice is 0.5% slower than the fastest on average; 64-high tiles alone at least
+// 1.6%, 128-high ones 14%.  Examples (us, 64 / 128 high, each with its best split count):
+// 1000 x 768 x 768 13 / 18, 2100 x 640 x 512 15 / 17, 16640 x 384 x 1536 38 / 38,
+// 12608 x 2304 x 768 83 / 69.
 static void act8_plan(int64_t N, int64_t K, int64_t Mr, int& rows, int& sp, int64_t& k_split) {
   struct Cost {
     int rows, per_cu;
     double k_us[4], tile_us;
   };
   static const Cost costs[] = {{64, 4, {0.67, 0.72, 0.80, 1.32}, 2.6}, {128, 2, {0.72, 0.80, 0, 0}, 2.9}};
-  const int64_t most = most_splits(N, K, Mr);
+  const int64_t most = act8_most_splits(N, K, Mr, true);
   double least = 0.0;
   for (const Cost& c : costs) {
     const int64_t tiles = cdiv(N, c.rows) * cdiv(K, 128), slots = 256 * c.per_cu;
@@ -123,7 +134,7 @@ static void act8_plan(int64_t N, int64_t K, int64_t Mr, int& rows, int& sp, int6
       const int64_t full = tiles * s / slots, last = cdiv(tiles * s % slots, 256);
       const double t = (double)full * (nk * c.k_us[c.per_cu - 1] + c.tile_us) +
                        (last ? nk * c.k_us[last - 1] + c.tile_us : 0.0) +
-                       (s > 1 ? 0.34 + 2.5e-6 * (double)(s * N * K) : 0.0);
+                       (s > 1 ? 2.0 + 2.5e-6 * (double)(s * N * K) : 0.0);
       if (least == 0.0 || t < least) {
         least = t;
         rows = c.rows;
@@ -197,13 +208,17 @@ static size_t db_partials_count(int splits, int64_t N, int64_t K) {
   return (size_t)splits * (size_t)((K + 127) / 128) * N;
 }
 
-extern "C" size_t mpx_linear_bwd_workspace(int64_t M, int64_t N, int64_t K) {
+// sized for the most splits any M up to this one may take: a workspace for the
+// largest batch serves every smaller one
+static size_t linear_bwd_workspace(int64_t M, int64_t N, int64_t K, bool a8) {
   if (M < 1 || N < 1 || K < 1) return 0;
-  // sized for the most splits any M up to this one may take: a workspace for the
-  // largest batch serves every smaller one
-  const int s = (int)most_splits(N, K, M);
+  const int s = (int)(a8 ? act8_most_splits(N, K, M, false) : most_splits(N, K, M));
   size_t ws = s > 1 ? db_partials_offset(s, N, K) + db_partials_count(s, N, K) * sizeof(float) : 0;
   return std::max(ws, colsum_workspace(M, N)) + 256;
+}
+
+extern "C" size_t mpx_linear_bwd_workspace(int64_t M, int64_t N, int64_t K) {
+  return linear_bwd_workspace(M, N, K, false);
 }
 
 // The layer's kept activations as 8-bit checkpoints: its input and, behind GELU,
@@ -242,7 +257,7 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
   MPX_REQUIRE_FN(dt != MPX_F32 || !d_nonfinite, "d_nonfinite is counted for half gradients only");
   if (dW || db) {  // only the weight and bias gradients use the workspace
     // a bias-only call needs just the column partials
-    const size_t need = dW ? mpx_linear_bwd_workspace(M, N, K) : colsum_workspace(M, N) + 256;
+    const size_t need = dW ? linear_bwd_workspace(M, N, K, a8 != nullptr) : colsum_workspace(M, N) + 256;
     if (ws_bytes < need || !workspace) {
       set_error(std::string(fn) + ": workspace of " + std::to_string(need) + " bytes required");
       return MPX_ERR_WORKSPACE;
@@ -271,7 +286,8 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
       g.db = (float*)db;
       int sp;
       int64_t ks;
-      split_plan(N, K, M, gemm_f32_direct(g, false, false) ? kF32Cost : kF32StagedCost, sp, ks);
+      split_plan(N, K, M, gemm_f32_direct(g, false, false) ? kF32Cost : kF32StagedCost, most_splits(N, K, M),
+                 sp, ks);
       if (sp > 1) {
         g.splits = sp;
         g.k_split = ks;
@@ -327,9 +343,11 @@ static int linear_bwd(const char* fn, const void* X, const void* W, const void* 
     int64_t ks;
     if (a8 && act8_dma_ok(g))
       act8_plan(N, K, M, g.act8_rows, sp, ks);
+    else if (a8)
+      split_plan(N, K, M, kAct8StagedCost, act8_most_splits(N, K, M, false), sp, ks);
     else
-      split_plan(N, K, M, !a8 && dma_ok(g, operands_aligned(g), false, false) ? kHalfCost : kHalfStagedCost, sp,
-                 ks);
+      split_plan(N, K, M, dma_ok(g, operands_aligned(g), false, false) ? kHalfCost : kHalfStagedCost,
+                 most_splits(N, K, M), sp, ks);
     if (sp > 1) {
       g.splits = sp;
       g.k_split = ks;
@@ -380,7 +398,7 @@ extern "C" int mpx_linear_bwd(const void* X, const void* W, const void* dY, cons
 }
 
 extern "C" size_t mpx_linear_bwd_act8_workspace(int64_t M, int64_t N, int64_t K) {
-  return mpx_linear_bwd_workspace(M, N, K);
+  return linear_bwd_workspace(M, N, K, true);
 }
 
 extern "C" int mpx_linear_bwd_act8(const uint8_t* Xc, const uint8_t* Xs, const void* W, const void* dY,

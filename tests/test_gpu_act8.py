@@ -176,6 +176,24 @@ def test_fewer_than_8_columns_in_the_last_tile(fmt, mnk, off):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("off", [0, 3], ids=["aligned", "any"])
+@pytest.mark.parametrize("mnk", [(449, 64, 128), (1672, 320, 192), (2050, 64, 16), (3089, 8, 8), (4223, 79, 131),
+                                 (2471, 287, 267), (4161, 64, 61), (3000, 6, 9)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_short_splits(fmt, mnk, off):
+    """Reductions of a few k tiles each in many splits, the last one shorter: dW
+    and db against float64 products, one rounding and two float32 orders."""
+    M, N, K = mnk
+    x, pre, w, dy = _problem(fmt, M, N, K, 4)
+    _, dw, db, bad, xv, _ = _run(fmt, M, N, K, x, pre, w, dy, mx.MPX_ACT_NONE, "wb", off=off)
+    _, rdw, rdb = ops.linear_bwd(Policy(fmt), xv, w, dy)
+    assert_within(to_host(dw), rdw, gemm_bound(dy.T, xv, rdw, fmt, M), "dW")
+    colb = ulp(rdb, fmt) + 2.0 * M * 2.0 ** -24 * np.abs(dy.astype(np.float64)).sum(axis=0)
+    assert_within(to_host(db), rdb, colb, "db")
+    assert bad == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("mnk", [(1100, 128, 256), (333, 72, 40), (64, 64, 128)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_subsets_are_the_full_call(fmt, mnk):
