@@ -194,6 +194,26 @@ def test_short_splits(fmt, mnk, off):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("wide", ["N", "K"])
+def test_every_width(fmt, wide):
+    """dX through GELU', dW and db at every width up to past the widest tile, with
+    bounds as in test_linear_bwd_act8."""
+    for n in range(1, 150):
+        M, (N, K) = (33, 70)[n % 2], (n, 41) if wide == "N" else (24, n)
+        x, pre, w, dy = _problem(fmt, M, N, K, 7)
+        dx, dw, db, bad, xv, pv = _run(fmt, M, N, K, x, pre, w, dy, mx.MPX_ACT_GELU_TANH, off=n % 3)
+        pol = Policy(fmt)
+        rdx, rdw, rdb = ops.linear_bwd(pol, xv, w, dy)
+        bound = 1.13 * gemm_bound(dy, w, rdx, fmt, N)
+        rdx = ops.gelu_bwd(pol, pv, rdx)
+        assert_within(to_host(dx), rdx, bound + ulp(rdx, fmt), f"dX {n}")
+        assert_within(to_host(dw), rdw, gemm_bound(dy.T, xv, rdw, fmt, M), f"dW {n}")
+        colb = ulp(rdb, fmt) + 2.0 * M * 2.0 ** -24 * np.abs(dy.astype(np.float64)).sum(axis=0)
+        assert_within(to_host(db), rdb, colb, f"db {n}")
+        assert bad == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("mnk", [(1100, 128, 256), (333, 72, 40), (64, 64, 128)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_subsets_are_the_full_call(fmt, mnk):
