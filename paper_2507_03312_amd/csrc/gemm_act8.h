@@ -325,6 +325,7 @@ void gemm_act8_kernel(GemmArgs g) {
 // operands.
 template <int DT>
 static hipError_t run_gemm_act8(GemmArgs g, hipStream_t s, bool* db_fused) {
+  if (!g.b8 || !g.b8_scale || g.dact8) return hipErrorInvalidValue;  // no kernel here has GELU'
   const int64_t lim = ((int64_t)1 << 31) - 4096;
   const bool any = g.M < 8 || g.N < 8 || g.lda * 256 >= lim || g.ldb * 64 >= lim;
   const int64_t t64 = ((g.M + 63) / 64) * ((g.N + 63) / 64);

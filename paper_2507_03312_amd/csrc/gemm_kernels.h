@@ -1050,6 +1050,14 @@ static int epilogue_mask(const GemmArgs& g) {
          (g.dact ? EPI_DACT : 0) | (g.resid ? EPI_RESID : 0) | (g.dact8 ? EPI_DACT8 : 0);
 }
 
+// Whether a product of half operands reads all that its arguments hold.  GELU' from
+// an 8-bit checkpoint is compiled in alone (EPI_DACT8), for one dX product: kernels
+// of other layouts or epilogues, the generic one too, would leave it out, and none
+// takes an 8-bit B (gemm_act8.h).
+static bool half_product_ok(const GemmArgs& g, bool ak, bool bk, int64_t nbatch) {
+  return !g.b8 && (!g.dact8 || (g.dact8_scale && ak && !bk && nbatch == 1 && epilogue_mask(g) == EPI_DACT8));
+}
+
 // Whole-tile epilogue preconditions that do not depend on the tile: output,
 // pre-activation, GELU' and residual operands 16-byte aligned with row
 // strides a multiple of 8, the bias 8-byte aligned, and the per-lane 32-bit
@@ -1331,6 +1339,7 @@ static hipError_t launch_small(const GemmArgs& g, bool ak, bool bk, hipStream_t 
 template <int DT>
 static hipError_t run_gemm(GemmArgs g, bool ak, bool bk, int64_t nbatch, hipStream_t s,
                            bool* db_fused) {
+  if (!half_product_ok(g, ak, bk, nbatch)) return hipErrorInvalidValue;
   const int cfg = choose_config(g, operands_aligned(g), ak, bk, nbatch);
   const bool fuse = g.db && (cfg == 7 || cfg == 2 || (cfg == 1 && g.splits == 1)) && !ak && !bk &&
                     nbatch == 1 && (g.splits == 1 || g.dbp);
