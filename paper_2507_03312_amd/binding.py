@@ -48,6 +48,8 @@ class RopePlan(C.Structure):
         pairs = list(pairs)
         if not 1 <= len(pairs) <= MPX_ROPE_MAX_AXES:
             raise ValueError(f"1 to {MPX_ROPE_MAX_AXES} axes")
+        if not all(-2 ** 31 <= n < 2 ** 31 for n in pairs):  # ctypes would keep their lower 32 bits
+            raise ValueError("pairs must fit 32 bits")
         bases = [float(base)] * len(pairs) if isinstance(base, (int, float)) else list(base)
         if len(bases) != len(pairs):
             raise ValueError("one base, or one per axis")

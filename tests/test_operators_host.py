@@ -108,6 +108,16 @@ def test_rope_plan_of_the_binding(mx):
         mx.RopePlan([3, 5], base=[10.0])
 
 
+@pytest.mark.parametrize("pairs", [[2 ** 32 + 8, 3], [8, 2 ** 31], [-2 ** 32 + 4], [-2 ** 31 - 1]])
+def test_rope_plan_keeps_no_part_of_a_number(mx, pairs):
+    """Counts that do not fit the plan's fields are refused, not cut to 32 bits."""
+    with pytest.raises(ValueError, match="pairs"):
+        mx.RopePlan(pairs)
+    plan = mx.RopePlan([2 ** 31 - 1, -2 ** 31])   # they fit: the calls refuse them
+    assert list(plan.pairs)[:2] == [2 ** 31 - 1, -2 ** 31]
+    refused(mx, "pairs", mx.mpx_rope_fwd, p, 192, 4096, 192, p, 6, 12, 2, 1, 64, plan, mx.MPX_BF16, 0)
+
+
 # Z ldz targets rows V k logp entropy stats top idx dt ws bytes stream
 @pytest.mark.parametrize("change, match", [
     ({0: None}, "NULL"), ({2: None}, "targets"), ({3: 0}, "sizes"), ({4: 0}, "sizes"), ({4: 1 << 31}, "sizes"),
