@@ -11,9 +11,10 @@ S = |dY|^T |X|; a bias gradient within 2e-2 sum |dY|."""
 import numpy as np
 import pytest
 
-from oracle import logprob, rotary
+from oracle import act8, logprob, ops, rotary
 from oracle.numfmt import round_to
-from tests.gpu_util import HAVE_GPU
+from oracle.policy import Policy
+from tests.gpu_util import HAVE_GPU, assert_within, gemm_bound, to_host, ulp
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not HAVE_GPU, reason="no GPU")]
 
@@ -155,6 +156,34 @@ def test_one_training_pass(fmt, T):
     S = np.abs(dz).sum(axis=0)
     assert np.all(np.abs(db - dz.sum(axis=0)) <= 2e-2 * np.maximum(S, np.abs(dz.sum(axis=0)).max()))
     assert int(step.nf.item()) == 0
+
+
+@pytest.mark.parametrize("fmt", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [65, 130])
+def test_products_of_the_pass(fmt, T):
+    """Every checkpoint and every linear gradient of the pass from the operands that
+    the pass itself left: codes byte for byte, each element of dW, dX and db within
+    one rounding and two float32 summation orders of the float64 product."""
+    arrays = _arrays(fmt, T, 1)
+    step, pol = Pass(fmt, T, arrays), Policy(fmt)
+    step.run(torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    M = step.M
+    for name, dy, x, ck, w, dx, db in (("wv", step.dz, step.a, step.ac, step.wv, step.da, step.g["bv"]),
+                                       ("wo", step.da, step.o, step.oc, step.wo, step.do, None),
+                                       ("wq", step.dqkv, step.x, step.xc, step.wq, None, None)):
+        values, e = act8.pack(to_host(x), fmt)
+        assert np.array_equal(ck[0].cpu().numpy(), act8.code_bytes(values)), name
+        assert np.array_equal(ck[1].cpu().numpy(), (e + 127).astype(np.uint8)), name
+        xv, dy, w = act8.values(values, e), to_host(dy), to_host(w)
+        assert np.isfinite(dy).all() and np.abs(dy).max() > 0.0, name
+        rdx, rdw, rdb = ops.linear_bwd(pol, xv, w, dy)
+        assert_within(to_host(step.g[name]), rdw, gemm_bound(dy.T, xv, rdw, fmt, M), "d" + name)
+        if dx is not None:
+            assert_within(to_host(dx), rdx, gemm_bound(dy, w, rdx, fmt, len(w)), "dX of " + name)
+        if db is not None:
+            colb = ulp(rdb, fmt) + 2.0 * M * 2.0 ** -24 * np.abs(dy.astype(np.float64)).sum(axis=0)
+            assert_within(to_host(db), rdb, colb, "db")
 
 
 @pytest.mark.parametrize("fmt", ["f16", "bf16"])

@@ -142,6 +142,18 @@ def test_logprob_workspace_is_checked(mx):
                     p if k else None, mx.MPX_F16, None, need, 0)
 
 
+@pytest.mark.parametrize("rows, V, k", [(1, 1 << 20, 8), (4, 262144, 0), (2, 100000, 16), (1023, 65536, 4)])
+def test_logprob_workspace_of_split_rows(mx, rows, V, k):
+    """Few long rows are split: they need a workspace, and a call without it, or
+    with a byte less, is refused.  Rows that fill the chip need none."""
+    need = mx.mpx_logprob_workspace(rows, V, k)
+    assert need >= rows * 2 * (12 + 8 * k)   # at least two splits
+    top = p if k else None
+    for ws, n in ((p, need - 1), (None, need), (p, 0)):
+        refused(mx, "workspace", mx.mpx_logprob_fwd, p, V, p, rows, V, k, p, p, p, top, top, mx.MPX_F16, ws, n, 0)
+    assert mx.mpx_logprob_workspace(4096, V, k) == 0
+
+
 # Z ldz targets rows V k stats entropy idx g_logp g_entropy g_top state dZ ldo dt stream
 @pytest.mark.parametrize("change, match", [
     ({0: None}, "NULL"), ({6: None}, "NULL"), ({13: None}, "NULL"), ({3: 0}, "sizes"), ({4: 0}, "sizes"),
