@@ -297,6 +297,8 @@ int mpx_act8_unpack(const uint8_t* codes, const uint8_t* scales, void* Y, int64_
  *        MPX_ACT_GELU_TANH (the layer's input was gelu(P); its checkpoint is
  *        (Xc, Xs));
  *   dW = half(dY^T X);  db = half(sum_m dY[m,:]).
+ * The product is rounded to half before GELU' and again behind it, as in
+ * mpx_linear_bwd: the gradient is that call's on the widened values.
  * Shapes, subsets (dX, dW, db may be NULL, not all), d_nonfinite and errors as
  * mpx_linear_bwd; Xc and Xs are needed for dW only, Pc and Ps for dX through
  * GELU only.  dt == MPX_F16 or MPX_BF16; codes and scales at any address.  Whatever
@@ -322,7 +324,10 @@ size_t mpx_linear_bwd_act8_workspace(int64_t M, int64_t N, int64_t K);
  * Angles are taken in float64 and reduced to less than one turn before they
  * are rounded, so positions far out lose nothing; the turn is computed in
  * float32 and rounded once.  A position of 0 leaves finite values as they are (an
- * infinite one or NaN reaches its partner at any position). */
+ * infinite one or NaN reaches its partner at any position).  Each axis has its own
+ * ladder of frequencies, from 1 down to 1 / base[a] (exclusive), and its own
+ * section: one ladder that runs on over several axes, values paired across the
+ * whole head, and rescaled frequencies have no plan. */
 #define MPX_ROPE_MAX_AXES 4
 typedef struct {
   int32_t axes;                       /* 1 .. MPX_ROPE_MAX_AXES */
@@ -459,12 +464,14 @@ int mpx_cross_entropy(const void* Z, int64_t ldz, const int32_t* labels, int64_t
  * float32 but top_idx (int32).  0 <= k <= MPX_LOGPROB_MAX_K, k <= V < 2^31; 1 <= rows <= 2^23.
  * Logits of -inf (masked ones) have probability 0 and add nothing; a row of
  * nothing else has stats (-inf, 0), logp and top_logp -inf, entropy 0 and
- * top_idx 0 .. k-1.  A NaN or +inf logit makes the row's float results NaN
- * (top_idx then lists NaN before +inf before the rest).  The padding columns V .. ldz-1
+ * top_idx 0 .. k-1.  A NaN or +inf logit makes the row's float results NaN (but
+ * the logp of a row without a target, which stays 0; top_idx then lists NaN before
+ * +inf before the rest).  The padding columns V .. ldz-1
  * are never read.  Results do not depend on what else runs (no atomics);
  * the order of a row's float32 sums goes by rows and V.
  * workspace: mpx_logprob_workspace(rows, V, k) bytes (device; may be NULL when
- * that is 0), not shared by calls that overlap.  dt: MPX_F16, MPX_BF16 or
+ * that is 0; few long rows need it and many do not, so a size asked for one number
+ * of rows does not serve another), not shared by calls that overlap.  dt: MPX_F16, MPX_BF16 or
  * MPX_F32; pointers aligned to their element. */
 #define MPX_LOGPROB_MAX_K 16
 int mpx_logprob_fwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t rows, int64_t V,

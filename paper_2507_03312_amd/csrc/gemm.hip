@@ -106,7 +106,7 @@ static int64_t act8_most_splits(int64_t N, int64_t K, int64_t Mr, bool direct) {
 }
 
 // Its register-staged tiles' cost, of least loss on 153 gradients (100 to 50000 rows,
-// 61 to 3200 outputs a side, all odd): 0.5% slower than the fastest count.  An unsplit
+// 61 to 3200 outputs a side, all odd): 0.5% slower than the fastest count on average.  An unsplit
 // one has smaller tiles, so the join's charge holds more than the join.
 static constexpr SplitCost kAct8StagedCost = {1.0, 1.35, 11.0, 2.5e-6};
 
@@ -114,9 +114,9 @@ static constexpr SplitCost kAct8StagedCost = {1.0, 1.35, 11.0, 2.5e-6};
 // or 128 x 128 ones, two, by estimated time.  A round of o workgroups per CU takes its
 // k tiles x k_us[o - 1] plus tile_us; partials cost 2.5 us per million outputs and
 // split (what they cost beside other work; alone less).  Of 275 measured gradients (100
-// to 60000 rows, 64 to 3200 outputs a side, both heights and the split counts timed)
-// the choice is 0.5% slower than the fastest on average; 64-high tiles alone at least
-// 1.6%, 128-high ones 14%.  Examples (us, 64 / 128 high, each with its best split count):
+// to 65536 rows, 64 to 3200 outputs a side, both heights and the split counts timed)
+// the choice is 0.5% slower than the fastest on average; 64-high tiles alone 1.5%,
+// 128-high ones 16%.  Examples (us, 64 / 128 high, each with its best split count):
 // 1000 x 768 x 768 13 / 18, 2100 x 640 x 512 15 / 17, 16640 x 384 x 1536 38 / 38,
 // 12608 x 2304 x 768 83 / 69.
 static void act8_plan(int64_t N, int64_t K, int64_t Mr, int& rows, int& sp, int64_t& k_split) {

@@ -165,8 +165,10 @@ struct BestK {
 };
 
 // Bound by HBM where the logits are many and the alternatives few (4096 x 65536
-// bf16: 95 us without entropy and alternatives, 5.7 TB/s; 109 with both and 4 of them,
-// 128 with 16), by the latency of the best's ordering in a few rows.
+// bf16, calls replayed from a graph: 90 us without entropy and alternatives, 6.0 TB/s;
+// 105 to 115 with both and 4 of them, 129 with 16; 4096 x 65537 float32 with 4 183 us,
+// 5.9 TB/s), by the latency of the best's ordering in a few rows (8 x 131072 with 8
+// 12.2 us, both kernels).
 // One wave's pass over a row: per lane the moments about `ref` (moved only when a
 // logit exceeds it by 8, so nearly never after the first vectors; the sums are
 // float32 and e^8 of them costs no accuracy), the largest logit, and over the wave
@@ -407,7 +409,7 @@ struct LogprobGrad {
 };
 
 // Bound by HBM (one read and one write of every logit: 4096 x 65536 bf16 173 us,
-// 6.2 TB/s).  A wave's part of a row: up to U vectors per lane, all loaded before
+// 6.2 TB/s, x 65537 184, float32 368, 5.8 TB/s; replayed from a graph).  A wave's part of a row: up to U vectors per lane, all loaded before
 // the first store.  With t = (z - m) - ln S and p = e^t the gradient is
 //   p (c0 + c1 t),  c0 = -scale (sum of the upstream cotangents + g_H H),
 //   c1 = -scale g_H,
@@ -621,7 +623,7 @@ extern "C" int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* target
   MPX_REQUIRE(aligned4({targets, stats, entropy, top_idx, g_logp, g_entropy, g_top, d_state}),
               "misaligned operand");
   const LogprobGrad g = {targets, top_idx, stats, entropy, g_logp, g_entropy, g_top, d_state};
-  // tasks of up to 4 vectors per lane, four to a workgroup (2^32 work-items)
+  // tasks of up to 4 vectors per lane, four to a workgroup: up to 2^31 work-items
   const int64_t row_waves = cdiv(V, 4 * 64 * (dt == MPX_F32 ? 4 : 8));
   MPX_REQUIRE(rows <= ((int64_t)1 << 25) / row_waves, "rows * V too large for one call");
   const unsigned blocks = (unsigned)cdiv(rows * row_waves, 4);

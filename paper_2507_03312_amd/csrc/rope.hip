@@ -124,7 +124,10 @@ __device__ __forceinline__ void rope_copies_and_turns(const RopeArgs& a, const t
 // has it (halves): y = x c + partner s, s negative in a section's first half.
 // Values behind the sections count as pairs that are not turned.  The lanes of a
 // head lie in one wave (a.chunks <= 64 runs).  12608 rows of 36 heads of 64 bf16 (116
-// MB) take 25 us, in place 16.5; 29997 of 48 heads of 128 f16 (737 MB) 119 us.
+// MB) take 25 us, in place 16.5; 29997 of 48 heads of 128 f16 (737 MB) 119 us; in
+// float32 45, 28 and 258.  Lanes that do not make up a whole head idle: 8192 rows of 12
+// heads of 256, 264 (33 of 64 lanes) and 320 (40) bf16 21.6, 27.7 and 29.2 us, in place
+// 18.8, 22.1 and 24.3; of 128, 160 (40) and 256 float32 20.3, 27.4 and 38.7.
 template <int DT, int VW, bool INTER, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   typedef typename RopeValue<DT>::type T;

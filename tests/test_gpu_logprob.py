@@ -385,3 +385,20 @@ def test_logits_past_the_cache(fmt, rows, V):
         assert torch.equal(part, dz[lo:lo + n])
     bwd(t, t, 0, rows)
     assert torch.equal(t, dz[:rows])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("V", [300, 5000, 100001])
+def test_spoilt_rows_without_a_target(fmt, V):
+    """NaN or +inf in a row that has no target: logp stays 0, every other float
+    result is NaN (one wave, one workgroup and several per row)."""
+    rows, k = 4, 3
+    rng = np.random.default_rng(V)
+    z = round_to(rng.normal(0, 2, (rows, V)), fmt).astype(np.float64)
+    z[0, 7], z[1, V - 1], z[2, 0] = np.nan, np.inf, np.nan
+    z[2, 5] = np.inf
+    targets = torch.tensor([-1, -5, 2, -1], dtype=torch.int32, device="cuda")
+    f, _ = _check_forward(z, _upload(z, fmt), targets, k, fmt)
+    logp = _np(f[0, :rows])
+    assert logp[0] == logp[1] == logp[3] == 0.0 and np.isnan(logp[2])
+    assert np.isnan(_np(f[1, :3])).all() and np.isnan(_stats(f, rows)[:3]).all()
