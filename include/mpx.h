@@ -298,7 +298,7 @@ int mpx_act8_unpack(const uint8_t* codes, const uint8_t* scales, void* Y, int64_
  *        (Xc, Xs));
  *   dW = half(dY^T X);  db = half(sum_m dY[m,:]).
  * The product is rounded to half before GELU' and again behind it, as in
- * mpx_linear_bwd: the gradient is that call's on the widened values.
+ * mpx_linear_bwd: dX is that call's on the widened values, up to the last place.
  * Shapes, subsets (dX, dW, db may be NULL, not all), d_nonfinite and errors as
  * mpx_linear_bwd; Xc and Xs are needed for dW only, Pc and Ps for dX through
  * GELU only.  dt == MPX_F16 or MPX_BF16; codes and scales at any address.  Whatever
