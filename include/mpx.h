@@ -15,8 +15,13 @@
  * Beside that path, for the same training step: activation checkpoints in 8
  * bits and the linear backward that reads them (mpx_act8_pack,
  * mpx_act8_unpack, mpx_linear_bwd_act8), rotary positions with several axes
- * (mpx_rope_fwd, mpx_rope_bwd), per-token log probabilities with entropy, top
- * alternatives and their gradient (mpx_logprob_fwd, mpx_logprob_bwd).
+ * (mpx_rope_fwd, mpx_rope_bwd), the same with norms of queries and keys for each
+ * head (mpx_qknorm_rope_fwd, mpx_qknorm_rope_bwd), gated feed-forward projections
+ * (mpx_gated_fwd, mpx_linear_bwd_gated), dropout whose mask is never stored
+ * (mpx_dropout_fwd, mpx_dropout_bwd, mpx_rng_advance), per-token log probabilities with
+ * entropy, top alternatives and their gradient (mpx_logprob_fwd, mpx_logprob_bwd), and
+ * cross entropy over a large vocabulary without its logits (mpx_linear_ce_fwd,
+ * mpx_linear_ce_bwd).
  *
  * Conventions shared by every call:
  *  - Pointers named d_* and every tensor pointer are DEVICE pointers; the
@@ -33,15 +38,17 @@
  *  - Full precision (MPX's use_mixed_precision switched off, the baseline of
  *    §4): mpx_linear_fwd/bwd, mpx_gemm_batched, mpx_layernorm_fwd/bwd,
  *    mpx_softmax_fwd/bwd, mpx_cross_entropy, mpx_mse, mpx_patchify_cast,
- *    mpx_embed_assemble(_bwd), mpx_rope_fwd/bwd and mpx_logprob_fwd/bwd also
+ *    mpx_embed_assemble(_bwd), mpx_rope_fwd/bwd, mpx_qknorm_rope_fwd/bwd,
+ *    mpx_gated_fwd, mpx_linear_bwd_gated, mpx_dropout_fwd/bwd and mpx_logprob_fwd/bwd also
  *    accept dt == MPX_F32: every tensor named "half" in their description is
  *    then float32 and half() is the identity (d_nonfinite must be NULL).
  *  - Return value: MPX_OK (0) or a negative code; mpx_last_error() gives a
  *    message (per host thread).  Invalid arguments are detected before
  *    anything is launched.  Non-finite DATA is never an error: it is reported
  *    through the non-finite count (MPX §2.1: overflow makes the step skip).
- *  - The calls that write parameter gradients (mpx_linear_bwd's and
- *    mpx_linear_bwd_act8's dW and db,
+ *  - The calls that write parameter gradients (mpx_linear_bwd's,
+ *    mpx_linear_bwd_act8's, mpx_linear_bwd_gated's and mpx_linear_ce_bwd's dW and db,
+ *    mpx_qknorm_rope_bwd's dwq and dwk,
  *    mpx_layernorm_bwd's and mpx_classifier_head's dgamma and dbeta,
  *    mpx_embed_assemble_bwd's dcls and dpos) take a nullable int32 device
  *    counter d_nonfinite: when set, the number of those half results whose
@@ -165,7 +172,7 @@ int mpx_adamw_masked(mpx_tlist p32, mpx_tlist m32, mpx_tlist v32, mpx_tlist grad
                      mpx_tlist half_copy, mpx_dtype half, void* stream);
 
 /* Activation codes. */
-enum { MPX_ACT_NONE = 0, MPX_ACT_GELU_TANH = 1 };
+enum { MPX_ACT_NONE = 0, MPX_ACT_GELU_TANH = 1, MPX_ACT_SILU = 2 /* x / (1 + e^-x); gated calls only */ };
 
 /* Half-precision linear layer forward (MPX §2: forward pass in half
  * precision; products accumulated in float32).  X [M,K], W [N,K], b [N]
@@ -230,6 +237,38 @@ size_t mpx_linear_bwd_workspace(int64_t M, int64_t N, int64_t K);
 int mpx_linear_bwd_noalloc(const void* X, const void* W, const void* dY, const void* Xpre,
                            int32_t x_act, void* dX, void* dW, void* db, int64_t M, int64_t N,
                            int64_t K, mpx_dtype dt, int32_t* d_nonfinite, void* stream);
+
+/* ---- Gated feed-forward block ----
+ *
+ * Both input projections of a gated feed-forward block, the gate's activation
+ * and the product in one kernel.  W [2N, K] holds the gate's rows and, behind
+ * them, the other projection's; b [2N] (nullable) likewise.  With g, u the
+ * float32 sums of X W^T + b for W's halves:
+ *   H [M, N]    = half(act(g) u)       (one rounding)
+ *   Pre [M, 2N] = [half(g) | half(u)]  (nullable: what the backward pass needs)
+ * act: MPX_ACT_SILU (x / (1 + e^-x)) or MPX_ACT_GELU_TANH.  All dense, row-major,
+ * pointers aligned to their element.  1 <= M < 2^31, 1 <= N, K <= 2^24.  The down
+ * projection is mpx_linear_fwd on H (with the block's residual).  Up to 32 rows
+ * (single tokens of some sequences) take a kernel that reads W once.  dt ==
+ * MPX_F32: full precision; Pre is then required (the sums are left there). */
+int mpx_gated_fwd(const void* X, const void* W, const void* b, void* H, void* Pre, int64_t M, int64_t N,
+                  int64_t K, mpx_dtype dt, int32_t act, void* stream);
+
+/* mpx_linear_bwd of the layer behind a gated pair (the down projection Y [M, N] =
+ * X W^T + b, W [N, K], whose input X [M, K] is the H above), with the cotangent
+ * of the pair's pre-activations in dX's place: with dH = dY W in float32 and g, u
+ * from Pre [M, 2K],
+ *   dPre [M, 2K] = [half(dH u act'(g)) | half(dH act(g))]   (needs W, Pre)
+ *   dW [N, K] = half(dY^T X), db [N] = half(sum_m dY[m,:]) as mpx_linear_bwd.
+ * dPre is the dY of the pair's own mpx_linear_bwd (with W [2K, K'], whatever its
+ * input).  Any subset may be requested (the others NULL).  dPre must not overlap
+ * Pre.  workspace: mpx_linear_bwd_gated_workspace(M, N, K) bytes when dW or db is
+ * requested.  d_nonfinite counts non-finite dW and db elements.  Sizes, types and
+ * alignment as mpx_gated_fwd (d_nonfinite must be NULL with MPX_F32). */
+int mpx_linear_bwd_gated(const void* X, const void* W, const void* dY, const void* Pre, int32_t act,
+                         void* dPre, void* dW, void* db, int64_t M, int64_t N, int64_t K, mpx_dtype dt,
+                         void* workspace, size_t ws_bytes, int32_t* d_nonfinite, void* stream);
+size_t mpx_linear_bwd_gated_workspace(int64_t M, int64_t N, int64_t K);
 
 /* Batched half GEMM with float32 accumulation (attention QK^T, PV and their
  * backward).  For i0 < nb0, i1 < nb1, with offsets o_X = i0*sX0 + i1*sX1
@@ -356,6 +395,39 @@ int mpx_rope_fwd(const void* X, int64_t ldx, void* Y, int64_t ldy, const float* 
 int mpx_rope_bwd(const void* dY, int64_t ldy, void* dX, int64_t ldx, const float* pos,
                  int64_t pos_rows, int64_t rows, int64_t heads_rot, int64_t heads_copy, int64_t hd,
                  const mpx_rope_plan* plan, mpx_dtype dt, void* stream);
+
+/* ---- Norms of queries and keys with the rotary positions ----
+ *
+ * For each of the first heads_q heads of every row of X (a query) and the heads_k
+ * heads behind them (keys): the head divided by the root of its mean square, times a
+ * gain for each of its values, turned by the row's position, in one pass:
+ *   r = 1 / sqrt(mean(x^2) + eps);  Y = half(turn(x r w)),  w = wq or wk [hd].
+ * The heads_copy heads behind those are copied (the values V).  wq, wk: nullable, a
+ * gain of 1; of type dt.  eps >= 0 (a head of nothing but zeros is NaN with eps 0).
+ * heads_q >= 1, heads_k >= 0 (0: one kind of heads only); plan, pos, strides, in
+ * place calls (Y == X; the backward pass then needs a copy of X) and sizes as
+ * mpx_rope_fwd; rows < 2^24.  Sums and the turn in float32 (values from 2^60 on pass
+ * its range once squared), one rounding.  A NaN or an infinity reaches its own head
+ * and no other. */
+int mpx_qknorm_rope_fwd(const void* X, int64_t ldx, void* Y, int64_t ldy, const void* wq, const void* wk,
+                        double eps, const float* pos, int64_t pos_rows, int64_t rows, int64_t heads_q,
+                        int64_t heads_k, int64_t heads_copy, int64_t hd, const mpx_rope_plan* plan,
+                        mpx_dtype dt, void* stream);
+
+/* Backward, from the forward's X and dY (row stride ldy): with dn = turn^-1(dY),
+ *   dX = half(r (w dn - x r^2 mean(w dn x)));  dwq, dwk [hd] = half(sum of dn x r
+ *        over rows and the heads of that kind)
+ * (each of dwq, dwk nullable; float32 sums in a fixed order).  dX has row stride ldo;
+ * dX == dY with ldo == ldy works in place, any other overlap is not allowed.  X's
+ * copied heads are not read (ldx may end before them), dY's are copied.  workspace:
+ * mpx_qknorm_rope_bwd_workspace(rows, hd) bytes, which never falls as rows grow.
+ * d_nonfinite (nullable) counts non-finite dwq and dwk elements. */
+int mpx_qknorm_rope_bwd(const void* X, int64_t ldx, const void* dY, int64_t ldy, void* dX, int64_t ldo,
+                        const void* wq, const void* wk, double eps, const float* pos, int64_t pos_rows,
+                        int64_t rows, int64_t heads_q, int64_t heads_k, int64_t heads_copy, int64_t hd,
+                        const mpx_rope_plan* plan, void* dwq, void* dwk, mpx_dtype dt, void* workspace,
+                        size_t ws_bytes, int32_t* d_nonfinite, void* stream);
+size_t mpx_qknorm_rope_bwd_workspace(int64_t rows, int64_t hd);
 
 /* Fused multi-head self-attention core (MPX §2.1 half products with float32
  * accumulation; §3.2 softmax and its backward in full precision), one pass
@@ -499,6 +571,44 @@ int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t 
                     const mpx_scale_state* d_state, void* dZ, int64_t ldo, mpx_dtype dt,
                     void* stream);
 
+/* ---- Cross entropy of a linear layer, without its logits ----
+ *
+ * For the logits z = X W^T + b (X [M, K], W [V, K], b [V] nullable; never stored):
+ *   stats[r] = (m, ln S),  m = max_j z_j,  S = sum_j e^(z_j - m)   (float32 [M, 2])
+ *   loss[r]  = m + ln S - z[targets[r]]                            (float32 [M])
+ *   *d_mean  = mean of loss over the rows that have a target (0 if none has)
+ * from float32 sums that are not rounded to half.  loss (needs targets), stats and
+ * d_mean (needs loss) are nullable, not both of the first two.  targets (int32 [M]):
+ * negative, the row has no target (loss 0, no gradient); V or more gives NaN.  A bias
+ * of -inf masks its column (probability 0, no gradient); a row of nothing but masked
+ * ones has stats (-inf, 0) and loss inf.  A NaN or +inf logit makes its row's ln S and
+ * loss NaN.  1 <= M <= 2^20, V <= 2^24, K <= 2^16; dt MPX_F16 or MPX_BF16; X and W
+ * dense, all aligned to their element (stats 8 bytes).  Operands 16-byte aligned with K
+ * a multiple of 64 go the fastest way.  workspace:
+ * mpx_linear_ce_fwd_workspace(M, V, K) bytes, 16-byte aligned, not shared by calls
+ * that overlap; results do not depend on what else runs (no atomics). */
+int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, const int32_t* targets, int64_t M,
+                      int64_t V, int64_t K, float* loss, float* stats, float* d_mean, mpx_dtype dt,
+                      void* workspace, size_t ws_bytes, void* stream);
+size_t mpx_linear_ce_fwd_workspace(int64_t M, int64_t V, int64_t K);
+
+/* Its gradient, from the forward's stats, for the cotangents g_loss [M] of loss
+ * (float32; NULL: 1 / the number of rows with a target, the gradient of d_mean):
+ *   dz = scale g (p - [j == target]),  p_j = e^((z_j - m) - ln S),  scale = d_state->scale
+ *   dX [M, K] = half(dz W);  dW [V, K] = half(dz^T X);  db [V] = half(sum_r dz)
+ * (d_state NULL: 1; any subset, the others NULL).  The logits are computed again, in
+ * pieces of the vocabulary: a piece's dz is held in the half type in the workspace
+ * (float16: scaled by a power of two that keeps small probabilities, and back), dX's
+ * sums over the pieces in float32.  A row whose stats are NaN, or whose target is V
+ * or more, makes its dX and all of dW NaN.  d_nonfinite (nullable) counts non-finite
+ * dW and db elements.  workspace: mpx_linear_ce_bwd_workspace(M, V, K) bytes, 16-byte
+ * aligned.  Sizes and types as the forward's; outputs overlap nothing. */
+int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, const int32_t* targets, int64_t M,
+                      int64_t V, int64_t K, const float* stats, const float* g_loss,
+                      const mpx_scale_state* d_state, void* dX, void* dW, void* db, mpx_dtype dt,
+                      void* workspace, size_t ws_bytes, int32_t* d_nonfinite, void* stream);
+size_t mpx_linear_ce_bwd_workspace(int64_t M, int64_t V, int64_t K);
+
 /* Workspace (bytes) of mpx_classifier_head for B rows of width d: the row
  * losses and one pair of float32 gamma / beta partial rows per 4 rows,
  * overwritten by every call. */
@@ -542,6 +652,31 @@ int mpx_classifier_head(const void* X, int64_t ldx, const void* gamma, const voi
 int mpx_mse(const void* Y, const void* T, int64_t n, const mpx_scale_state* d_state,
             float* d_loss, void* dY, mpx_dtype dt, void* workspace, size_t ws_bytes,
             void* stream);
+
+/* ---- Dropout, its mask made again instead of stored ----
+ *
+ * State of the generator, resident in device memory: a step's masks follow from
+ * (seed, step) alone.  mpx_rng_advance adds 1 to step, in stream order (also inside a
+ * captured graph, so every replay draws anew). */
+typedef struct {
+  uint64_t seed;
+  uint64_t step;
+} mpx_rng_state;
+int mpx_rng_advance(mpx_rng_state* d_rng, void* stream);
+
+/* Y = half(R + keep X / (1 - q)) over n values (R nullable: the residual stream; one
+ * rounding): value i is kept when its draw is at least T = round(65536 p), q = T / 65536.
+ * Its draw: 16 bits of Philox4x32-10 (Salmon et al., SC 2011) with key (seed's lower,
+ * upper word) and counter (i / 8, site, step's lower word, upper word): word (i % 8) / 2 of
+ * the block's four, the lower half for even i.  `site` tells apart the calls of a step.
+ * A dropped value adds 0, whatever X holds there.  1 <= n <= 2^34, 0 <= p < 1 with T
+ * < 65536; dense; pointers aligned to their element; Y may be X or R itself. */
+int mpx_dropout_fwd(const void* X, const void* R, void* Y, int64_t n, double p, const mpx_rng_state* d_rng,
+                    uint32_t site, mpx_dtype dt, void* stream);
+/* dX = half(keep dY / (1 - q)) with the forward's p, state and site (R's gradient is dY).
+ * dX may be dY. */
+int mpx_dropout_bwd(const void* dY, void* dX, int64_t n, double p, const mpx_rng_state* d_rng, uint32_t site,
+                    mpx_dtype dt, void* stream);
 
 /* Cast float32 NHWC images [B,H,W,C] to half patch vectors [B*G, p*p*C]
  * (MPX §3.4: inputs cast to half).  Patches row-major over the grid; a

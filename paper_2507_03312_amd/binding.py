@@ -16,7 +16,7 @@ import os
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmpx.so")
 
 MPX_F32, MPX_F16, MPX_BF16 = 0, 1, 2
-MPX_ACT_NONE, MPX_ACT_GELU_TANH = 0, 1
+MPX_ACT_NONE, MPX_ACT_GELU_TANH, MPX_ACT_SILU = 0, 1, 2
 MPX_ACT8_GROUP = 32        # rows of a column that share a checkpoint's scale
 MPX_ROPE_MAX_AXES = 4
 MPX_LOGPROB_MAX_K = 16
@@ -94,6 +94,21 @@ _SIGS = {
     "mpx_linear_bwd_act8_workspace": (SZ, [I64, I64, I64]),
     "mpx_rope_fwd": (C.c_int, [P, I64, P, I64, P, I64, I64, I64, I64, I64, C.POINTER(RopePlan), I32, P]),
     "mpx_rope_bwd": (C.c_int, [P, I64, P, I64, P, I64, I64, I64, I64, I64, C.POINTER(RopePlan), I32, P]),
+    "mpx_qknorm_rope_fwd": (C.c_int, [P, I64, P, I64, P, P, C.c_double, P, I64, I64, I64, I64, I64, I64,
+                                      C.POINTER(RopePlan), I32, P]),
+    "mpx_qknorm_rope_bwd": (C.c_int, [P, I64, P, I64, P, I64, P, P, C.c_double, P, I64, I64, I64, I64, I64,
+                                      I64, C.POINTER(RopePlan), P, P, I32, P, SZ, P, P]),
+    "mpx_qknorm_rope_bwd_workspace": (SZ, [I64, I64]),
+    "mpx_gated_fwd": (C.c_int, [P, P, P, P, P, I64, I64, I64, I32, I32, P]),
+    "mpx_linear_bwd_gated": (C.c_int, [P, P, P, P, I32, P, P, P, I64, I64, I64, I32, P, SZ, P, P]),
+    "mpx_linear_bwd_gated_workspace": (SZ, [I64, I64, I64]),
+    "mpx_linear_ce_fwd": (C.c_int, [P, P, P, P, I64, I64, I64, P, P, P, I32, P, SZ, P]),
+    "mpx_linear_ce_fwd_workspace": (SZ, [I64, I64, I64]),
+    "mpx_linear_ce_bwd": (C.c_int, [P, P, P, P, I64, I64, I64, P, P, P, P, P, P, I32, P, SZ, P, P]),
+    "mpx_linear_ce_bwd_workspace": (SZ, [I64, I64, I64]),
+    "mpx_rng_advance": (C.c_int, [P, P]),
+    "mpx_dropout_fwd": (C.c_int, [P, P, P, I64, C.c_double, P, C.c_uint32, I32, P]),
+    "mpx_dropout_bwd": (C.c_int, [P, P, I64, C.c_double, P, C.c_uint32, I32, P]),
     "mpx_attention_fwd": (C.c_int, [P, P, P, I64, I64, I64, I64, I32, P]),
     "mpx_attention_bwd": (C.c_int, [P, P, P, P, I64, I64, I64, I64, I32, P, SZ, P]),
     "mpx_attention_bwd_workspace": (SZ, [I64, I64, I64, I64]),
@@ -212,6 +227,13 @@ mpx_act8_unpack = _call("mpx_act8_unpack")
 mpx_linear_bwd_act8 = _call("mpx_linear_bwd_act8")
 mpx_rope_fwd = _call("mpx_rope_fwd")
 mpx_rope_bwd = _call("mpx_rope_bwd")
+mpx_qknorm_rope_fwd = _call("mpx_qknorm_rope_fwd")
+mpx_qknorm_rope_bwd = _call("mpx_qknorm_rope_bwd")
+mpx_gated_fwd = _call("mpx_gated_fwd")
+mpx_linear_bwd_gated = _call("mpx_linear_bwd_gated")
+mpx_linear_ce_fwd = _call("mpx_linear_ce_fwd")
+mpx_linear_ce_bwd = _call("mpx_linear_ce_bwd")
+mpx_rng_advance = _call("mpx_rng_advance")   # state: int64 device tensor [seed, step]
 mpx_attention_fwd = _call("mpx_attention_fwd")
 mpx_attention_bwd = _call("mpx_attention_bwd")
 mpx_layernorm_fwd = _call("mpx_layernorm_fwd")
@@ -231,12 +253,44 @@ mpx_gather_rows = _call("mpx_gather_rows")
 mpx_zero = _call("mpx_zero")
 
 
+def _site(site: int) -> int:
+    if not 0 <= site < 2 ** 32:  # ctypes would keep its lower 32 bits
+        raise ValueError("site must fit 32 bits")
+    return site
+
+
+def mpx_dropout_fwd(X, R, Y, n, p, d_rng, site, dt, stream):
+    """mpx_dropout_fwd (include/mpx.h); raises MPXError on failure."""
+    _check(lib.mpx_dropout_fwd(X, R, Y, n, p, d_rng, _site(site), dt, stream), "mpx_dropout_fwd")
+
+
+def mpx_dropout_bwd(dY, dX, n, p, d_rng, site, dt, stream):
+    """mpx_dropout_bwd (include/mpx.h); raises MPXError on failure."""
+    _check(lib.mpx_dropout_bwd(dY, dX, n, p, d_rng, _site(site), dt, stream), "mpx_dropout_bwd")
+
+
 def mpx_linear_bwd_workspace(M: int, N: int, K: int) -> int:
     return int(lib.mpx_linear_bwd_workspace(M, N, K))
 
 
 def mpx_linear_bwd_act8_workspace(M: int, N: int, K: int) -> int:
     return int(lib.mpx_linear_bwd_act8_workspace(M, N, K))
+
+
+def mpx_linear_bwd_gated_workspace(M: int, N: int, K: int) -> int:
+    return int(lib.mpx_linear_bwd_gated_workspace(M, N, K))
+
+
+def mpx_linear_ce_fwd_workspace(M: int, V: int, K: int) -> int:
+    return int(lib.mpx_linear_ce_fwd_workspace(M, V, K))
+
+
+def mpx_linear_ce_bwd_workspace(M: int, V: int, K: int) -> int:
+    return int(lib.mpx_linear_ce_bwd_workspace(M, V, K))
+
+
+def mpx_qknorm_rope_bwd_workspace(rows: int, hd: int) -> int:
+    return int(lib.mpx_qknorm_rope_bwd_workspace(rows, hd))
 
 
 def mpx_logprob_workspace(rows: int, V: int, k: int) -> int:

@@ -431,6 +431,16 @@ struct DmaOperand {
       }
     }
   }
+  // an mn-major operand whose matrix has only `rows` (>= 1) more k rows: those behind
+  // read the last one again
+  __device__ __forceinline__ DmaOperand until(int rows, int64_t ld, int wave, int lane) const {
+    static_assert(!KMAJ, "k rows");
+    DmaOperand o = *this;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      o.off[q] -= (uint32_t)(max(0, (64 * (wave + NWAVES * q) + lane) / (ROWS / 8) - (rows - 1)) * ld * 2);
+    return o;
+  }
   // copy the tile whose first element is at base into LDS at lds (both
   // wave-uniform; made explicitly scalar for the copy instruction)
   __device__ __forceinline__ void issue(const uint16_t* base, uint32_t lds, int wave) const {
@@ -672,6 +682,48 @@ struct FragReader {
   }
 };
 
+// Operand B of a gated product: two k-major matrices of equal shape, `apart` elements
+// from one another (a gate's rows and those of the projection it multiplies).  A tile
+// of ROWS rows holds ROWS / 2 of each, the first's ahead of the second's, so a wave's
+// fragment 0 is 32 columns of the one and fragment 1 the same columns of the other.
+template <int ROWS, int NWAVES, int STG>
+struct PairOperand {
+  std::conditional_t<STG != 0, StagedOperand<ROWS / 2, true, NWAVES, STG == 2>, DmaOperand<ROWS / 2, true, NWAVES>>
+      x[STG != 0 ? 2 : 1];  // direct copies of both have the same lane offsets
+  int64_t step;
+  template <class Rows>
+  __device__ __forceinline__ void init(int64_t ld, Rows rows, int wave, int lane) {
+    x[0].init(ld, rows, wave, lane);
+    if constexpr (STG != 0) x[1].init(ld, rows, wave, lane);
+    else step = x[0].step;
+  }
+  __device__ __forceinline__ void issue(const uint16_t* base, int64_t apart, uint32_t lds, int wave) const {
+    x[0].issue(base, lds, wave);
+    x[0].issue(base + apart, lds + ROWS / 2 * 128, wave);
+  }
+  template <int P>
+  __device__ __forceinline__ void load(const uint16_t* tile, int64_t apart, int kr, bool past) {
+    x[0].template load<P>(tile, kr, past);
+    x[1].template load<P>(tile + apart, kr, past);
+  }
+  template <int P>
+  __device__ __forceinline__ void store(uint8_t* lds, int wave, int lane) {
+    x[0].template store<P>(lds, wave, lane);
+    x[1].template store<P>(lds + ROWS / 2 * 128, wave, lane);
+  }
+};
+
+// Its fragments, for a wave whose columns start at w0 of either matrix's tile.
+template <int ROWS>
+struct PairFragReader {
+  FragReader<ROWS, true, 1> x;
+  __device__ __forceinline__ void init(int w0, int lane) { x.init(w0, lane); }
+  template <int I, int KK>
+  __device__ __forceinline__ uint4 read(uint32_t lds) const {
+    return x.template read<0, KK>(lds + I * (ROWS / 2 * 128));
+  }
+};
+
 // Sum of the 8 half values of an MFMA operand fragment, in a fixed pairwise order.
 template <int DT>
 __device__ __forceinline__ float frag_sum8(const uint4& f) {
@@ -720,11 +772,39 @@ __device__ __forceinline__ float frag_sum8(const uint4& f) {
 // so a load has two k tiles to land.  (One-value loads served these operands
 // before: 8415 x 768 x 588 in bf16 forward / dX / dW took 89 / 145 / 157 us.)
 // B8: operand B is an 8-bit checkpoint (register-staged kernels only).
+//
+// Args: GemmArgs, or a type derived from it with an end of its own: its epilogue()
+// gets the accumulators in place of the epilogues above, its lds_bytes() is the LDS
+// that takes, and with kPair operand B is a pair of matrices (PairOperand, g.pair
+// elements apart; N, n0 and nw count columns of one).  With kRagged the reduction of a
+// product with an mn-major B may end inside a k tile: A has zeros behind it, up to the
+// tile's end, and B's last k row is read again there.  The sums of DBS go to dbp, also
+// without splits.
+template <class Args, int BM, int BN, int WM, int WN>
+constexpr int own_epilogue_bytes() {
+  if constexpr (std::is_same_v<Args, GemmArgs>) return 0;
+  else return Args::lds_bytes(BM, BN, WM, WN);
+}
+template <class Args>
+constexpr bool ragged_reduction() {
+  if constexpr (std::is_same_v<Args, GemmArgs>) return false;
+  else return Args::kRagged;
+}
+template <class Args>
+constexpr bool pair_operand() {
+  if constexpr (std::is_same_v<Args, GemmArgs>) return false;
+  else return Args::kPair;
+}
+
 template <int DT, int BM, int BN, int WM, int WN, int OCC, bool AK, bool BKM, int E, bool DBS = false,
-          int STG = 0, bool B8 = false>
+          int STG = 0, bool B8 = false, class Args = GemmArgs>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64)
 __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
-void gemm_tile_kernel(GemmArgs g) {
+void gemm_tile_kernel(Args g) {
+  constexpr bool kOwn = !std::is_same_v<Args, GemmArgs>, kPair = pair_operand<Args>();
+  constexpr bool kRagged = ragged_reduction<Args>() && STG == 0;
+  static_assert(!kOwn || (E == 0 && !B8), "an epilogue of its own has no other");
+  static_assert(!kPair || (BKM && WN == 64), "a pair's fragments: 32 columns of each");
   constexpr int NWAVES = (BM / WM) * (BN / WN);
   constexpr int TM = WM / 32, TN = WN / 32;
   constexpr int A_BYTES = BM * 64 * 2, B_BYTES = BN * 64 * 2;
@@ -735,7 +815,7 @@ void gemm_tile_kernel(GemmArgs g) {
   constexpr int kReads = TM * (AK ? 1 : 2) + TN * (BKM ? 1 : 2);
   // the epilogue works on 64 columns of a wave at a time
   constexpr int EC = WN < 64 ? WN : 64;
-  constexpr int EPI = NWAVES * WM * (EC + 4) * 2;
+  constexpr int EPI = kOwn ? own_epilogue_bytes<Args, BM, BN, WM, WN>() : NWAVES * WM * (EC + 4) * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE > EPI ? 2 * STAGE : EPI];
   const uint32_t lds0 = lds_u32(smem);
 
@@ -743,10 +823,10 @@ void gemm_tile_kernel(GemmArgs g) {
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm0 = (wave / (BN / WN)) * WM;
-  const int wn0 = (wave % (BN / WN)) * WN;
+  const int wn0 = (wave % (BN / WN)) * (kPair ? 32 : WN);
 
   int64_t m0, n0;
-  tile_origin<BM, BN>(g.M, g.N, m0, n0);
+  tile_origin<BM, kPair ? BN / 2 : BN>(g.M, g.N, m0, n0);
   int64_t z = blockIdx.y;
   int split = 0;
   int64_t offA = 0, offB = 0, offC = 0;
@@ -760,15 +840,16 @@ void gemm_tile_kernel(GemmArgs g) {
   }
   const int64_t kbeg = (int64_t)split * g.k_split;
   const int64_t kend = min(g.K, kbeg + g.k_split);
-  const int nk = (int)((kend - kbeg + (STG ? 63 : 0)) / 64);
+  const int nk = (int)((kend - kbeg + (STG || kRagged ? 63 : 0)) / 64);
 
   const uint16_t* Ab = g.A + offA + (AK ? m0 * g.lda + kbeg : kbeg * g.lda + m0);
   const uint16_t* Bb = g.B + offB + (BKM ? n0 * g.ldb + kbeg : kbeg * g.ldb + n0);
   std::conditional_t<STG != 0, StagedOperand<BM, AK, NWAVES, STG == 2>, DmaOperand<BM, AK, NWAVES>> da;
   static_assert(!B8 || (STG != 0 && !BKM), "an 8-bit operand is staged, mn-major");
-  std::conditional_t<B8, StagedAct8<DT, BN, NWAVES, STG == 2>,
-                     std::conditional_t<STG != 0, StagedOperand<BN, BKM, NWAVES, STG == 2>,
-                                        DmaOperand<BN, BKM, NWAVES>>> db;
+  std::conditional_t<kPair, PairOperand<BN, NWAVES, STG>,
+                     std::conditional_t<B8, StagedAct8<DT, BN, NWAVES, STG == 2>,
+                                        std::conditional_t<STG != 0, StagedOperand<BN, BKM, NWAVES, STG == 2>,
+                                                           DmaOperand<BN, BKM, NWAVES>>>> db;
   if constexpr (STG != 0) {
     da.init(g.lda, g.M - m0, wave, lane);
     db.init(g.ldb, g.N - n0, wave, lane);
@@ -803,12 +884,21 @@ void gemm_tile_kernel(GemmArgs g) {
       if constexpr (B8)
         db.template load<par>(g.b8 + ((kbeg + 64 * (int64_t)kt) * g.ldb + n0),
                               g.b8_scale + ((kbeg + 64 * (int64_t)kt) / MPX_ACT8_GROUP * g.ldb + n0), krem, past);
+      else if constexpr (kPair) db.template load<par>(Bb + (int64_t)kt * 64, g.pair, krem, past);
       else db.template load<par>(Bb + (int64_t)kt * (BKM ? 64 : 64 * g.ldb), krem, past);
     } else {
       const uint32_t st = lds0 + (uint32_t)((kt & 1) * STAGE);
       da.issue(reinterpret_cast<const uint16_t*>(reinterpret_cast<const uint8_t*>(Ab) + kt * da.step), st, wave);
-      db.issue(reinterpret_cast<const uint16_t*>(reinterpret_cast<const uint8_t*>(Bb) + kt * db.step),
-               st + A_BYTES, wave);
+      const uint16_t* b = reinterpret_cast<const uint16_t*>(reinterpret_cast<const uint8_t*>(Bb) + kt * db.step);
+      if constexpr (kPair) {
+        db.issue(b, g.pair, st + A_BYTES, wave);
+      } else if constexpr (kRagged) {
+        const int krem = (int)(kend - kbeg - 64 * (int64_t)kt);
+        if (krem >= 64) db.issue(b, st + A_BYTES, wave);  // uniform
+        else db.until(krem, g.ldb, wave, lane).issue(b, st + A_BYTES, wave);
+      } else {
+        db.issue(b, st + A_BYTES, wave);
+      }
     }
   };
   auto put = [&](auto par) {  // STG: a loaded k tile (register set par) into stage par
@@ -834,7 +924,7 @@ void gemm_tile_kernel(GemmArgs g) {
   }
 
   FragReader<BM, AK, TM> fa;
-  FragReader<BN, BKM, TN> fb;
+  std::conditional_t<kPair, PairFragReader<BN>, FragReader<BN, BKM, TN>> fb;
   fa.init(wm0, lane);
   fb.init(wn0, lane);
   f32x16 acc[TM][TN];
@@ -846,9 +936,10 @@ void gemm_tile_kernel(GemmArgs g) {
   });
   // bias-gradient sums: tile columns sharing the A rows, this one's index,
   // and the next k tile this wave adds up (uniform over the wave)
-  const int db_cols = g.splits > 1 ? (int)((g.N + BN - 1) / BN) : 1;
-  const int db_col = g.splits > 1 ? (int)(n0 / BN) : 0;
-  const bool dbw = DBS && wn0 == 0 && (g.splits > 1 || n0 == 0);
+  const bool db_parts = kOwn || g.splits > 1;
+  const int db_cols = db_parts ? (int)((g.N + BN - 1) / BN) : 1;
+  const int db_col = db_parts ? (int)(n0 / BN) : 0;
+  const bool dbw = DBS && wn0 == 0 && (db_parts || n0 == 0);
   int db_next = db_col;
   float dbs[TM];
 #pragma unroll
@@ -932,7 +1023,7 @@ void gemm_tile_kernel(GemmArgs g) {
         const int64_t row = mw + 32 * i + lane;
         if (lane < 32 && row < g.M) {
           const float v = dbs[i] + other;
-          if (g.splits > 1) {
+          if (db_parts) {
             g.dbp[row * ((int64_t)g.splits * db_cols) + (int64_t)split * db_cols + db_col] = v;
           } else {
             const uint16_t h = f2h<DT>(v);
@@ -945,6 +1036,10 @@ void gemm_tile_kernel(GemmArgs g) {
     }
   }
   // the accumulators hold C^T blocks (the MFMA operands are swapped above)
+  if constexpr (kOwn) {
+    g.template epilogue<DT, BM, BN, WM, WN>(acc, m0, n0, mw, nw, lane, wave, split, smem);
+    return;
+  }
   if (g.splits > 1) {
     gemm_partials<TM, TN>(g, acc, mw, nw, lane, split);
     return;

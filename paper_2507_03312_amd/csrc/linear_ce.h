@@ -1,0 +1,278 @@
+// Cross entropy straight from the last hidden states, on the tile kernels of
+// gemm_kernels.h: the logits z = X W^T + b exist only as a tile's accumulators.
+//   forward   per row m = max z, S = sum e^(z - m): a tile leaves its own (m, S) per row,
+//             and the target's logit; a second kernel joins them.
+//   backward  in pieces of the vocabulary: z again, dz = f (p - [target]) to a workspace of
+//             one piece in the half type, dX += dz W (float32), dW = dz^T X.
+// f = c scale g of the row.  c is a power of two, taken out of the results again: it
+// brings float16's dz into the middle of its range (a probability of 2^-28 still has
+// all its bits), and is 1 for bf16.
+// Internal; not part of the ABI.
+#pragma once
+
+#include "gemm_rows.h"
+
+namespace mpx {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// The sum of the other half wave's lane, or its maximum.
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// Forward.  A = X, B = W; lane l of a 32 x 32 block has row l % 32 and 16 of its 32
+// columns, so a row's maximum and sum take one exchange beside the lane's own values.
+struct CeFwdArgs : GemmArgs {
+  static constexpr bool kPair = false, kRagged = false;
+  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm * (bn / wn) * 8; }
+  float2* part;  // [tile column][M]
+  float* zt;     // [M]: the target's logit
+  const int32_t* targets;
+  template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
+  __device__ __forceinline__ void epilogue(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int64_t mw, int64_t nw,
+                                           int lane, int wave, int, uint8_t* smem) const {
+    __syncthreads();  // every wave is done reading the stage buffers
+    float2* rows = reinterpret_cast<float2*>(smem);  // [wave column][BM]
+    const int hi = lane >> 5, wc = wave % (BN / WN), wr = wave / (BN / WN);
+    const int nv = (int)min<int64_t>(WN, N - nw);  // may be <= 0
+    if (bias) {
+      static_for<TN>([&](auto j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int col = 32 * j + 8 * (e / 4) + 4 * hi + e % 4;
+          const float b = nv > 0 ? h2f<DT>(bias[nw + min(col, nv - 1)]) : 0.0f;
+          static_for<TM>([&](auto i) { acc[i][j][e] += b; });
+        }
+      });
+    }
+    if (nv < WN) {  // uniform: columns behind the vocabulary have probability 0
+      static_for<TN>([&](auto j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const bool in = 32 * j + 8 * (e / 4) + 4 * hi + e % 4 < nv;
+          static_for<TM>([&](auto i) { acc[i][j][e] = in ? acc[i][j][e] : -__builtin_inff(); });
+        }
+      });
+    }
+    static_for<TM>([&](auto i) {
+      const int64_t row = mw + 32 * i + (lane & 31);
+      if (targets) {
+        const int64_t t = row < M ? (int64_t)targets[row] - nw : -1;
+        if (__ballot(t >= 0 && t < nv)) {  // few tiles hold a target
+          static_for<TN>([&](auto j) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (t == 32 * j + 8 * (e / 4) + 4 * hi + e % 4 && t < nv) zt[row] = acc[i][j][e];
+          });
+        }
+      }
+      float m = acc[i][0][0];
+      static_for<TN>([&](auto j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
+      });
+      m = fmaxf(m, other_half(m));
+      const float at = m == -__builtin_inff() ? 0.0f : m * kLog2e;  // nothing but masked ones: S = 0
+      float s = 0.0f;
+      static_for<TN>([&](auto j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, -at));
+      });
+      s += other_half(s);
+      if (hi == 0) rows[wc * BM + wr * WM + 32 * i + lane] = make_float2(m, s);
+    });
+    __syncthreads();
+    float2* out = part + n0 / BN * M + m0;
+    for (int r = threadIdx.x; r < BM && m0 + r < M; r += BM / WM * (BN / WN) * 64) {
+      float2 a = rows[r];
+#pragma unroll
+      for (int w = 1; w < BN / WN; ++w) {
+        const float2 b = rows[w * BM + r];
+        const float m = fmaxf(a.x, b.x), at = m == -__builtin_inff() ? 0.0f : m;
+        a = make_float2(m, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) +
+                               b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
+      }
+      out[r] = a;
+    }
+  }
+};
+
+// Backward, dz of a piece: the same product, C = dz [M rounded up to 64][ldc], with
+// zeros in rows behind M and columns behind N (up to ldc), as the products that reduce
+// over them need.  A masked logit (-inf) has no gradient, but in a row that is NaN.
+struct CeGradArgs : GemmArgs {
+  static constexpr bool kPair = false, kRagged = false;
+  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
+  const float2* stats;
+  const float* scalars;  // {1 / c, c scale, or c scale / rows with a target when g_loss is NULL}
+  const float* g_loss;
+  const int32_t* targets;
+  int32_t v0, vocabulary;  // the piece's first column, and the columns of all
+  template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
+  __device__ __forceinline__ void epilogue(f32x16 (&acc)[TM][TN], int64_t, int64_t, int64_t mw, int64_t nw, int lane,
+                                           int wave, int, uint8_t* smem) const {
+    static_assert(TN == 2, "64 columns of a wave");
+    __syncthreads();
+    const int64_t rows64 = (M + 63) / 64 * 64;
+    if (mw >= rows64 || nw >= ldc) return;  // uniform over the wave
+    float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
+    const float unit = scalars[1];
+    const int hi = lane >> 5, nv = (int)min<int64_t>(64, N - nw);  // >= 1: ldc is N rounded up to 64
+    if (bias) {
+      static_for<2>([&](auto j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float b = h2f<DT>(bias[nw + min(32 * j + 8 * (e / 4) + 4 * hi + e % 4, nv - 1)]);
+          static_for<TM>([&](auto i) { acc[i][j][e] += b; });
+        }
+      });
+    }
+    static_for<TM>([&](auto i) {
+      const int64_t row = mw + 32 * i + (lane & 31), rc = min(row, M - 1);
+      const float2 st = stats[rc];
+      const int32_t target = targets[rc];
+      const int64_t t = (int64_t)target - v0 - nw;
+      const float g = g_loss ? g_loss[rc] * unit : unit;
+      const float f = target < 0 ? 0.0f : target >= vocabulary ? __builtin_nanf("") : g;
+      const bool in = row < M;
+      // all masked: every p below is e^-inf
+      const float m = st.x == -__builtin_inff() ? 0.0f : st.x;
+      const float ln = st.x == -__builtin_inff() ? 0.0f : st.y * kLog2e;
+      const bool bad = ln != ln || f != f;  // the whole row is NaN
+      static_for<2>([&](auto j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int col = 32 * j + 8 * (e / 4) + 4 * hi + e % 4;
+          const float z = acc[i][j][e];
+          float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z - m, kLog2e, -ln));
+          p = (p - (col == t ? 1.0f : 0.0f)) * f;
+          acc[i][j][e] = in && col < nv && (bad || z != -__builtin_inff()) ? p : 0.0f;
+        }
+      });
+      rows_put(acc[i][0], lds, lane, 0);
+      rows_put(acc[i][1], lds, lane, 32);
+      asm volatile("" ::: "memory");  // the lanes' writes come before the wave's reads
+#pragma unroll
+      for (int t4 = 0; t4 < 4; ++t4) {
+        const int r = (lane >> 3) + 8 * t4;
+        float v[8];
+        rows_get8(lds + r * kRowsPitch + 8 * (lane & 7), v);
+        if (mw + 32 * i + r < rows64)
+          *reinterpret_cast<u32x4*>(C + (mw + 32 * i + r) * ldc + nw + 8 * (lane & 7)) = pack8<DT>(v);
+      }
+      asm volatile("" ::: "memory");  // and its reads before the next block's writes
+    });
+  }
+};
+
+// Backward, products of a piece: C = half(alpha acc), or (part set) float32 partial
+// sums per split, on top of an earlier piece's with `add`.
+struct CeOutArgs : GemmArgs {
+  static constexpr bool kPair = false, kRagged = true;
+  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
+  float* part;         // [splits][M][N]
+  const float* alpha;  // 1 / c
+  int32_t add;
+  template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
+  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], int64_t, int64_t, int64_t mw, int64_t nw,
+                                           int lane, int wave, int split, uint8_t* smem) const {
+    static_assert(TN == 2, "64 columns of a wave");
+    __syncthreads();
+    const int mv = (int)min<int64_t>(WM, M - mw), c8 = 8 * (lane & 7);
+    const int nc = (int)min<int64_t>(8, N - nw - c8);
+    if (mv <= 0 || N - nw <= 0) return;  // uniform over the wave
+    float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
+    const float scale = part ? 1.0f : *alpha;
+    const bool whole = nc == 8 && N % 4 == 0;
+    int bad = 0;
+    static_for<TM>([&](auto i) {
+      rows_put(acc[i][0], lds, lane, 0);
+      rows_put(acc[i][1], lds, lane, 32);
+      asm volatile("" ::: "memory");
+      f32x4 old[8];
+      if (part && add && whole) {  // all in flight before the first is used
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int row = min(32 * i + (lane >> 3) + 8 * t, mv - 1);
+          const float* p = part + ((int64_t)split * M + mw + row) * N + nw + c8;
+          old[2 * t] = *reinterpret_cast<const f32x4*>(p);
+          old[2 * t + 1] = *reinterpret_cast<const f32x4*>(p + 4);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int r = (lane >> 3) + 8 * t, row = 32 * i + r;
+        float v[8];
+        rows_get8(lds + r * kRowsPitch + c8, v);
+        if (row >= mv || nc <= 0) continue;
+        if (part) {
+          float* p = part + ((int64_t)split * M + mw + row) * N + nw + c8;
+          if (whole) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] += add ? old[2 * t + c / 4][c % 4] : 0.0f;
+            *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+          } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              if (c < nc) p[c] = add ? p[c] + v[c] : v[c];
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) v[c] *= scale;
+          const u32x4 w = pack8<DT>(v);
+          store8(C + (mw + row) * N + nw + c8, w, nc);
+          if (nonfinite) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              bad += c < nc && h_nonfinite<DT>((uint16_t)(w[c / 2] >> (16 * (c & 1)))) ? 1 : 0;
+          }
+        }
+      }
+      asm volatile("" ::: "memory");
+    });
+    if (nonfinite && !part) add_nonfinite(nonfinite, bad);
+  }
+};
+
+// Which tile a product takes.
+enum CeTile { CE_32x128, CE_64x128, CE_128x128, CE_256x256, CE_STAGED_64, CE_STAGED_128, CE_STAGED_ANY };
+constexpr int ce_tile_cols(CeTile t) {
+  return t == CE_256x256 ? 256 : t == CE_STAGED_64 || t == CE_STAGED_ANY ? 64 : 128;
+}
+
+// Launchers, compiled once per half type.  The layouts: forward and dz k-major operands,
+// dX a k-major A, dW neither.
+hipError_t run_ce_fwd_f16(const CeFwdArgs& g, CeTile t, hipStream_t s);
+hipError_t run_ce_fwd_bf16(const CeFwdArgs& g, CeTile t, hipStream_t s);
+hipError_t run_ce_grad_f16(const CeGradArgs& g, CeTile t, hipStream_t s);
+hipError_t run_ce_grad_bf16(const CeGradArgs& g, CeTile t, hipStream_t s);
+hipError_t run_ce_out_f16(const CeOutArgs& g, bool ak, CeTile t, hipStream_t s);
+hipError_t run_ce_out_bf16(const CeOutArgs& g, bool ak, CeTile t, hipStream_t s);
+
+template <int DT, class Args, bool AK, bool BKM, bool DBS, int BM, int BN, int WM, int WN, int OCC, int STG>
+hipError_t launch_ce_tiles(const Args& g, hipStream_t s) {
+  const dim3 grid((unsigned)(cdiv(g.M, BM) * cdiv(g.N, BN)), (unsigned)g.splits);
+  gemm_tile_kernel<DT, BM, BN, WM, WN, OCC, AK, BKM, 0, DBS, STG, false, Args>
+      <<<grid, BM / WM * (BN / WN) * 64, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+template <int DT, class Args, bool AK, bool BKM, bool DBS>
+hipError_t launch_ce(const Args& g, CeTile t, hipStream_t s) {
+  switch (t) {
+    case CE_32x128:
+      if constexpr (std::is_same_v<Args, CeFwdArgs>) return launch_ce_tiles<DT, Args, AK, BKM, DBS, 32, 128, 32, 32, 4, 0>(g, s);
+      return hipErrorInvalidValue;
+    case CE_64x128:
+      if constexpr (AK) return launch_ce_tiles<DT, Args, AK, BKM, DBS, 64, 128, 32, 64, 3, 0>(g, s);
+      return hipErrorInvalidValue;
+    case CE_128x128: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 0>(g, s);
+    case CE_256x256: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 256, 256, 128, 64, 2, 0>(g, s);
+    case CE_STAGED_64: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 1>(g, s);
+    case CE_STAGED_128: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 1>(g, s);
+    case CE_STAGED_ANY: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 2>(g, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace mpx

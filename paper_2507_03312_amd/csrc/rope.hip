@@ -1,119 +1,7 @@
 // Rotary positions with several axes (mpx_rope_fwd, mpx_rope_bwd).
-#include <hip/hip_runtime.h>
-
-#include <algorithm>
-#include <cmath>
-
-#include "common.h"
+#include "rope.h"
 
 namespace mpx {
-
-constexpr int kRopeMaxHd = 512;
-constexpr int kRopeTable = 1024;  // turns (cosine, sine) that a workgroup holds in LDS
-
-struct RopeArgs {
-  const void* X;
-  void* Y;
-  const float* pos;
-  int64_t ldx, ldy;
-  uint32_t pos_rows, rows, heads_rot, copy;  // copy: values copied behind the turned heads
-  int32_t hd, axes, npairs, interleaved, back, in_place;
-  int32_t stream;  // more than the last-level cache holds
-  // a workgroup's rows, and the threads that share a row's heads: thread
-  // (slot, chunk) takes heads slot % head_slots, + head_slots, ... of row
-  // slot / head_slots, with the pairs of `chunk` of each
-  int32_t wg_rows, head_slots, chunks;
-  int32_t first_pair[MPX_ROPE_MAX_AXES + 1];  // axis a owns pairs [first_pair[a], first_pair[a + 1])
-  double step[MPX_ROPE_MAX_AXES];             // log2(base) / pairs
-};
-
-template <int DT> struct RopeValue { typedef uint16_t type; };
-template <> struct RopeValue<MPX_F32> { typedef float type; };
-
-typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
-typedef rope_u32x4 rope_u32x4_any __attribute__((aligned(2)));
-
-// N values at any alignment of theirs (global accesses need no more on gfx950)
-template <int DT, int N> struct RopeVec {
-  typedef typename RopeValue<DT>::type T;
-  T v[N];
-  // NT (16-byte vectors): around the caches
-  template <bool NT = false>
-  __device__ __forceinline__ void load(const T* p) {
-    if constexpr (NT) {
-      const rope_u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const rope_u32x4_any*>(p));
-      __builtin_memcpy(v, &w, sizeof(v));
-    } else {
-      __builtin_memcpy(v, p, sizeof(v));
-    }
-  }
-  template <bool NT = false>
-  __device__ __forceinline__ void store(T* p) const {
-    if constexpr (NT) {
-      rope_u32x4 w;
-      __builtin_memcpy(&w, v, sizeof(v));
-      __builtin_nontemporal_store(w, reinterpret_cast<rope_u32x4_any*>(p));
-    } else {
-      __builtin_memcpy(p, v, sizeof(v));
-    }
-  }
-  // the same vector of another lane
-  __device__ __forceinline__ RopeVec from_lane(int l) const {
-    constexpr int W = (sizeof(v) + 3) / 4;
-    int w[W] = {};
-    __builtin_memcpy(w, v, sizeof(v));
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = __builtin_amdgcn_ds_bpermute(4 * l, w[i]);
-    RopeVec o;
-    __builtin_memcpy(o.v, w, sizeof(v));
-    return o;
-  }
-  __device__ __forceinline__ float get(int i) const {
-    if constexpr (DT == MPX_F32) return v[i];
-    else return h2f<DT>(v[i]);
-  }
-  __device__ __forceinline__ void set(int i, float f) {
-    if constexpr (DT == MPX_F32) v[i] = f;
-    else v[i] = f2h<DT>(f);
-  }
-};
-
-// What both kernels begin with: the copied heads of the workgroup's rows (COPY),
-// and their turns into LDS.
-template <int DT, bool COPY>
-__device__ __forceinline__ void rope_copies_and_turns(const RopeArgs& a, const typename RopeValue<DT>::type* X,
-                                                      typename RopeValue<DT>::type* Y, uint32_t row0,
-                                                      uint32_t nrows, float2* turns) {
-  typedef typename RopeValue<DT>::type T;
-  if (COPY && !a.in_place && a.copy) {
-    constexpr uint32_t VE = 16 / sizeof(T);
-    const int64_t w0 = (int64_t)a.heads_rot * a.hd;
-    const uint32_t nv = a.copy / VE, rest = a.copy % VE;
-    for (uint32_t i = threadIdx.x; i < nrows * nv; i += 256) {
-      const uint32_t r = i / nv, c = (i % nv) * VE;
-      RopeVec<DT, VE> v;
-      v.load(X + r * a.ldx + w0 + c);
-      v.store(Y + r * a.ldy + w0 + c);
-    }
-    for (uint32_t i = threadIdx.x; i < nrows * rest; i += 256) {
-      const int64_t r = i / rest, c = w0 + nv * VE + i % rest;
-      Y[r * a.ldy + c] = X[r * a.ldx + c];
-    }
-  }
-  for (uint32_t i = threadIdx.x; i < nrows * a.npairs; i += 256) {
-    const uint32_t r = i / a.npairs, p = i % a.npairs;
-    int ax = 0;
-#pragma unroll
-    for (int k = 1; k < MPX_ROPE_MAX_AXES; ++k) ax += (int)p >= a.first_pair[k] ? 1 : 0;
-    const double turn = exp2(-(double)((int)p - a.first_pair[ax]) * a.step[ax]) * 0.15915494309189533577;
-    double t = (double)a.pos[(int64_t)((row0 + r) % a.pos_rows) * a.axes + ax] * turn;
-    t -= rint(t);  // exact: what is left is at most half a turn
-    float s, c;
-    sincospif(2.0f * (float)t, &s, &c);
-    turns[i] = make_float2(c, a.back ? -s : s);
-  }
-  __syncthreads();
-}
 
 // Bound by HBM (every value read and written once).  The turns are as many as
 // rows x pairs, far fewer than the values, but dear (float64 angles): a
@@ -139,7 +27,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   // runs of 16 bytes also serve the copied heads, like turned ones (a loop of
   // their own: 12608 x 36 heads of 64 bf16 28.6 us)
   constexpr bool kWide = VW * sizeof(T) == 16;
-  rope_copies_and_turns<DT, !kWide>(a, X, Y, row0, nrows, turns);
+  if constexpr (!kWide) rope_copies<DT>(a, X, a.ldx, Y, nrows);
+  rope_turns(a, row0, nrows, turns);
 
   const int lane = threadIdx.x & 63;
   const uint32_t chunk = lane % a.chunks, wave_slots = 64 / a.chunks;
@@ -219,7 +108,8 @@ __global__ __launch_bounds__(256) void rope_pairs_kernel(RopeArgs a) {
   T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
   const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
 
-  rope_copies_and_turns<DT, true>(a, X, Y, row0, nrows, turns);
+  rope_copies<DT>(a, X, a.ldx, Y, nrows);
+  rope_turns(a, row0, nrows, turns);
 
   const uint32_t chunk = threadIdx.x % a.chunks, slot = threadIdx.x / a.chunks;
   const uint32_t r = slot / a.head_slots, h0 = slot % a.head_slots;
@@ -343,34 +233,15 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
   const int64_t width = (heads_rot + heads_copy) * hd;
   MPX_REQUIRE_FN(ldx >= width && ldy >= width, "row stride below (heads_rot + heads_copy) * hd");
   MPX_REQUIRE_FN(X != Y || ldx == ldy, "in place needs equal row strides");
-  MPX_REQUIRE_FN(plan->axes >= 1 && plan->axes <= MPX_ROPE_MAX_AXES, "axes must be in [1, 4]");
-  MPX_REQUIRE_FN(plan->interleaved == 0 || plan->interleaved == 1, "interleaved must be 0 or 1");
   const uintptr_t mis = reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(Y);
   MPX_REQUIRE_FN(mis % (dt == MPX_F32 ? 4 : 2) == 0 && reinterpret_cast<uintptr_t>(pos) % 4 == 0,
                  "pointers must be aligned to their element");
   RopeArgs a{};
-  int64_t n = 0;
-  // Values of one run: a power of two, at most 16 bytes, that divides every
-  // section's halves (interleaved: twice the pairs), and what is not turned.
-  const bool inter = plan->interleaved != 0;
-  const int wide = dt == MPX_F32 ? 4 : 8;
-  int vw = wide, vp = hd % 2 ? 1 : wide;  // of the kernel of runs, and of pairs of runs
-  for (int ax = 0; ax < plan->axes; ++ax) {
-    const int64_t p = plan->pairs[ax];
-    const double base = plan->base[ax];
-    MPX_REQUIRE_FN(p >= 1 && 2 * (n + p) <= hd, "pairs must be >= 1 and 2 * their sum <= hd");
-    MPX_REQUIRE_FN(std::isfinite(base) && base > 1.0, "base must be finite and > 1");
-    a.step[ax] = std::log2(base) / (double)p;
-    a.first_pair[ax] = (int32_t)n;
-    n += p;
-    while (!inter && p % vw) vw /= 2;
-    while (!inter && p % vp) vp /= 2;
-  }
-  while (2 * n % vw || (hd - 2 * n) % vw) vw /= 2;
-  while (n % vp || (hd / 2 - n) % vp) vp /= 2;
+  int vw, vp;  // of the kernel of runs, and of pairs of runs
+  if (const char* why = rope_plan(plan, hd, dt, a, vw, vp)) MPX_REQUIRE_FN(false, why);
+  const int64_t n = a.npairs;
   const bool pairs = hd / vw > 64 || vw == 1;
   if (pairs) vw = vp;
-  for (int ax = plan->axes; ax <= MPX_ROPE_MAX_AXES; ++ax) a.first_pair[ax] = (int32_t)n;
   a.X = X;
   a.Y = Y;
   a.pos = pos;
@@ -378,10 +249,6 @@ static int rope(const char* fn, bool back, const void* X, int64_t ldx, void* Y, 
   a.ldy = ldy;
   a.heads_rot = (uint32_t)heads_rot;
   a.copy = (uint32_t)(heads_copy * hd);
-  a.hd = (int32_t)hd;
-  a.axes = plan->axes;
-  a.npairs = (int32_t)n;
-  a.interleaved = plan->interleaved;
   a.back = back ? 1 : 0;
   a.in_place = X == Y ? 1 : 0;
   // Values past the 256 MB last-level cache go around it (29997 rows of 48 heads of
