@@ -178,8 +178,12 @@ extern "C" int mpx_gated_fwd(const void* X, const void* W, const void* b, void* 
   GemmArgs g = gated_args(X, W, H, M, N, K, K, N, act);
   g.bias = (const uint16_t*)b;
   g.pre = (uint16_t*)Pre;
-  if (M <= 32) MPX_HIP(dt == MPX_F16 ? launch_few<MPX_F16>(g, s) : launch_few<MPX_BF16>(g, s));
-  else MPX_HIP(dt == MPX_F16 ? run_gated_fwd_f16(g, N * K, s) : run_gated_fwd_bf16(g, N * K, s));
+  if (M <= 32) {
+    MPX_HIP(dt == MPX_F16 ? launch_few<MPX_F16>(g, s) : launch_few<MPX_BF16>(g, s));
+    return MPX_OK;
+  }
+  const RowTile t = gated_tile(g, true);
+  MPX_HIP(dt == MPX_F16 ? run_gated_fwd_f16(g, N * K, t, s) : run_gated_fwd_bf16(g, N * K, t, s));
   return MPX_OK;
 }
 
@@ -219,7 +223,8 @@ extern "C" int mpx_linear_bwd_gated(const void* X, const void* W, const void* dY
     } else {
       GemmArgs g = gated_args(dY, W, dPre, M, K, N, K, 2 * K, act);
       g.dact = (const uint16_t*)Pre;
-      MPX_HIP(dt == MPX_F16 ? run_gated_bwd_f16(g, s) : run_gated_bwd_bf16(g, s));
+      const RowTile t = gated_tile(g, false);
+      MPX_HIP(dt == MPX_F16 ? run_gated_bwd_f16(g, t, s) : run_gated_bwd_bf16(g, t, s));
     }
   }
   if (dW || db)

@@ -36,48 +36,61 @@ __device__ __forceinline__ void gate_act_grad(float x, float& a, float& d) {
 // accumulator columns are G and U of the same 32 columns of H.
 template <int ACT>
 struct GatedArgs : GemmArgs {  // C = H, pre = [G | U] or NULL, bias [2 N] or NULL
-  static constexpr bool kPair = true, kRagged = false;
-  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
+  static constexpr bool kPair = true, kRagged = false, kNarrow = false;
+  static constexpr int kPitch = 104, kBytes = 32 * kPitch * 2;  // 32 rows of H, G and U
+  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kBytes; }
   int64_t pair;
+  template <int DT, int TM, int STG>
+  __device__ __forceinline__ NoPrefetch prefetch(int64_t, int64_t, int) const { return {}; }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
-  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], int64_t, int64_t, int64_t mw, int64_t nw,
-                                           int lane, int wave, int, uint8_t* smem) const {
+  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], const NoPrefetch&, int64_t, int64_t, int64_t mw,
+                                           int64_t nw, int lane, int wave, int, uint8_t* smem) const {
     __syncthreads();  // every wave is done reading the stage buffers
     const int mv = (int)min<int64_t>(WM, M - mw), c8 = 8 * (lane & 3);
     const int nc = (int)min<int64_t>(8, N - nw - c8);
     if (mv <= 0 || N - nw <= 0) return;  // uniform over the wave
-    float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
-    float bg[8] = {}, bu[8] = {};
-    if (bias && nc > 0) {
-      unpack8<DT>(load8(bias + nw + c8, nc), bg);
-      unpack8<DT>(load8(bias + N + nw + c8, nc), bu);
+    const int nv = (int)min<int64_t>(32, N - nw);
+    uint16_t* lds = reinterpret_cast<uint16_t*>(smem + wave * kBytes);
+    f32x4 bg[4] = {}, bu[4] = {};
+    if (bias) {  // uniform
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = min(8 * q + 4 * (lane >> 5), nv - 1);
+        bg[q] = load4<DT>(bias + nw + at, nv - at);
+        bu[q] = load4<DT>(bias + N + nw + at, nv - at);
+      }
     }
     static_for<TM>([&](auto i) {
-      rows_put(acc[i][0], lds, lane, 0);
-      rows_put(acc[i][1], lds, lane, 32);
+      asm volatile("" ::: "memory");  // the wave's reads of the block before come first
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float g[4], u[4], h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          g[k] = acc[i][0][4 * q + k] + bg[q][k];
+          u[k] = acc[i][1][4 * q + k] + bu[q][k];
+          h[k] = gate_act<ACT>(g[k]) * u[k];
+        }
+        half_put<DT, kPitch>(h[0], h[1], h[2], h[3], lds, lane, 8 * q);
+        if (pre) {
+          half_put<DT, kPitch>(g[0], g[1], g[2], g[3], lds, lane, 32 + 8 * q);
+          half_put<DT, kPitch>(u[0], u[1], u[2], u[3], lds, lane, 64 + 8 * q);
+        }
+      }
       asm volatile("" ::: "memory");  // the lanes' writes come before the wave's reads
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int r = (lane >> 2) + 16 * t, row = 32 * i + r;
-        float a[8], b[8], h[8];
-        rows_get8(lds + r * kRowsPitch + c8, a);
-        rows_get8(lds + r * kRowsPitch + 32 + c8, b);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          a[c] += bg[c];
-          b[c] += bu[c];
-          h[c] = gate_act<ACT>(a[c]) * b[c];
-        }
+        const uint16_t* p = lds + r * kPitch + c8;
         if (row < mv && nc > 0) {
-          store8(C + (mw + row) * N + nw + c8, pack8<DT>(h), nc);
+          store8(C + (mw + row) * N + nw + c8, *reinterpret_cast<const u32x4*>(p), nc);
           if (pre) {
-            uint16_t* p = pre + (mw + row) * 2 * N + nw + c8;
-            store8(p, pack8<DT>(a), nc);
-            store8(p + N, pack8<DT>(b), nc);
+            uint16_t* o = pre + (mw + row) * 2 * N + nw + c8;
+            store8(o, *reinterpret_cast<const u32x4*>(p + 32), nc);
+            store8(o + N, *reinterpret_cast<const u32x4*>(p + 64), nc);
           }
         }
       }
-      asm volatile("" ::: "memory");  // and its reads before the next block's writes
     });
   }
 };
@@ -86,11 +99,13 @@ struct GatedArgs : GemmArgs {  // C = H, pre = [G | U] or NULL, bias [2 N] or NU
 // layout (dact = [G | U], C = [dG | dU], rows of 2 N).
 template <int ACT>
 struct GatedBwdArgs : GemmArgs {
-  static constexpr bool kPair = false, kRagged = false;
+  static constexpr bool kPair = false, kRagged = false, kNarrow = false;
   static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
+  template <int DT, int TM, int STG>
+  __device__ __forceinline__ NoPrefetch prefetch(int64_t, int64_t, int) const { return {}; }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
-  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], int64_t, int64_t, int64_t mw, int64_t nw,
-                                           int lane, int wave, int, uint8_t* smem) const {
+  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], const NoPrefetch&, int64_t, int64_t, int64_t mw,
+                                           int64_t nw, int lane, int wave, int, uint8_t* smem) const {
     static_assert(TN == 2, "64 columns of a wave");
     __syncthreads();
     const int mv = (int)min<int64_t>(WM, M - mw), c8 = 8 * (lane & 7);
@@ -98,7 +113,9 @@ struct GatedBwdArgs : GemmArgs {
     if (mv <= 0 || N - nw <= 0) return;
     float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
     static_for<TM>([&](auto i) {
-      u32x4 gw[4], uw[4];  // all in flight before the first is used
+      // all in flight before the first is used.  (Loaded ahead of the main loop they cost
+      // more than they hide: 12608 x 2048 x 768 74.5 -> 77.9 us, 8320 x 1024 x 384 21.5 -> 23.6)
+      u32x4 gw[4], uw[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int row = min(32 * i + (lane >> 3) + 8 * t, mv - 1);
@@ -134,47 +151,46 @@ struct GatedBwdArgs : GemmArgs {
   }
 };
 
-// Tile launches.  Both products have a k-major A and no splits; BKM: the layout of B.
-template <int DT, class Args, bool BKM, int BM, int BN, int WM, int OCC, int STG>
-hipError_t launch_gated_tiles(const Args& g, hipStream_t s) {
-  constexpr int BC = Args::kPair ? BN / 2 : BN;
-  const int64_t tiles = cdiv(g.M, BM) * cdiv(g.N, BC);
-  gemm_tile_kernel<DT, BM, BN, WM, 64, OCC, true, BKM, 0, false, STG, false, Args>
-      <<<(unsigned)tiles, BM / WM * (BN / 64) * 64, 0, s>>>(g);
-  return hipGetLastError();
-}
-
-template <int DT, class Args, bool BKM>
-hipError_t launch_gated(const Args& g, hipStream_t s) {
-  const bool dma = dma_ok(g, operands_aligned(g), true, BKM);
-  const int64_t cols = Args::kPair ? 2 * g.N : g.N;
-  if (!dma) {
-    if (staged_any(g, true, BKM)) return launch_gated_tiles<DT, Args, BKM, 64, 64, 32, 2, 2>(g, s);
-    if (cdiv(g.M, 64) * cdiv(cols, 64) <= 512) return launch_gated_tiles<DT, Args, BKM, 64, 64, 32, 2, 1>(g, s);
-    return launch_gated_tiles<DT, Args, BKM, 128, 128, 64, 2, 1>(g, s);
+// Tile of either product; pair: W's halves side by side, two columns for each of H.  Direct
+// tiles: forward without and with Pre 1.1% and 0.9% slower than the fastest on average
+// (64 x 128 alone 2.1 and 1.5, where the largest lose 20), backward 0.3%.  256 x 256 tiles
+// were never more than 0.1% better a choice.
+inline RowTile gated_tile(const GemmArgs& g, bool pair) {
+  const int64_t cols = pair ? 2 * g.N : g.N;
+  if (!dma_ok(g, operands_aligned(g), true, pair)) {
+    if (staged_any(g, true, pair)) return STAGED_ANY;
+    return cdiv(g.M, 64) * cdiv(cols, 64) <= 512 ? STAGED_64 : STAGED_128;
   }
-  if (cdiv(g.M, 256) * cdiv(cols, 256) >= 512) return launch_gated_tiles<DT, Args, BKM, 256, 256, 128, 2, 0>(g, s);
-  if (cdiv(g.M, 128) * cdiv(cols, 128) >= 384) return launch_gated_tiles<DT, Args, BKM, 128, 128, 64, 2, 0>(g, s);
-  return launch_gated_tiles<DT, Args, BKM, 64, 128, 32, 3, 0>(g, s);
+  static const RowCost fwd[] = {{TILE_64x128, 64, 128, 3, {0.21, 0.60, 0.87}, 2.07},
+                                {TILE_128x128, 128, 128, 2, {0.62, 0.62, 0}, 4.58},
+                                {TILE_192x128, 192, 128, 2, {0.63, 1.00, 0}, 5.62}};
+  static const RowCost keep[] = {{TILE_64x128, 64, 128, 3, {0.35, 0.62, 0.84}, 1.68},
+                                 {TILE_128x128, 128, 128, 2, {0.73, 0.73, 0}, 3.82},
+                                 {TILE_192x128, 192, 128, 2, {0.76, 0.80, 0}, 5.86}};
+  static const RowCost bwd[] = {{TILE_64x128, 64, 128, 3, {0.92, 0.95, 1.02}, 2.33},
+                                {TILE_128x128, 128, 128, 2, {0.83, 0.83, 0}, 6.84},
+                                {TILE_192x128, 192, 128, 2, {1.12, 1.12, 0}, 10.0}};
+  return choose_rows(!pair ? bwd : g.pre ? keep : fwd, g.M, cols, g.K).tile;
 }
 
-hipError_t run_gated_fwd_f16(const GemmArgs& g, int64_t pair, hipStream_t s);
-hipError_t run_gated_fwd_bf16(const GemmArgs& g, int64_t pair, hipStream_t s);
-hipError_t run_gated_bwd_f16(const GemmArgs& g, hipStream_t s);
-hipError_t run_gated_bwd_bf16(const GemmArgs& g, hipStream_t s);
+// Launchers, compiled once per half type
+hipError_t run_gated_fwd_f16(const GemmArgs& g, int64_t pair, RowTile t, hipStream_t s);
+hipError_t run_gated_fwd_bf16(const GemmArgs& g, int64_t pair, RowTile t, hipStream_t s);
+hipError_t run_gated_bwd_f16(const GemmArgs& g, RowTile t, hipStream_t s);
+hipError_t run_gated_bwd_bf16(const GemmArgs& g, RowTile t, hipStream_t s);
 
 template <int DT, int ACT>
-hipError_t run_gated_fwd(const GemmArgs& g, int64_t pair, hipStream_t s) {
+hipError_t run_gated_fwd(const GemmArgs& g, int64_t pair, RowTile t, hipStream_t s) {
   GatedArgs<ACT> a;
   static_cast<GemmArgs&>(a) = g;
   a.pair = pair;
-  return launch_gated<DT, GatedArgs<ACT>, true>(a, s);
+  return launch_rows<DT, GatedArgs<ACT>, true, true, false>(a, t, s);
 }
 template <int DT, int ACT>
-hipError_t run_gated_bwd(const GemmArgs& g, hipStream_t s) {
+hipError_t run_gated_bwd(const GemmArgs& g, RowTile t, hipStream_t s) {
   GatedBwdArgs<ACT> a;
   static_cast<GemmArgs&>(a) = g;
-  return launch_gated<DT, GatedBwdArgs<ACT>, false>(a, s);
+  return launch_rows<DT, GatedBwdArgs<ACT>, true, false, false>(a, t, s);
 }
 
 }  // namespace mpx

@@ -774,12 +774,12 @@ __device__ __forceinline__ float frag_sum8(const uint4& f) {
 // B8: operand B is an 8-bit checkpoint (register-staged kernels only).
 //
 // Args: GemmArgs, or a type derived from it with an end of its own: its epilogue()
-// gets the accumulators in place of the epilogues above, its lds_bytes() is the LDS
-// that takes, and with kPair operand B is a pair of matrices (PairOperand, g.pair
+// gets the accumulators in place of the epilogues above, with what its prefetch() loaded
+// ahead of the main loop; its lds_bytes() is the LDS that takes, and with kPair operand B is a pair of matrices (PairOperand, g.pair
 // elements apart; N, n0 and nw count columns of one).  With kRagged the reduction of a
 // product with an mn-major B may end inside a k tile: A has zeros behind it, up to the
-// tile's end, and B's last k row is read again there.  The sums of DBS go to dbp, also
-// without splits.
+// tile's end, and B's last k row is read again there.  The sums of DBS go to dbp, or
+// without splits, where db is set, times db_scale() to db.
 template <class Args, int BM, int BN, int WM, int WN>
 constexpr int own_epilogue_bytes() {
   if constexpr (std::is_same_v<Args, GemmArgs>) return 0;
@@ -875,6 +875,11 @@ void gemm_tile_kernel(Args g) {
     }
   }
 
+  // likewise what an own epilogue reads
+  const auto early = [&] {
+    if constexpr (kOwn) return g.template prefetch<DT, TM, STG>(mw, nw, lane);
+    else return 0;
+  }();
   auto issue = [&](int kt, auto par) {  // par: STG's register set, kt & 1
     if constexpr (STG != 0) {
       const bool past = kt >= nk;
@@ -936,7 +941,7 @@ void gemm_tile_kernel(Args g) {
   });
   // bias-gradient sums: tile columns sharing the A rows, this one's index,
   // and the next k tile this wave adds up (uniform over the wave)
-  const bool db_parts = kOwn || g.splits > 1;
+  const bool db_parts = (kOwn && !g.db) || g.splits > 1;
   const int db_cols = db_parts ? (int)((g.N + BN - 1) / BN) : 1;
   const int db_col = db_parts ? (int)(n0 / BN) : 0;
   const bool dbw = DBS && wn0 == 0 && (db_parts || n0 == 0);
@@ -1026,7 +1031,9 @@ void gemm_tile_kernel(Args g) {
           if (db_parts) {
             g.dbp[row * ((int64_t)g.splits * db_cols) + (int64_t)split * db_cols + db_col] = v;
           } else {
-            const uint16_t h = f2h<DT>(v);
+            uint16_t h;
+            if constexpr (kOwn) h = f2h<DT>(v * g.db_scale());
+            else h = f2h<DT>(v);
             g.db[row] = h;
             bad += h_nonfinite<DT>(h) ? 1 : 0;
           }
@@ -1037,7 +1044,7 @@ void gemm_tile_kernel(Args g) {
   }
   // the accumulators hold C^T blocks (the MFMA operands are swapped above)
   if constexpr (kOwn) {
-    g.template epilogue<DT, BM, BN, WM, WN>(acc, m0, n0, mw, nw, lane, wave, split, smem);
+    g.template epilogue<DT, BM, BN, WM, WN>(acc, early, m0, n0, mw, nw, lane, wave, split, smem);
     return;
   }
   if (g.splits > 1) {

@@ -39,6 +39,15 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
     v[2 * k + 1] = h2f<DT>((uint16_t)(w[k] >> 16));
   }
 }
+// The same of results that need nothing from the row layout: rounded to half first, which
+// halves the LDS traffic.  Rows of PITCH halves, a multiple of 8 for 16-byte reads.
+template <int DT, int PITCH>
+__device__ __forceinline__ void half_put(float a, float b, float c, float d, uint16_t* lds, int lane, int col) {
+  *reinterpret_cast<u32x2*>(lds + (lane & 31) * PITCH + col + 4 * (lane >> 5)) =
+      u32x2{f2h<DT>(a) | ((uint32_t)f2h<DT>(b) << 16), f2h<DT>(c) | ((uint32_t)f2h<DT>(d) << 16)};
+}
+constexpr int kHalfPitch = 72;  // 64 columns
+constexpr int kHalfBytes = 32 * kHalfPitch * 2;
 // 8 halves at p, or the first nc of them
 __device__ __forceinline__ void store8(uint16_t* p, u32x4 w, int nc) {
   if (nc >= 8) {
@@ -56,6 +65,115 @@ __device__ __forceinline__ u32x4 load8(const uint16_t* p, int nc) {
   for (int c = 0; c < 8; ++c)
     if (c < nc) w[c / 2] |= (uint32_t)p[c] << (16 * (c & 1));
   return w;
+}
+
+// Values p[0 .. 3] of a vector, the last `left` (>= 1) of its ones from p on at most; what is
+// past them repeats the last one.
+template <int DT>
+__device__ __forceinline__ f32x4 load4(const uint16_t* p, int left) {
+  typedef u32x2 u32x2_half __attribute__((aligned(2)));
+  f32x4 v;
+  if (left >= 4) {
+    const u32x2 w = *reinterpret_cast<const u32x2_half*>(p);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = h2f<DT>((uint16_t)(w[c / 2] >> (16 * (c & 1))));
+  } else {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = h2f<DT>(p[min(c, left - 1)]);
+  }
+  return v;
+}
+// acc += bias of its columns, from b on, nv (>= 1) of them in the output
+template <int DT, int TM, int TN>
+__device__ __forceinline__ void add_bias(f32x16 (&acc)[TM][TN], const uint16_t* b, int nv, int lane) {
+  static_for<TN>([&](auto j) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = 32 * j + 8 * q + 4 * (lane >> 5);
+      const int at = min(col, nv - 1);
+      const f32x4 v = load4<DT>(b + at, nv - at);
+      static_for<TM>([&](auto i) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] += v[k];
+      });
+    }
+  });
+}
+
+struct NoPrefetch {};
+
+// Which tile a product with an end of its own takes: direct-to-LDS ones by size, or
+// register-staged ones (any alignment; STAGED_ANY: also rows of fewer than 8 values).
+enum RowTile { TILE_32x128, TILE_64x128, TILE_128x128, TILE_256x256, TILE_192x128, STAGED_64, STAGED_128, STAGED_ANY };
+constexpr int tile_cols(RowTile t) {
+  return t == TILE_256x256 ? 256 : t == STAGED_64 || t == STAGED_ANY ? 64 : 128;
+}
+
+// Direct-to-LDS tiles by estimated time: a chip of 256 CUs runs 256 x per_cu workgroups at
+// a time; a round of o per CU takes its k tiles of 64 x k_us[o - 1] plus o x tile_us for what
+// surrounds the k loops, and the last round has the workgroups that are left.  The
+// constants are set for the choice, not for the times: those of least loss on 70% of
+// 520 products of each kind (33 to 16640 rows, 128 to 32768 columns, reductions of 64 to
+// 1536, a quarter of them large), operands from HBM; what they lose on the other 30%
+// stands at each table.
+struct RowCost {
+  RowTile tile;
+  int bm, bn, per_cu;
+  double k_us[3], tile_us;
+};
+struct RowChoice {
+  RowTile tile;
+  int splits;
+  double us;
+};
+// cols: columns of operand B's tiles; splits 1 .. most, each with `len` / splits of the
+// reduction.  join_us, part_us: what a second split costs, and every output of a split.
+template <int N>
+inline RowChoice choose_rows(const RowCost (&costs)[N], int64_t M, int64_t cols, int64_t len, int64_t most = 1,
+                             double join_us = 0.0, double part_us = 0.0, bool one_is_free = true) {
+  RowChoice best{costs[0].tile, 1, 0.0};
+  for (const RowCost& c : costs) {
+    const int64_t tiles = cdiv(M, c.bm) * cdiv(cols, c.bn), slots = 256 * c.per_cu;
+    for (int64_t s = 1; s <= most; ++s) {
+      const double nk = (double)cdiv(len, 64 * s);
+      auto round = [&](int64_t o) { return o ? nk * c.k_us[o - 1] + c.tile_us * (double)o : 0.0; };
+      const double t = (double)(tiles * s / slots) * round(c.per_cu) + round(cdiv(tiles * s % slots, 256)) +
+                       (s > 1 ? join_us : 0.0) +
+                       (s > 1 || !one_is_free ? part_us * (double)s * (double)M * (double)cols : 0.0);
+      if (best.us == 0.0 || t < best.us) best = {c.tile, (int)s, t};
+    }
+  }
+  return best;
+}
+
+template <int DT, class Args, bool AK, bool BKM, bool DBS, int BM, int BN, int WM, int WN, int OCC, int STG>
+hipError_t launch_row_tiles(const Args& g, hipStream_t s) {
+  const dim3 grid((unsigned)(cdiv(g.M, BM) * cdiv(g.N, Args::kPair ? BN / 2 : BN)), (unsigned)g.splits);
+  gemm_tile_kernel<DT, BM, BN, WM, WN, OCC, AK, BKM, 0, DBS, STG, false, Args>
+      <<<grid, BM / WM * (BN / WN) * 64, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+// AK, BKM: the operands' layouts; DBS: with the sums of A's rows.  32 x 128 tiles (waves of
+// 32 columns) only where Args can end them.
+template <int DT, class Args, bool AK, bool BKM, bool DBS>
+hipError_t launch_rows(const Args& g, RowTile t, hipStream_t s) {
+  switch (t) {
+    case TILE_32x128:
+      if constexpr (Args::kNarrow)
+        return launch_row_tiles<DT, Args, AK, BKM, DBS, 32, 128, 32, 32, 4, 0>(g, s);
+      return hipErrorInvalidValue;
+    case TILE_64x128:
+      if constexpr (AK) return launch_row_tiles<DT, Args, AK, BKM, DBS, 64, 128, 32, 64, 3, 0>(g, s);
+      return hipErrorInvalidValue;
+    case TILE_128x128: return launch_row_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 0>(g, s);
+    case TILE_192x128: return launch_row_tiles<DT, Args, AK, BKM, DBS, 192, 128, 96, 64, 2, 0>(g, s);
+    case TILE_256x256: return launch_row_tiles<DT, Args, AK, BKM, DBS, 256, 256, 128, 64, 2, 0>(g, s);
+    case STAGED_64: return launch_row_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 1>(g, s);
+    case STAGED_128: return launch_row_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 1>(g, s);
+    case STAGED_ANY: return launch_row_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 2>(g, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace mpx

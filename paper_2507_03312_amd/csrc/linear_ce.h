@@ -22,28 +22,33 @@ __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32);
 // Forward.  A = X, B = W; lane l of a 32 x 32 block has row l % 32 and 16 of its 32
 // columns, so a row's maximum and sum take one exchange beside the lane's own values.
 struct CeFwdArgs : GemmArgs {
-  static constexpr bool kPair = false, kRagged = false;
+  static constexpr bool kPair = false, kRagged = false, kNarrow = true;
   static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm * (bn / wn) * 8; }
   float2* part;  // [tile column][M]
   float* zt;     // [M]: the target's logit
   const int32_t* targets;
+  template <int TM>
+  struct Rows {
+    int32_t target[TM];
+  };
+  template <int DT, int TM, int STG>
+  __device__ __forceinline__ Rows<TM> prefetch(int64_t mw, int64_t, int lane) const {
+    Rows<TM> r;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int64_t row = mw + 32 * i + (lane & 31);
+      r.target[i] = targets && row < M ? targets[row] : -1;
+    }
+    return r;
+  }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
-  __device__ __forceinline__ void epilogue(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int64_t mw, int64_t nw,
-                                           int lane, int wave, int, uint8_t* smem) const {
+  __device__ __forceinline__ void epilogue(f32x16 (&acc)[TM][TN], const Rows<TM>& early, int64_t m0, int64_t n0,
+                                           int64_t mw, int64_t nw, int lane, int wave, int, uint8_t* smem) const {
     __syncthreads();  // every wave is done reading the stage buffers
     float2* rows = reinterpret_cast<float2*>(smem);  // [wave column][BM]
     const int hi = lane >> 5, wc = wave % (BN / WN), wr = wave / (BN / WN);
     const int nv = (int)min<int64_t>(WN, N - nw);  // may be <= 0
-    if (bias) {
-      static_for<TN>([&](auto j) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int col = 32 * j + 8 * (e / 4) + 4 * hi + e % 4;
-          const float b = nv > 0 ? h2f<DT>(bias[nw + min(col, nv - 1)]) : 0.0f;
-          static_for<TM>([&](auto i) { acc[i][j][e] += b; });
-        }
-      });
-    }
+    if (bias && nv > 0) add_bias<DT>(acc, bias + nw, nv, lane);
     if (nv < WN) {  // uniform: columns behind the vocabulary have probability 0
       static_for<TN>([&](auto j) {
 #pragma unroll
@@ -55,15 +60,13 @@ struct CeFwdArgs : GemmArgs {
     }
     static_for<TM>([&](auto i) {
       const int64_t row = mw + 32 * i + (lane & 31);
-      if (targets) {
-        const int64_t t = row < M ? (int64_t)targets[row] - nw : -1;
-        if (__ballot(t >= 0 && t < nv)) {  // few tiles hold a target
-          static_for<TN>([&](auto j) {
+      const int64_t t = early.target[i] < 0 ? -1 : early.target[i] - nw;
+      if (__ballot(t >= 0 && t < nv)) {  // few tiles hold a target
+        static_for<TN>([&](auto j) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (t == 32 * j + 8 * (e / 4) + 4 * hi + e % 4 && t < nv) zt[row] = acc[i][j][e];
-          });
-        }
+          for (int e = 0; e < 16; ++e)
+            if (t == 32 * j + 8 * (e / 4) + 4 * hi + e % 4 && t < nv) zt[row] = acc[i][j][e];
+        });
       }
       float m = acc[i][0][0];
       static_for<TN>([&](auto j) {
@@ -99,82 +102,116 @@ struct CeFwdArgs : GemmArgs {
 // Backward, dz of a piece: the same product, C = dz [M rounded up to 64][ldc], with
 // zeros in rows behind M and columns behind N (up to ldc), as the products that reduce
 // over them need.  A masked logit (-inf) has no gradient, but in a row that is NaN.
+// twice (up to 64 rows): row 64 + r holds what rounding row r to half left, and the
+// products take both.  Few rows have few large dz (their targets'), whose roundings do
+// not average out: 4 rows of 170 columns bf16 3.3e-3 of dX's norm against 1.8e-3 for one
+// rounding of the result, while the second rows cost nothing beside the reading of W.
 struct CeGradArgs : GemmArgs {
-  static constexpr bool kPair = false, kRagged = false;
-  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
+  static constexpr bool kPair = false, kRagged = false, kNarrow = false;
+  static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kHalfBytes; }
   const float2* stats;
   const float* scalars;  // {1 / c, c scale, or c scale / rows with a target when g_loss is NULL}
   const float* g_loss;
   const int32_t* targets;
   int32_t v0, vocabulary;  // the piece's first column, and the columns of all
+  int32_t twice;
+  template <int TM>
+  struct Rows {
+    float2 stats[TM];
+    float g[TM];
+    int32_t target[TM];
+    float unit;
+  };
+  template <int DT, int TM, int STG>
+  __device__ __forceinline__ Rows<TM> prefetch(int64_t mw, int64_t, int lane) const {
+    Rows<TM> r;
+    r.unit = scalars[1];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int64_t row = min(mw + 32 * i + (lane & 31), M - 1);
+      r.stats[i] = stats[row];
+      r.target[i] = targets[row];
+      r.g[i] = g_loss ? g_loss[row] : 1.0f;
+    }
+    return r;
+  }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
-  __device__ __forceinline__ void epilogue(f32x16 (&acc)[TM][TN], int64_t, int64_t, int64_t mw, int64_t nw, int lane,
-                                           int wave, int, uint8_t* smem) const {
+  __device__ __forceinline__ void epilogue(f32x16 (&acc)[TM][TN], const Rows<TM>& early, int64_t, int64_t, int64_t mw,
+                                           int64_t nw, int lane, int wave, int, uint8_t* smem) const {
     static_assert(TN == 2, "64 columns of a wave");
     __syncthreads();
     const int64_t rows64 = (M + 63) / 64 * 64;
     if (mw >= rows64 || nw >= ldc) return;  // uniform over the wave
-    float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
-    const float unit = scalars[1];
+    uint16_t* lds = reinterpret_cast<uint16_t*>(smem + wave * kHalfBytes);
     const int hi = lane >> 5, nv = (int)min<int64_t>(64, N - nw);  // >= 1: ldc is N rounded up to 64
-    if (bias) {
-      static_for<2>([&](auto j) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float b = h2f<DT>(bias[nw + min(32 * j + 8 * (e / 4) + 4 * hi + e % 4, nv - 1)]);
-          static_for<TM>([&](auto i) { acc[i][j][e] += b; });
-        }
-      });
-    }
+    if (bias) add_bias<DT>(acc, bias + nw, nv, lane);
     static_for<TM>([&](auto i) {
-      const int64_t row = mw + 32 * i + (lane & 31), rc = min(row, M - 1);
-      const float2 st = stats[rc];
-      const int32_t target = targets[rc];
+      const int64_t row = mw + 32 * i + (lane & 31);
+      const float2 st = early.stats[i];
+      const int32_t target = early.target[i];
       const int64_t t = (int64_t)target - v0 - nw;
-      const float g = g_loss ? g_loss[rc] * unit : unit;
-      const float f = target < 0 ? 0.0f : target >= vocabulary ? __builtin_nanf("") : g;
-      const bool in = row < M;
-      // all masked: every p below is e^-inf
-      const float m = st.x == -__builtin_inff() ? 0.0f : st.x;
-      const float ln = st.x == -__builtin_inff() ? 0.0f : st.y * kLog2e;
-      const bool bad = ln != ln || f != f;  // the whole row is NaN
-      static_for<2>([&](auto j) {
+      const float f = row >= M || target < 0 ? 0.0f
+                      : target >= vocabulary ? __builtin_nanf("") : early.g[i] * early.unit;
+      // f p = f 2^(z log2 e + c): a masked z gives 0, a NaN in ln or f a NaN row.  All
+      // masked (m = -inf): c = 0
+      const float c = row >= M ? -__builtin_inff()
+                      : st.x == -__builtin_inff() ? 0.0f : -__builtin_fmaf(st.x, kLog2e, st.y * kLog2e);
+      const bool plain = nv == 64 && !__ballot(t >= 0 && t < 64);  // uniform: no target, no edge
+      for (int low = 0; low <= twice; ++low) {
+        asm volatile("" ::: "memory");  // the wave's reads of the block before come first
+        static_for<2>([&](auto j) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int col = 32 * j + 8 * (e / 4) + 4 * hi + e % 4;
-          const float z = acc[i][j][e];
-          float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z - m, kLog2e, -ln));
-          p = (p - (col == t ? 1.0f : 0.0f)) * f;
-          acc[i][j][e] = in && col < nv && (bad || z != -__builtin_inff()) ? p : 0.0f;
+          for (int q = 0; q < 4; ++q) {
+            float p[4];
+            if (plain) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                p[k] = f * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + k], kLog2e, c));
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int col = 32 * j + 8 * q + 4 * hi + k;
+                const float z = acc[i][j][4 * q + k];
+                p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, c));
+                p[k] = f * (p[k] - (col == t && z != -__builtin_inff() ? 1.0f : 0.0f));
+                p[k] = col < nv ? p[k] : 0.0f;
+              }
+            }
+            if (low) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) p[k] -= h2f<DT>(f2h<DT>(p[k]));
+            }
+            half_put<DT, kHalfPitch>(p[0], p[1], p[2], p[3], lds, lane, 32 * j + 8 * q);
+          }
+        });
+        asm volatile("" ::: "memory");  // the lanes' writes come before the wave's reads
+#pragma unroll
+        for (int t4 = 0; t4 < 4; ++t4) {
+          const int r = (lane >> 3) + 8 * t4;
+          const u32x4 w = *reinterpret_cast<const u32x4*>(lds + r * kHalfPitch + 8 * (lane & 7));
+          if (mw + 32 * i + r < rows64)
+            *reinterpret_cast<u32x4*>(C + (mw + 32 * i + r + 64 * low) * ldc + nw + 8 * (lane & 7)) = w;
         }
-      });
-      rows_put(acc[i][0], lds, lane, 0);
-      rows_put(acc[i][1], lds, lane, 32);
-      asm volatile("" ::: "memory");  // the lanes' writes come before the wave's reads
-#pragma unroll
-      for (int t4 = 0; t4 < 4; ++t4) {
-        const int r = (lane >> 3) + 8 * t4;
-        float v[8];
-        rows_get8(lds + r * kRowsPitch + 8 * (lane & 7), v);
-        if (mw + 32 * i + r < rows64)
-          *reinterpret_cast<u32x4*>(C + (mw + 32 * i + r) * ldc + nw + 8 * (lane & 7)) = pack8<DT>(v);
       }
-      asm volatile("" ::: "memory");  // and its reads before the next block's writes
     });
   }
 };
 
 // Backward, products of a piece: C = half(alpha acc), or (part set) float32 partial
-// sums per split, on top of an earlier piece's with `add`.
+// sums per split, on top of an earlier piece's in the first `add` of them.
 struct CeOutArgs : GemmArgs {
-  static constexpr bool kPair = false, kRagged = true;
+  static constexpr bool kPair = false, kRagged = true, kNarrow = false;
   static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
   float* part;         // [splits][M][N]
   const float* alpha;  // 1 / c
   int32_t add;
+  __device__ __forceinline__ float db_scale() const { return *alpha; }
+  template <int DT, int TM, int STG>
+  __device__ __forceinline__ NoPrefetch prefetch(int64_t, int64_t, int) const { return {}; }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
-  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], int64_t, int64_t, int64_t mw, int64_t nw,
-                                           int lane, int wave, int split, uint8_t* smem) const {
+  __device__ __forceinline__ void epilogue(const f32x16 (&acc)[TM][TN], const NoPrefetch&, int64_t, int64_t,
+                                           int64_t mw, int64_t nw, int lane, int wave, int split,
+                                           uint8_t* smem) const {
     static_assert(TN == 2, "64 columns of a wave");
     __syncthreads();
     const int mv = (int)min<int64_t>(WM, M - mw), c8 = 8 * (lane & 7);
@@ -182,14 +219,14 @@ struct CeOutArgs : GemmArgs {
     if (mv <= 0 || N - nw <= 0) return;  // uniform over the wave
     float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
     const float scale = part ? 1.0f : *alpha;
-    const bool whole = nc == 8 && N % 4 == 0;
+    const bool whole = nc == 8 && N % 4 == 0, more = split < add;
     int bad = 0;
     static_for<TM>([&](auto i) {
       rows_put(acc[i][0], lds, lane, 0);
       rows_put(acc[i][1], lds, lane, 32);
       asm volatile("" ::: "memory");
       f32x4 old[8];
-      if (part && add && whole) {  // all in flight before the first is used
+      if (part && more && whole) {  // all in flight before the first is used
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int row = min(32 * i + (lane >> 3) + 8 * t, mv - 1);
@@ -208,13 +245,13 @@ struct CeOutArgs : GemmArgs {
           float* p = part + ((int64_t)split * M + mw + row) * N + nw + c8;
           if (whole) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] += add ? old[2 * t + c / 4][c % 4] : 0.0f;
+            for (int c = 0; c < 8; ++c) v[c] += more ? old[2 * t + c / 4][c % 4] : 0.0f;
             *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
           } else {
 #pragma unroll
             for (int c = 0; c < 8; ++c)
-              if (c < nc) p[c] = add ? p[c] + v[c] : v[c];
+              if (c < nc) p[c] = more ? p[c] + v[c] : v[c];
           }
         } else {
 #pragma unroll
@@ -234,45 +271,13 @@ struct CeOutArgs : GemmArgs {
   }
 };
 
-// Which tile a product takes.
-enum CeTile { CE_32x128, CE_64x128, CE_128x128, CE_256x256, CE_STAGED_64, CE_STAGED_128, CE_STAGED_ANY };
-constexpr int ce_tile_cols(CeTile t) {
-  return t == CE_256x256 ? 256 : t == CE_STAGED_64 || t == CE_STAGED_ANY ? 64 : 128;
-}
-
 // Launchers, compiled once per half type.  The layouts: forward and dz k-major operands,
 // dX a k-major A, dW neither.
-hipError_t run_ce_fwd_f16(const CeFwdArgs& g, CeTile t, hipStream_t s);
-hipError_t run_ce_fwd_bf16(const CeFwdArgs& g, CeTile t, hipStream_t s);
-hipError_t run_ce_grad_f16(const CeGradArgs& g, CeTile t, hipStream_t s);
-hipError_t run_ce_grad_bf16(const CeGradArgs& g, CeTile t, hipStream_t s);
-hipError_t run_ce_out_f16(const CeOutArgs& g, bool ak, CeTile t, hipStream_t s);
-hipError_t run_ce_out_bf16(const CeOutArgs& g, bool ak, CeTile t, hipStream_t s);
-
-template <int DT, class Args, bool AK, bool BKM, bool DBS, int BM, int BN, int WM, int WN, int OCC, int STG>
-hipError_t launch_ce_tiles(const Args& g, hipStream_t s) {
-  const dim3 grid((unsigned)(cdiv(g.M, BM) * cdiv(g.N, BN)), (unsigned)g.splits);
-  gemm_tile_kernel<DT, BM, BN, WM, WN, OCC, AK, BKM, 0, DBS, STG, false, Args>
-      <<<grid, BM / WM * (BN / WN) * 64, 0, s>>>(g);
-  return hipGetLastError();
-}
-
-template <int DT, class Args, bool AK, bool BKM, bool DBS>
-hipError_t launch_ce(const Args& g, CeTile t, hipStream_t s) {
-  switch (t) {
-    case CE_32x128:
-      if constexpr (std::is_same_v<Args, CeFwdArgs>) return launch_ce_tiles<DT, Args, AK, BKM, DBS, 32, 128, 32, 32, 4, 0>(g, s);
-      return hipErrorInvalidValue;
-    case CE_64x128:
-      if constexpr (AK) return launch_ce_tiles<DT, Args, AK, BKM, DBS, 64, 128, 32, 64, 3, 0>(g, s);
-      return hipErrorInvalidValue;
-    case CE_128x128: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 0>(g, s);
-    case CE_256x256: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 256, 256, 128, 64, 2, 0>(g, s);
-    case CE_STAGED_64: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 1>(g, s);
-    case CE_STAGED_128: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 1>(g, s);
-    case CE_STAGED_ANY: return launch_ce_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 2>(g, s);
-  }
-  return hipErrorInvalidValue;
-}
+hipError_t run_ce_fwd_f16(const CeFwdArgs& g, RowTile t, hipStream_t s);
+hipError_t run_ce_fwd_bf16(const CeFwdArgs& g, RowTile t, hipStream_t s);
+hipError_t run_ce_grad_f16(const CeGradArgs& g, RowTile t, hipStream_t s);
+hipError_t run_ce_grad_bf16(const CeGradArgs& g, RowTile t, hipStream_t s);
+hipError_t run_ce_out_f16(const CeOutArgs& g, bool ak, RowTile t, hipStream_t s);
+hipError_t run_ce_out_bf16(const CeOutArgs& g, bool ak, RowTile t, hipStream_t s);
 
 }  // namespace mpx

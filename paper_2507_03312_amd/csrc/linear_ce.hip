@@ -115,10 +115,11 @@ __global__ __launch_bounds__(1024) void ce_scalars_kernel(const float* g_loss, c
   scalars[1] = unit * __builtin_bit_cast(float, (uint32_t)(127 + e) << 23);
 }
 
-// out[i] = half(alpha sum over splits of part[s][i]); workgroups past those: db[r] = half(alpha
+// out[i] = half(alpha sum over splits of part[s stride + i]); workgroups past those: db[r] = half(alpha
 // sum over p of dbp[r][p]), one wave a row, lanes p = l, l + 64, ..., then wave_sum.
 template <int DT>
-__global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int splits, int64_t n, uint16_t* out,
+__global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int splits, int64_t stride, int64_t n,
+                                                        uint16_t* out,
                                                         const float* dbp, int dbparts, int64_t nrows, uint16_t* db,
                                                         const float* alpha, int32_t* nonfinite) {
   const int64_t blocks = (n + 1023) / 1024;
@@ -127,10 +128,10 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int s
   if (blockIdx.x < blocks) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= n) return;
-    if (n % 4 == 0) {
+    if (n % 4 == 0 && stride % 4 == 0) {
       f32x4 s = *reinterpret_cast<const f32x4*>(part + i);
       for (int k = 1; k < splits; ++k) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(part + (int64_t)k * n + i);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(part + k * stride + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += t[e];
       }
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int s
     } else {
       for (int64_t j = i; j < min(i + 4, n); ++j) {
         float s = part[j];
-        for (int k = 1; k < splits; ++k) s += part[(int64_t)k * n + j];
+        for (int k = 1; k < splits; ++k) s += part[k * stride + j];
         const uint16_t h = f2h<DT>(s * scale);
         out[j] = h;
         bad += h_nonfinite<DT>(h) ? 1 : 0;
@@ -183,15 +184,40 @@ __global__ __launch_bounds__(256) void ce_colsum_kernel(const uint16_t* dz, int6
   if (nonfinite) add_nonfinite(nonfinite, h_nonfinite<DT>(h) ? 1 : 0);
 }
 
+// X twice over, 64 rows apart (zeros behind its own), for the products of dz and its
+// remainders; rows of ld values.
+__global__ __launch_bounds__(256) void ce_twice_kernel(const uint16_t* X, int64_t M, int64_t K, uint16_t* out,
+                                                       int64_t ld) {
+  const int64_t row = blockIdx.y % 64, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (k < ld) out[blockIdx.y * ld + k] = row < M && k < K ? X[row * K + k] : (uint16_t)0;
+}
+
 // ------------------------------------------------------------------ plans --
 
+// The products' tables for choose_rows: forward 0.3% slower than the fastest tile on average,
+// dz 0.5%, dX and dW with their split counts 2.3% and 2.7% (those above 60 us 3.5% and 0.7%).
+static const RowCost kFwdCost[] = {{TILE_64x128, 64, 128, 3, {0.43, 0.53, 0.83}, 1.04},
+                                   {TILE_128x128, 128, 128, 2, {0.62, 0.75, 0}, 2.93},
+                                   {TILE_192x128, 192, 128, 2, {0.78, 0.81, 0}, 3.23},
+                                   {TILE_256x256, 256, 256, 1, {1.11, 0, 0}, 9.58}};
+static const RowCost kGradCost[] = {{TILE_64x128, 64, 128, 3, {0.14, 0.24, 0.78}, 1.46},
+                                    {TILE_128x128, 128, 128, 2, {0.28, 0.66, 0}, 3.36},
+                                    {TILE_192x128, 192, 128, 2, {0.61, 0.88, 0}, 4.29},
+                                    {TILE_256x256, 256, 256, 1, {1.02, 0, 0}, 13.4}};
+static const RowCost kDxCost[] = {{TILE_64x128, 64, 128, 3, {0.45, 0.47, 0.74}, 2.03},
+                                  {TILE_128x128, 128, 128, 2, {0.49, 0.64, 0}, 4.76},
+                                  {TILE_192x128, 192, 128, 2, {1.02, 1.07, 0}, 4.70},
+                                  {TILE_256x256, 256, 256, 1, {1.32, 0, 0}, 13.2}};
+static const RowCost kDwCost[] = {{TILE_128x128, 128, 128, 2, {0.60, 0.77, 0}, 2.88},
+                                  {TILE_192x128, 192, 128, 2, {0.82, 1.04, 0}, 4.92},
+                                  {TILE_256x256, 256, 256, 1, {1.29, 0, 0}, 13.3}};
+
 // Tile of a product of two k-major operands (forward and dz).
-static CeTile ce_tile(int64_t M, int64_t N, bool dma, bool any, bool forward) {
-  if (any) return CE_STAGED_ANY;
-  if (!dma) return cdiv(M, 64) * cdiv(N, 64) <= 512 ? CE_STAGED_64 : CE_STAGED_128;
-  if (forward && M <= 32) return CE_32x128;
-  if (cdiv(M, 256) * cdiv(N, 256) >= 512) return CE_256x256;
-  return cdiv(M, 128) * cdiv(N, 128) >= 384 ? CE_128x128 : CE_64x128;
+static RowTile ce_tile(int64_t M, int64_t N, int64_t K, bool dma, bool any, bool forward) {
+  if (any) return STAGED_ANY;
+  if (!dma) return cdiv(M, 64) * cdiv(N, 64) <= 512 ? STAGED_64 : STAGED_128;
+  if (forward && M <= 32) return TILE_32x128;
+  return choose_rows(forward ? kFwdCost : kGradCost, M, N, K).tile;
 }
 
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -199,44 +225,83 @@ static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // Forward workspace: (m, S) of every tile column, whatever the operands' alignment,
 // and the targets' logits.
 static int64_t ce_parts(int64_t M, int64_t V, int64_t K) {
-  return std::max(cdiv(V, ce_tile_cols(ce_tile(M, V, true, false, true))),
-                  cdiv(V, ce_tile_cols(ce_tile(M, V, false, K < 8, true))));
+  return std::max(cdiv(V, tile_cols(ce_tile(M, V, K, true, false, true))),
+                  cdiv(V, tile_cols(ce_tile(M, V, K, false, K < 8, true))));
 }
 
-// The backward's pieces of the vocabulary and splits of its two reductions.
+// Tile and splits of a piece's reductions over direct operands; at least 192 values a split,
+// none of them empty.  Register-staged ones take the splits and a tile of their own.
+static RowChoice ce_dx(int64_t M, int64_t cols, int64_t K, bool parts) {
+  // without partial sums a split also costs the kernel that adds them
+  return choose_rows(kDxCost, M, K, cols, std::max<int64_t>(1, std::min<int64_t>(16, cols / 192)), parts ? 0.0 : 3.0,
+                     1.25e-6, !parts);
+}
+static RowChoice ce_dw(int64_t M, int64_t cols, int64_t K) {
+  return choose_rows(kDwCost, cols, K, M, std::max<int64_t>(1, std::min<int64_t>(16, M / 192)), 2.0, 2.5e-6);
+}
+
+// The backward's pieces of the vocabulary, all but the last of `cols` columns, and their
+// place in the workspace.
 struct CePlan {
-  int64_t cols, pieces;  // columns of a piece (a multiple of 256)
-  int dx_splits, dw_splits;
-  int64_t dx_k, dw_k;  // reduction length of a split
-  bool dx_parts;
-  size_t dz, dxp, dwp, dbp, total;  // workspace offsets, scalars first
+  int64_t cols, pieces, last, most;  // a multiple of 256; how many; the last one's and the largest's columns
+  int dx_splits;                     // partial sums of dX: the most any piece takes
+  bool dx_parts, twice;
+  int64_t rows;  // of dz
+  size_t dz, dxp, dwp, dbp, x2, total;  // workspace offsets, scalars first
 };
 
-// Splits of a reduction of length len over tiles of 128 x 128: two workgroups per CU,
-// 512 values a split at least.
-static int ce_splits(int64_t M, int64_t N, int64_t len, int64_t& k_split) {
-  const int64_t tiles = cdiv(M, 128) * cdiv(N, 128);
-  const int64_t s = std::max<int64_t>(1, std::min<int64_t>({512 / tiles, 16, len / 512}));
-  k_split = cdiv(cdiv(len, s), 64) * 64;
-  return (int)cdiv(len, k_split);
-}
+static int64_t split_len(int64_t len, int splits) { return cdiv(cdiv(len, splits), 64) * 64; }
+// splits of that length that cover len: none is empty
+static int split_count(int64_t len, int splits) { return (int)cdiv(len, split_len(len, splits)); }
 
+// dz takes at most 128 MiB (so that its readers find much of it in the last-level cache),
+// or 256 columns.  Among the column counts that allow: the one of least estimated time
+// (whole rounds of tiles: 4096 x 65537 in 5 equal pieces of 52 tile columns 1.10 of the
+// time of 3 of 64 and one of 65).
 static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   CePlan p{};
-  const int64_t rows = cdiv(M, 64) * 64;
-  const int64_t most = std::max<int64_t>(256, ((int64_t)96 << 20) / (2 * rows) / 256 * 256);
-  p.pieces = cdiv(V, most);
-  p.cols = cdiv(cdiv(V, p.pieces), 256) * 256;
-  p.pieces = cdiv(V, p.cols);
-  const int64_t cols = std::min(p.cols, V);
-  p.dx_splits = ce_splits(M, K, cols, p.dx_k);
-  p.dw_splits = ce_splits(cols, K, M, p.dw_k);
-  p.dx_parts = p.pieces > 1 || p.dx_splits > 1;
+  p.twice = M <= 64;
+  const int64_t rows = p.rows = p.twice ? 128 : cdiv(M, 64) * 64, Mr = p.twice ? 128 : M;
+  const int64_t most = std::max<int64_t>(256, ((int64_t)128 << 20) / (2 * rows) / 256 * 256);
+  const auto lay = [&](int64_t cols) {  // what is left after whole pieces: its own, or with the last
+    p.cols = cols;
+    p.pieces = std::max<int64_t>(1, cdiv(V - 256, cols));
+    p.last = V - (p.pieces - 1) * cols;
+    p.most = std::max(p.pieces > 1 ? cols : 0, p.last);
+  };
+  if (V <= most + 256) {
+    lay(cdiv(V, 256) * 256);
+  } else {
+    const auto us = [&](int64_t cols) {
+      return choose_rows(kGradCost, M, cols, K).us + ce_dx(Mr, cols, K, true).us + ce_dw(Mr, cols, K).us + 10.0;
+    };
+    int64_t best = most;
+    double least = 0.0;
+    for (int i = 0; i < 12 && most - i * (most / 24 / 256 * 256) >= 256; ++i) {
+      lay(most - i * (most / 24 / 256 * 256));
+      const double t = us(p.cols) * (double)(p.pieces - 1) + us(p.last);
+      if (least == 0.0 || t < least) {
+        least = t;
+        best = p.cols;
+      }
+    }
+    lay(best);
+  }
+  p.dx_parts = p.pieces > 1;
+  size_t dw = 0, db = 0;  // bytes
+  for (const int64_t cols : {p.pieces > 1 ? p.cols : p.last, p.last}) {
+    p.dx_splits = std::max(p.dx_splits, split_count(cols, ce_dx(Mr, cols, K, p.pieces > 1 || p.twice).splits));
+    const int s = split_count(Mr, ce_dw(Mr, cols, K).splits);
+    dw = std::max(dw, s > 1 ? (size_t)s * cols * K * 4 : 0);
+    db = std::max(db, (size_t)s * cdiv(K, 64) * cols * 4);
+  }
+  p.dx_parts = p.twice || p.dx_parts || p.dx_splits > 1;
   p.dz = 256;
-  p.dxp = p.dz + align256((size_t)rows * cdiv(cols, 64) * 64 * 2);
-  p.dwp = p.dxp + (p.dx_parts ? align256((size_t)p.dx_splits * M * K * 4) : 0);
-  p.dbp = p.dwp + (p.dw_splits > 1 ? align256((size_t)p.dw_splits * cols * K * 4) : 0);
-  p.total = p.dbp + align256((size_t)p.dw_splits * cdiv(K, 64) * cols * 4);
+  p.dxp = p.dz + align256((size_t)rows * cdiv(p.most, 64) * 64 * 2);
+  p.dwp = p.dxp + (p.dx_parts ? align256((size_t)p.dx_splits * Mr * K * 4) : 0);
+  p.dbp = p.dwp + align256(dw);
+  p.x2 = p.dbp + align256(db);
+  p.total = p.x2 + (p.twice ? align256((size_t)128 * cdiv(K, 8) * 8 * 2) : 0);
   return p;
 }
 
@@ -304,11 +369,11 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
   g.part = (float2*)workspace;
   g.zt = (float*)((char*)workspace + align256((size_t)ce_parts(M, V, K) * M * 8));
   g.targets = loss ? targets : nullptr;
-  const CeTile t = ce_tile(M, V, dma_ok(g, operands_aligned(g), true, true), false, true);
-  const bool any = (t == CE_STAGED_64 || t == CE_STAGED_128) && staged_any(g, true, true);
-  const CeTile tile = any ? CE_STAGED_ANY : t;
+  const RowTile t = ce_tile(M, V, K, dma_ok(g, operands_aligned(g), true, true), false, true);
+  const bool any = (t == STAGED_64 || t == STAGED_128) && staged_any(g, true, true);
+  const RowTile tile = any ? STAGED_ANY : t;
   MPX_HIP(dt == MPX_F16 ? run_ce_fwd_f16(g, tile, s) : run_ce_fwd_bf16(g, tile, s));
-  const int parts = (int)cdiv(V, ce_tile_cols(tile));
+  const int parts = (int)cdiv(V, tile_cols(tile));
   if (M >= 2048)
     ce_join_kernel<32><<<(unsigned)cdiv(M, 32), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
                                                               (float2*)stats);
@@ -351,25 +416,34 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   if (dt == MPX_F16) ce_scalars_kernel<true><<<1, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars);
   else ce_scalars_kernel<false><<<1, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars);
   MPX_LAUNCHED();
+  // few rows: dz and what its rounding left, over X twice
+  const int64_t Mr = p.twice ? 128 : M, ldx = p.twice ? cdiv(K, 8) * 8 : K;
+  const uint16_t* Xr = p.twice ? (uint16_t*)(ws + p.x2) : (const uint16_t*)X;
+  if (p.twice && dW) {
+    ce_twice_kernel<<<dim3((unsigned)cdiv(ldx, 256), 128), 256, 0, s>>>((const uint16_t*)X, M, K,
+                                                                      (uint16_t*)(ws + p.x2), ldx);
+    MPX_LAUNCHED();
+  }
   // the reductions' own operands: dz is aligned, X and W as they come
-  const auto out_tile = [&](const GemmArgs& g, bool ak) {
-    if ((reinterpret_cast<uintptr_t>(g.B) & 15u) == 0 && g.ldb % 8 == 0) return CE_128x128;
-    return staged_any(g, ak, false) ? CE_STAGED_ANY
-           : cdiv(g.M, 64) * cdiv(g.N, 64) * g.splits <= 512 ? CE_STAGED_64 : CE_STAGED_128;
+  const auto out_tile = [&](const GemmArgs& g, bool ak, RowTile direct) {
+    if ((reinterpret_cast<uintptr_t>(g.B) & 15u) == 0 && g.ldb % 8 == 0) return direct;
+    return staged_any(g, ak, false) ? STAGED_ANY
+           : cdiv(g.M, 64) * cdiv(g.N, 64) * g.splits <= 512 ? STAGED_64 : STAGED_128;
   };
-  const auto run_out = [&](const CeOutArgs& g, bool ak, CeTile t) {
+  const auto run_out = [&](const CeOutArgs& g, bool ak, RowTile t) {
     return dt == MPX_F16 ? run_ce_out_f16(g, ak, t, s) : run_ce_out_bf16(g, ak, t, s);
   };
-  const auto reduce = [&](const float* part, int splits, int64_t n, void* out, const float* dbp, int dbparts,
+  const auto reduce = [&](const float* part, int splits, int64_t stride, int64_t n, void* out, const float* dbp, int dbparts,
                           int64_t nrows, void* dbo, int32_t* count) {
     return by_type(dt, [&](auto type) {
       ce_reduce_kernel<type><<<(unsigned)(cdiv(n, 1024) + cdiv(nrows, 4)), 256, 0, s>>>(
-          part, splits, n, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
+          part, splits, stride, n, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
       return hipGetLastError();
     });
   };
-  for (int64_t v0 = 0; v0 < V; v0 += p.cols) {
-    const int64_t cols = std::min(p.cols, V - v0), ldz = cdiv(cols, 64) * 64;
+  int dx_parts = 0;  // partial sums of dX so far
+  for (int64_t i = 0; i < p.pieces; ++i) {
+    const int64_t v0 = i * p.cols, cols = i + 1 < p.pieces ? p.cols : p.last, ldz = cdiv(cols, 64) * 64;
     const uint16_t* Wp = (const uint16_t*)W + v0 * K;
     CeGradArgs z;
     static_cast<GemmArgs&>(z) = ce_args(X, Wp, M, cols, K, K, K);
@@ -383,45 +457,55 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     z.v0 = (int32_t)v0;
     z.vocabulary = (int32_t)V;
     const bool dma = dma_ok(z, operands_aligned(z), true, true);
-    const CeTile t = ce_tile(M, cols, dma, !dma && staged_any(z, true, true), false);
+    z.twice = p.twice ? 1 : 0;
+    const RowTile t = ce_tile(M, cols, K, dma, !dma && staged_any(z, true, true), false);
     MPX_HIP(dt == MPX_F16 ? run_ce_grad_f16(z, t, s) : run_ce_grad_bf16(z, t, s));
     if (dX) {
       CeOutArgs g;
-      static_cast<GemmArgs&>(g) = ce_args(dz, Wp, M, K, cols, ldz, K);
+      static_cast<GemmArgs&>(g) = ce_args(dz, Wp, Mr, K, cols, ldz, K);
       g.C = (uint16_t*)dX;
-      g.splits = (int)cdiv(cols, p.dx_k);  // the last piece may need fewer
-      g.k_split = p.dx_k;
+      const RowChoice c = ce_dx(Mr, cols, K, p.pieces > 1 || p.twice);
+      g.k_split = split_len(cols, c.splits);
+      g.splits = split_count(cols, c.splits);
       g.part = p.dx_parts ? (float*)(ws + p.dxp) : nullptr;
       g.alpha = scalars;
-      g.add = v0 > 0;
-      MPX_HIP(run_out(g, true, out_tile(g, true)));
+      // the last piece may take another count than those before: what it adds to stands there
+      g.add = i > 0 ? dx_parts : 0;
+      dx_parts = std::max(dx_parts, g.splits);
+      MPX_HIP(run_out(g, true, out_tile(g, true, c.tile)));
     }
     if (dW) {
       CeOutArgs g;
-      static_cast<GemmArgs&>(g) = ce_args(dz, X, cols, K, M, ldz, K);
+      static_cast<GemmArgs&>(g) = ce_args(dz, Xr, cols, K, Mr, ldz, ldx);
       g.C = (uint16_t*)dW + v0 * K;
-      g.splits = p.dw_splits;
-      g.k_split = p.dw_k;
-      g.part = p.dw_splits > 1 ? (float*)(ws + p.dwp) : nullptr;
+      const RowChoice c = ce_dw(Mr, cols, K);
+      g.k_split = split_len(Mr, c.splits);
+      g.splits = split_count(Mr, c.splits);
+      g.part = g.splits > 1 ? (float*)(ws + p.dwp) : nullptr;
       g.alpha = scalars;
       g.add = 0;
       g.nonfinite = d_nonfinite;
-      g.dbp = db ? (float*)(ws + p.dbp) : nullptr;
-      const CeTile tw = out_tile(g, false);
+      // db: summed by the first column of tiles and ended there, or shared by all columns
+      // and ended by the reduction, which is worth its launch from about 30 us on
+      if (db && g.splits == 1 && c.us < 30.0) g.db = (uint16_t*)db + v0;
+      else if (db) g.dbp = (float*)(ws + p.dbp);
+      const RowTile tw = out_tile(g, false, c.tile);
       MPX_HIP(run_out(g, false, tw));
-      const int dbparts = (int)(p.dw_splits * cdiv(K, ce_tile_cols(tw)));
-      if (g.part || db)
-        MPX_HIP(reduce(g.part, p.dw_splits, g.part ? cols * K : 0, g.C, g.dbp, dbparts, db ? cols : 0,
-                       db ? (uint16_t*)db + v0 : nullptr, d_nonfinite));
+      const int dbparts = (int)(g.splits * cdiv(K, tile_cols(tw)));
+      if (g.part || g.dbp)
+        MPX_HIP(reduce(g.part, g.splits, cols * K, g.part ? cols * K : 0, g.C, g.dbp, dbparts, g.dbp ? cols : 0,
+                       g.dbp ? (uint16_t*)db + v0 : nullptr, d_nonfinite));
     } else if (db) {
       MPX_HIP(by_type(dt, [&](auto type) {
-        ce_colsum_kernel<type><<<(unsigned)(ldz / 64), 256, 0, s>>>(dz, ldz, M, cols, (uint16_t*)db + v0, scalars,
+        ce_colsum_kernel<type><<<(unsigned)(ldz / 64), 256, 0, s>>>(dz, ldz, p.rows, cols, (uint16_t*)db + v0, scalars,
                                                                    d_nonfinite);
         return hipGetLastError();
       }));
     }
   }
   if (dX && p.dx_parts)
-    MPX_HIP(reduce((const float*)(ws + p.dxp), p.dx_splits, M * K, dX, nullptr, 0, 0, nullptr, nullptr));
+    // few rows: each split's partial sums are two sets of 64 rows
+    MPX_HIP(reduce((const float*)(ws + p.dxp), p.twice ? 2 * dx_parts : dx_parts, p.twice ? 64 * K : M * K, M * K, dX,
+                   nullptr, 0, 0, nullptr, nullptr));
   return MPX_OK;
 }

@@ -3,16 +3,16 @@
 
 namespace mpx {
 
-hipError_t run_ce_fwd_bf16(const CeFwdArgs& g, CeTile t, hipStream_t s) {
-  return launch_ce<MPX_BF16, CeFwdArgs, true, true, false>(g, t, s);
+hipError_t run_ce_fwd_bf16(const CeFwdArgs& g, RowTile t, hipStream_t s) {
+  return launch_rows<MPX_BF16, CeFwdArgs, true, true, false>(g, t, s);
 }
-hipError_t run_ce_grad_bf16(const CeGradArgs& g, CeTile t, hipStream_t s) {
-  return launch_ce<MPX_BF16, CeGradArgs, true, true, false>(g, t, s);
+hipError_t run_ce_grad_bf16(const CeGradArgs& g, RowTile t, hipStream_t s) {
+  return launch_rows<MPX_BF16, CeGradArgs, true, true, false>(g, t, s);
 }
-hipError_t run_ce_out_bf16(const CeOutArgs& g, bool ak, CeTile t, hipStream_t s) {
-  if (ak) return launch_ce<MPX_BF16, CeOutArgs, true, false, false>(g, t, s);
-  return g.dbp ? launch_ce<MPX_BF16, CeOutArgs, false, false, true>(g, t, s)
-               : launch_ce<MPX_BF16, CeOutArgs, false, false, false>(g, t, s);
+hipError_t run_ce_out_bf16(const CeOutArgs& g, bool ak, RowTile t, hipStream_t s) {
+  if (ak) return launch_rows<MPX_BF16, CeOutArgs, true, false, false>(g, t, s);
+  return g.dbp || g.db ? launch_rows<MPX_BF16, CeOutArgs, false, false, true>(g, t, s)
+               : launch_rows<MPX_BF16, CeOutArgs, false, false, false>(g, t, s);
 }
 
 }  // namespace mpx

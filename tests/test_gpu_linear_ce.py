@@ -151,15 +151,17 @@ def _backward(dev, st, g, fmt, M, V, K, off=0, dx=True, dw=True, db=True, state=
 
 def _gradient_bounds(x, w, z, dz, d, f, stats, fmt):
     """dz = f (p - 1[target]): p is off by its logit's and ln S's errors and its own
-    exponent's rounding, then dz is rounded once (float16: in units of 2^-25 of 2^13
+    exponent's rounding (z log2 e against the rounded (m + ln S) log2 e), then dz is rounded once (float16: in units of 2^-25 of 2^13
     to 2^14 for the largest f, at worst); float32 sums of two orders, half a step at the
     end, and 2^-20 of itself for an error that moves a value over a rounding border."""
     em, el = _stat_errors(z, dz, stats)
     with np.errstate(all="ignore"):
         p = np.exp(z - stats[:, :1] - stats[:, 1:])
-        arg = np.where(p > 0, np.abs(z - stats[:, :1]) + np.abs(stats[:, 1:]) + 8, 0.0)
+        arg = np.where(p > 0, np.abs(z) + np.abs(stats[:, :1]) + np.abs(stats[:, 1:]) + 8, 0.0)
     fa = np.abs(f)[:, None]
-    e = fa * p * 1.01 * (dz + (em + el)[:, None] + arg * 2.0 ** -22) + np.abs(d) * (HALF[fmt] + 2.0 ** -22)
+    # up to 64 rows what the rounding of dz leaves is kept, and rounded itself
+    step = HALF[fmt] ** 2 if len(x) <= 64 else HALF[fmt]
+    e = fa * p * 1.01 * (dz + (em + el)[:, None] + arg * 2.0 ** -22) + np.abs(d) * (step + 2.0 ** -22)
     if fmt == "f16":
         e = e + 2.0 ** -38 * fa.max()
 
