@@ -181,14 +181,14 @@ hipError_t run_gated_bwd_bf16(const GemmArgs& g, RowTile t, hipStream_t s);
 
 template <int DT, int ACT>
 hipError_t run_gated_fwd(const GemmArgs& g, int64_t pair, RowTile t, hipStream_t s) {
-  GatedArgs<ACT> a;
+  GatedArgs<ACT> a{};
   static_cast<GemmArgs&>(a) = g;
   a.pair = pair;
   return launch_rows<DT, GatedArgs<ACT>, true, true, false>(a, t, s);
 }
 template <int DT, int ACT>
 hipError_t run_gated_bwd(const GemmArgs& g, RowTile t, hipStream_t s) {
-  GatedBwdArgs<ACT> a;
+  GatedBwdArgs<ACT> a{};
   static_cast<GemmArgs&>(a) = g;
   return launch_rows<DT, GatedBwdArgs<ACT>, true, false, false>(a, t, s);
 }

@@ -134,7 +134,7 @@ inline RowChoice choose_rows(const RowCost (&costs)[N], int64_t M, int64_t cols,
   RowChoice best{costs[0].tile, 1, 0.0};
   for (const RowCost& c : costs) {
     const int64_t tiles = cdiv(M, c.bm) * cdiv(cols, c.bn), slots = 256 * c.per_cu;
-    for (int64_t s = 1; s <= most; ++s) {
+    for (int64_t s = 1; s <= most; s += s < 6 ? 1 : s < 16 ? 2 : s / 4) {
       const double nk = (double)cdiv(len, 64 * s);
       auto round = [&](int64_t o) { return o ? nk * c.k_us[o - 1] + c.tile_us * (double)o : 0.0; };
       const double t = (double)(tiles * s / slots) * round(c.per_cu) + round(cdiv(tiles * s % slots, 256)) +

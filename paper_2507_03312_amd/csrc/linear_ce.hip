@@ -79,11 +79,20 @@ __global__ __launch_bounds__(1024) void ce_mean_kernel(const float* loss, const 
   if (threadIdx.x == 0) *mean = n ? s / (float)n : 0.0f;
 }
 
-// The backward's scalars: c (see linear_ce.h) from the largest |scale g|, and
-// without g_loss the number of rows with a target.  C16: float16.
+// The backward's scalars, by workgroup 0: c (see linear_ce.h) from the largest |scale g|, and
+// without g_loss the number of rows with a target.  C16: float16.  The workgroups behind it
+// copy a row each of X twice over, 64 rows apart (zeros behind its own), for the products of
+// dz and its remainders; rows of ld values.
 template <bool C16>
-__global__ __launch_bounds__(1024) void ce_scalars_kernel(const float* g_loss, const int32_t* targets, int64_t M,
-                                                          const mpx_scale_state* state, float* scalars) {
+__global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, const int32_t* targets, int64_t M,
+                                                          const mpx_scale_state* state, float* scalars,
+                                                          const uint16_t* X, int64_t K, uint16_t* twice, int64_t ld) {
+  if (blockIdx.x > 0) {
+    const int64_t at = blockIdx.x - 1, row = at % 64;
+    for (int64_t k = threadIdx.x; k < ld; k += 1024)
+      twice[at * ld + k] = row < M && k < K ? X[row * K + k] : (uint16_t)0;
+    return;
+  }
   __shared__ float most[1024];
   __shared__ int counts[1024];
   const float scale = state ? state->scale : 1.0f;
@@ -115,42 +124,35 @@ __global__ __launch_bounds__(1024) void ce_scalars_kernel(const float* g_loss, c
   scalars[1] = unit * __builtin_bit_cast(float, (uint32_t)(127 + e) << 23);
 }
 
-// out[i] = half(alpha sum over splits of part[s stride + i]); workgroups past those: db[r] = half(alpha
-// sum over p of dbp[r][p]), one wave a row, lanes p = l, l + 64, ..., then wave_sum.
-template <int DT>
+// out[i] = half(alpha sum over splits of part[s stride + i]), VEC: 4 a thread (n, stride and
+// part allow 16 bytes); workgroups past those: db[r] = half(alpha sum over p of dbp[r][p]),
+// one wave a row, lanes p = l, l + 64, ..., then wave_sum.
+template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int splits, int64_t stride, int64_t n,
-                                                        uint16_t* out,
-                                                        const float* dbp, int dbparts, int64_t nrows, uint16_t* db,
-                                                        const float* alpha, int32_t* nonfinite) {
-  const int64_t blocks = (n + 1023) / 1024;
+                                                        uint16_t* out, const float* dbp, int dbparts, int64_t nrows,
+                                                        uint16_t* db, const float* alpha, int32_t* nonfinite) {
+  constexpr int PER = VEC ? 4 : 1;
+  const int64_t blocks = (n + 256 * PER - 1) / (256 * PER);
   const float scale = *alpha;
   int bad = 0;
   if (blockIdx.x < blocks) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * PER;
     if (i >= n) return;
-    if (n % 4 == 0 && stride % 4 == 0) {
-      f32x4 s = *reinterpret_cast<const f32x4*>(part + i);
-      for (int k = 1; k < splits; ++k) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(part + k * stride + i);
+    float s[PER] = {};
+#pragma unroll 8
+    for (int k = 0; k < splits; ++k) {
+      float t[PER];
+      __builtin_memcpy(t, part + k * stride + i, sizeof(t));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += t[e];
-      }
-      uint16_t h[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        h[e] = f2h<DT>(s[e] * scale);
-        bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
-      }
-      __builtin_memcpy(out + i, h, 8);
-    } else {
-      for (int64_t j = i; j < min(i + 4, n); ++j) {
-        float s = part[j];
-        for (int k = 1; k < splits; ++k) s += part[k * stride + j];
-        const uint16_t h = f2h<DT>(s * scale);
-        out[j] = h;
-        bad += h_nonfinite<DT>(h) ? 1 : 0;
-      }
+      for (int e = 0; e < PER; ++e) s[e] += t[e];
     }
+    uint16_t h[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      h[e] = f2h<DT>(s[e] * scale);
+      bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
+    }
+    __builtin_memcpy(out + i, h, sizeof(h));
   } else {
     const int64_t row = ((int64_t)blockIdx.x - blocks) * 4 + (threadIdx.x >> 6);
     if (row >= nrows) return;  // uniform over the wave
@@ -182,14 +184,6 @@ __global__ __launch_bounds__(256) void ce_colsum_kernel(const uint16_t* dz, int6
   const uint16_t h = f2h<DT>((lds[0][lane] + lds[1][lane] + lds[2][lane] + lds[3][lane]) * *alpha);
   db[c] = h;
   if (nonfinite) add_nonfinite(nonfinite, h_nonfinite<DT>(h) ? 1 : 0);
-}
-
-// X twice over, 64 rows apart (zeros behind its own), for the products of dz and its
-// remainders; rows of ld values.
-__global__ __launch_bounds__(256) void ce_twice_kernel(const uint16_t* X, int64_t M, int64_t K, uint16_t* out,
-                                                       int64_t ld) {
-  const int64_t row = blockIdx.y % 64, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (k < ld) out[blockIdx.y * ld + k] = row < M && k < K ? X[row * K + k] : (uint16_t)0;
 }
 
 // ------------------------------------------------------------------ plans --
@@ -233,11 +227,11 @@ static int64_t ce_parts(int64_t M, int64_t V, int64_t K) {
 // none of them empty.  Register-staged ones take the splits and a tile of their own.
 static RowChoice ce_dx(int64_t M, int64_t cols, int64_t K, bool parts) {
   // without partial sums a split also costs the kernel that adds them
-  return choose_rows(kDxCost, M, K, cols, std::max<int64_t>(1, std::min<int64_t>(16, cols / 192)), parts ? 0.0 : 3.0,
+  return choose_rows(kDxCost, M, K, cols, std::max<int64_t>(1, std::min<int64_t>(64, cols / 192)), parts ? 0.0 : 3.0,
                      1.25e-6, !parts);
 }
 static RowChoice ce_dw(int64_t M, int64_t cols, int64_t K) {
-  return choose_rows(kDwCost, cols, K, M, std::max<int64_t>(1, std::min<int64_t>(16, M / 192)), 2.0, 2.5e-6);
+  return choose_rows(kDwCost, cols, K, M, std::max<int64_t>(1, std::min<int64_t>(64, M / 192)), 2.0, 2.5e-6);
 }
 
 // The backward's pieces of the vocabulary, all but the last of `cols` columns, and their
@@ -363,7 +357,7 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
     return MPX_ERR_WORKSPACE;
   }
   hipStream_t s = (hipStream_t)stream;
-  CeFwdArgs g;
+  CeFwdArgs g{};
   static_cast<GemmArgs&>(g) = ce_args(X, W, M, V, K, K, K);
   g.bias = (const uint16_t*)b;
   g.part = (float2*)workspace;
@@ -413,17 +407,16 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   char* ws = (char*)workspace;
   float* scalars = (float*)ws;
   uint16_t* dz = (uint16_t*)(ws + p.dz);
-  if (dt == MPX_F16) ce_scalars_kernel<true><<<1, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars);
-  else ce_scalars_kernel<false><<<1, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars);
-  MPX_LAUNCHED();
   // few rows: dz and what its rounding left, over X twice
   const int64_t Mr = p.twice ? 128 : M, ldx = p.twice ? cdiv(K, 8) * 8 : K;
-  const uint16_t* Xr = p.twice ? (uint16_t*)(ws + p.x2) : (const uint16_t*)X;
-  if (p.twice && dW) {
-    ce_twice_kernel<<<dim3((unsigned)cdiv(ldx, 256), 128), 256, 0, s>>>((const uint16_t*)X, M, K,
-                                                                      (uint16_t*)(ws + p.x2), ldx);
-    MPX_LAUNCHED();
-  }
+  uint16_t* X2 = (uint16_t*)(ws + p.x2);
+  const uint16_t* Xr = p.twice ? X2 : (const uint16_t*)X;
+  const unsigned grid = p.twice && dW ? 129 : 1;
+  if (dt == MPX_F16)
+    ce_prepare_kernel<true><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X, K, X2, ldx);
+  else
+    ce_prepare_kernel<false><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X, K, X2, ldx);
+  MPX_LAUNCHED();
   // the reductions' own operands: dz is aligned, X and W as they come
   const auto out_tile = [&](const GemmArgs& g, bool ak, RowTile direct) {
     if ((reinterpret_cast<uintptr_t>(g.B) & 15u) == 0 && g.ldb % 8 == 0) return direct;
@@ -436,16 +429,20 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   const auto reduce = [&](const float* part, int splits, int64_t stride, int64_t n, void* out, const float* dbp, int dbparts,
                           int64_t nrows, void* dbo, int32_t* count) {
     return by_type(dt, [&](auto type) {
-      ce_reduce_kernel<type><<<(unsigned)(cdiv(n, 1024) + cdiv(nrows, 4)), 256, 0, s>>>(
-          part, splits, stride, n, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
-      return hipGetLastError();
+      const auto launch = [&](auto kernel, int64_t per) {
+        kernel<<<(unsigned)(cdiv(n, 256 * per) + cdiv(nrows, 4)), 256, 0, s>>>(
+            part, splits, stride, n, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
+        return hipGetLastError();
+      };
+      return n % 4 == 0 && stride % 4 == 0 ? launch(ce_reduce_kernel<type, true>, 4)
+                                           : launch(ce_reduce_kernel<type, false>, 1);
     });
   };
   int dx_parts = 0;  // partial sums of dX so far
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t v0 = i * p.cols, cols = i + 1 < p.pieces ? p.cols : p.last, ldz = cdiv(cols, 64) * 64;
     const uint16_t* Wp = (const uint16_t*)W + v0 * K;
-    CeGradArgs z;
+    CeGradArgs z{};
     static_cast<GemmArgs&>(z) = ce_args(X, Wp, M, cols, K, K, K);
     z.bias = b ? (const uint16_t*)b + v0 : nullptr;
     z.C = dz;
@@ -461,7 +458,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     const RowTile t = ce_tile(M, cols, K, dma, !dma && staged_any(z, true, true), false);
     MPX_HIP(dt == MPX_F16 ? run_ce_grad_f16(z, t, s) : run_ce_grad_bf16(z, t, s));
     if (dX) {
-      CeOutArgs g;
+      CeOutArgs g{};
       static_cast<GemmArgs&>(g) = ce_args(dz, Wp, Mr, K, cols, ldz, K);
       g.C = (uint16_t*)dX;
       const RowChoice c = ce_dx(Mr, cols, K, p.pieces > 1 || p.twice);
@@ -475,7 +472,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       MPX_HIP(run_out(g, true, out_tile(g, true, c.tile)));
     }
     if (dW) {
-      CeOutArgs g;
+      CeOutArgs g{};
       static_cast<GemmArgs&>(g) = ce_args(dz, Xr, cols, K, Mr, ldz, ldx);
       g.C = (uint16_t*)dW + v0 * K;
       const RowChoice c = ce_dw(Mr, cols, K);

@@ -81,20 +81,32 @@ struct QkRun {
   }
 };
 
-// The values' partners, and those of a gain in registers.
-template <int VW, bool INTER>
-__device__ __forceinline__ void partners(const float (&x)[VW], int lane, float (&o)[VW]) {
+// A thread's run of both gains (ones where there is none).
+template <int DT, int VW>
+struct QkGains {
+  RopeVec<DT, VW> w[2];
+  __device__ __forceinline__ void load(const QkArgs& a, int v0) {
+    typedef typename RopeValue<DT>::type T;
 #pragma unroll
-  for (int i = 0; i < VW; ++i) {
-    if constexpr (INTER) o[i] = x[i ^ 1];
-    else o[i] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * lane, __builtin_bit_cast(int, x[i])));
+    for (int p = 0; p < 2; ++p) {
+      const T* g = (const T*)(p ? a.wk : a.wq);
+      if (g) {
+        w[p].load(g + v0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) w[p].set(i, 1.0f);
+      }
+    }
   }
-}
+  __device__ __forceinline__ float get(bool key, int i) const { return key ? w[1].get(i) : w[0].get(i); }
+};
 
 // Bound by HBM: every value is read and written once.  As rope_kernel: a row's turns once
 // into LDS, a thread keeps one run of VW values of every head it takes, U heads in
-// flight; the lanes of a head lie in one wave and share its sum of squares.
-template <int DT, int VW, bool INTER>
+// flight; the lanes of a head lie in one wave and share its sum of squares.  Queries, keys
+// and (in runs of 16 bytes) the copied heads are one list, so that few heads of a kind
+// leave no thread without one (a loop for each kind: 12608 rows of 3 x 12 heads of 64 bf16 31.5 us).
+template <int DT, int VW, bool INTER, bool NT>
 __global__ __launch_bounds__(256) void qknorm_rope_kernel(QkArgs a) {
   typedef typename RopeValue<DT>::type T;
   __shared__ float2 turns[kRopeTable];
@@ -102,78 +114,83 @@ __global__ __launch_bounds__(256) void qknorm_rope_kernel(QkArgs a) {
   const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
   T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
   const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
-  rope_copies<DT>(a, X, a.ldx, Y, nrows);
-  rope_turns(a, row0, nrows, turns);
-
+  constexpr bool kWide = VW * sizeof(T) == 16;
   const int lane = threadIdx.x & 63;
   const uint32_t chunk = lane % a.chunks, wave_slots = 64 / a.chunks;
   const uint32_t slot = (threadIdx.x >> 6) * wave_slots + lane / a.chunks;
   const uint32_t r = slot / a.head_slots, h0 = slot % a.head_slots;
-  if ((uint32_t)lane >= wave_slots * a.chunks || r >= nrows) return;  // all lanes of a head or none
+  const uint32_t heads = a.heads_rot + (kWide && !a.in_place ? a.copy / a.hd : 0);
+  const bool mine = (uint32_t)lane < wave_slots * a.chunks && r < nrows;  // all lanes of a head or none
+  const T* x = X + r * a.ldx + chunk * VW;
+  T* y = Y + r * a.ldy + chunk * VW;
+  // the first heads' values in flight while the turns are made
+  constexpr int U = 4;
+  RopeVec<DT, VW> v[U];
+  auto load = [&](uint32_t h) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u].template load<NT>(x + (int64_t)min(h + u * a.head_slots, heads - 1) * a.hd);
+  };
+  if (mine) load(h0);
+  if constexpr (!kWide) rope_copies<DT>(a, X, a.ldx, Y, nrows);
+  rope_turns(a, row0, nrows, turns);
+  if (!mine) return;
   QkRun<VW, INTER> run;
   run.init(a, chunk, lane);
   float c[VW], s[VW];
   run.factors(turns + r * a.npairs, c, s);
-  const T* x = X + r * a.ldx + run.v0;
-  T* y = Y + r * a.ldy + run.v0;
+  QkGains<DT, VW> own, other;
+  own.load(a, run.v0);
+  if constexpr (!INTER) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) other.w[p] = own.w[p].from_lane(run.partner);
+  }
   const float over = 1.0f / (float)a.hd;
-  constexpr int U = 4;
-  for (int part = 0; part < 2; ++part) {  // queries, keys
-    const uint32_t lo = part ? a.hq : 0, hi = part ? a.heads_rot : a.hq;
-    float wc[VW], ws[VW];  // the gains times the turn
-    {
-      RopeVec<DT, VW> w;
-      float f[VW], o[VW];
-      const T* g = (const T*)(part ? a.wk : a.wq);
-      if (g) w.load(g + run.v0);
+  for (uint32_t h = h0; h < heads; h += U * a.head_slots) {
+    float ss[U];
+    if (h != h0) load(h);
 #pragma unroll
-      for (int i = 0; i < VW; ++i) f[i] = g ? w.get(i) : 1.0f;
-      partners<VW, INTER>(f, run.partner, o);
+    for (int u = 0; u < U; ++u) {
+      ss[u] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < VW; ++i) {
-        wc[i] = f[i] * c[i];
-        ws[i] = o[i] * s[i];
-      }
+      for (int i = 0; i < VW; ++i) ss[u] = __builtin_fmaf(v[u].get(i), v[u].get(i), ss[u]);
     }
-    for (uint32_t h = lo + h0; h < hi; h += U * a.head_slots) {
-      RopeVec<DT, VW> v[U];
-      float ss[U];
+    head_sum<U>(ss, a.chunks, lane);
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u].load(x + (int64_t)min(h + u * a.head_slots, hi - 1) * a.hd);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        ss[u] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < VW; ++i) ss[u] = __builtin_fmaf(v[u].get(i), v[u].get(i), ss[u]);
-      }
-      head_sum<U>(ss, a.chunks, lane);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        RopeVec<DT, VW> o;
-        if constexpr (!INTER) o = v[u].from_lane(run.partner);
-        if (h + u * a.head_slots >= hi) break;
+    for (int u = 0; u < U; ++u) {
+      const uint32_t at = h + u * a.head_slots;
+      if (at >= heads) break;
+      RopeVec<DT, VW> o;
+      if constexpr (!INTER) o = v[u].from_lane(run.partner);
+      if (!kWide || at < a.heads_rot) {
+        const bool key = at >= a.hq;
         const float inv = rsqrtf(__builtin_fmaf(ss[u], over, a.eps));
-        RopeVec<DT, VW> n;
+        float n[VW];
 #pragma unroll
         for (int i = 0; i < VW; ++i) {
-          const float other = INTER ? v[u].get(i ^ 1) : o.get(i);
-          // values that are not turned keep clear of their neighbours
-          n.set(i, inv * (run.turned ? __builtin_fmaf(v[u].get(i), wc[i], other * ws[i]) : v[u].get(i) * wc[i]));
+          n[i] = v[u].get(i) * own.get(key, i) * c[i];
+          if (run.turned) {  // values that are not turned keep clear of their neighbours
+            if constexpr (INTER) n[i] = __builtin_fmaf(v[u].get(i ^ 1) * own.get(key, i ^ 1), s[i], n[i]);
+            else n[i] = __builtin_fmaf(o.get(i) * other.get(key, i), s[i], n[i]);
+          }
         }
-        n.store(y + (int64_t)(h + u * a.head_slots) * a.hd);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) v[u].set(i, inv * n[i]);
       }
+      v[u].template store<NT>(y + (int64_t)at * a.hd);
     }
   }
 }
 
-// Backward, likewise, over a grid that strides over the rows: a thread adds up dw for its own
-// run of values, a workgroup its threads' sums in order, and qk_gains_kernel the
-// workgroups'.
-template <int DT, int VW, bool INTER>
-__global__ __launch_bounds__(256) void qknorm_rope_bwd_kernel(QkArgs a) {
+// Backward, likewise, over a grid that strides over the rows.  A thread's sums of dw for its
+// run of values stand in LDS (their 16 registers serve the loads in flight); a workgroup
+// adds up its threads' in order, and qk_gains_kernel the workgroups'.
+template <int DT, int VW, bool INTER, bool NT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4)))
+void qknorm_rope_bwd_kernel(QkArgs a) {
   typedef typename RopeValue<DT>::type T;
   __shared__ float2 turns[kRopeTable];
-  __shared__ float sums[256 * VW];
+  __shared__ float sums[2][256 * VW];
+  constexpr bool kWide = VW * sizeof(T) == 16;
   const int lane = threadIdx.x & 63;
   const uint32_t chunk = lane % a.chunks, wave_slots = 64 / a.chunks;
   const uint32_t slot = (threadIdx.x >> 6) * wave_slots + lane / a.chunks;
@@ -181,110 +198,97 @@ __global__ __launch_bounds__(256) void qknorm_rope_bwd_kernel(QkArgs a) {
   const bool whole = (uint32_t)lane < wave_slots * a.chunks;
   QkRun<VW, INTER> run;
   run.init(a, chunk, lane);
+  float* own = &sums[0][slot * a.hd + run.v0];
+  QkGains<DT, VW> w;
+  if (whole) {
+    w.load(a, run.v0);
+#pragma unroll
+    for (int i = 0; i < VW; ++i) own[i] = own[256 * VW + i] = 0.0f;
+  }
   const float over = 1.0f / (float)a.hd;
-  float dw[2][VW] = {};
+  const uint32_t heads = a.heads_rot + (kWide && !a.in_place ? a.copy / a.hd : 0);
   for (uint32_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
     const uint32_t row0 = tile * a.wg_rows;
     const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
     const T* D = (const T*)a.dY + (int64_t)row0 * a.ldy_in;
     T* Y = (T*)a.Y + (int64_t)row0 * a.ldy;
     const uint32_t nrows = min((uint32_t)a.wg_rows, a.rows - row0);
-    __syncthreads();  // the last tile's turns have been read
-    rope_copies<DT>(a, D, a.ldy_in, Y, nrows);
-    rope_turns(a, row0, nrows, turns);
-    if (!whole || r >= nrows) continue;
-    float c[VW], s[VW];
-    run.factors(turns + r * a.npairs, c, s);
+    const bool mine = whole && r < nrows;
     const T* x = X + r * a.ldx + run.v0;
     const T* d = D + r * a.ldy_in + run.v0;
     T* y = Y + r * a.ldy + run.v0;
-    constexpr int U = 2;
+    // a head's values in flight while the one before is worked on, the first ones
+    // while the turns are made
+    RopeVec<DT, VW> nv, ng;
+    auto load = [&](uint32_t h) {
+      nv.template load<NT>(x + (int64_t)min(h, a.heads_rot - 1) * a.hd);  // X has no copied heads
+      ng.template load<NT>(d + (int64_t)min(h, heads - 1) * a.hd);
+    };
+    if (mine) load(h0);
+    __syncthreads();  // the last tile's turns have been read
+    if constexpr (!kWide) rope_copies<DT>(a, D, a.ldy_in, Y, nrows);
+    rope_turns(a, row0, nrows, turns);
+    if (!mine) continue;
+    float c[VW], s[VW];
+    run.factors(turns + r * a.npairs, c, s);
+    for (uint32_t h = h0; h < heads; h += a.head_slots) {
+      const RopeVec<DT, VW> v = nv, g = ng;
+      load(h + a.head_slots);
+      const bool key = h >= a.hq;
+      RopeVec<DT, VW> o;
+      if constexpr (!INTER) o = g.from_lane(run.partner);
+      float sum[2] = {0.0f, 0.0f}, dn[VW];
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      const uint32_t lo = part ? a.hq : 0, hi = part ? a.heads_rot : a.hq;
-      float w[VW];
-      {
-        RopeVec<DT, VW> g;
-        const T* p = (const T*)(part ? a.wk : a.wq);
-        if (p) g.load(p + run.v0);
-#pragma unroll
-        for (int i = 0; i < VW; ++i) w[i] = p ? g.get(i) : 1.0f;
+      for (int i = 0; i < VW; ++i) {
+        const float other = INTER ? g.get(i ^ 1) : o.get(i);
+        dn[i] = run.turned ? __builtin_fmaf(g.get(i), c[i], other * s[i]) : g.get(i);
+        sum[0] = __builtin_fmaf(v.get(i), v.get(i), sum[0]);
+        sum[1] = __builtin_fmaf(w.get(key, i) * dn[i], v.get(i), sum[1]);
       }
-      for (uint32_t h = lo + h0; h < hi; h += U * a.head_slots) {
-        RopeVec<DT, VW> v[U], g[U];
-        float sum[2 * U], dn[U][VW];
+      head_sum<2>(sum, a.chunks, lane);
+      RopeVec<DT, VW> out = g;
+      if (!kWide || h < a.heads_rot) {
+        const float inv = rsqrtf(__builtin_fmaf(sum[0], over, a.eps));
+        const float k = inv * inv * (sum[1] * over);
+        float* add = own + (key ? 256 * VW : 0);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int64_t at = (int64_t)min(h + u * a.head_slots, hi - 1) * a.hd;
-          v[u].load(x + at);
-          g[u].load(d + at);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          RopeVec<DT, VW> o;
-          if constexpr (!INTER) o = g[u].from_lane(run.partner);
-          sum[2 * u] = sum[2 * u + 1] = 0.0f;
-#pragma unroll
-          for (int i = 0; i < VW; ++i) {
-            const float other = INTER ? g[u].get(i ^ 1) : o.get(i);
-            dn[u][i] = run.turned ? __builtin_fmaf(g[u].get(i), c[i], other * s[i]) : g[u].get(i);
-            sum[2 * u] = __builtin_fmaf(v[u].get(i), v[u].get(i), sum[2 * u]);
-            sum[2 * u + 1] = __builtin_fmaf(w[i] * dn[u][i], v[u].get(i), sum[2 * u + 1]);
-          }
-        }
-        head_sum<2 * U>(sum, a.chunks, lane);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (h + u * a.head_slots >= hi) break;
-          const float inv = rsqrtf(__builtin_fmaf(sum[2 * u], over, a.eps));
-          const float k = inv * inv * (sum[2 * u + 1] * over);
-          RopeVec<DT, VW> n;
-#pragma unroll
-          for (int i = 0; i < VW; ++i) {
-            const float xi = v[u].get(i);
-            dw[part][i] = __builtin_fmaf(dn[u][i], xi * inv, dw[part][i]);
-            n.set(i, inv * __builtin_fmaf(-xi, k, w[i] * dn[u][i]));
-          }
-          n.store(y + (int64_t)(h + u * a.head_slots) * a.hd);
+        for (int i = 0; i < VW; ++i) {
+          const float xi = v.get(i);
+          add[i] = __builtin_fmaf(dn[i], xi * inv, add[i]);
+          out.set(i, inv * __builtin_fmaf(-xi, k, w.get(key, i) * dn[i]));
         }
       }
+      out.template store<NT>(y + (int64_t)h * a.hd);
     }
   }
   // the workgroup's sums: its slots in order
-#pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    __syncthreads();
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < VW; ++i) sums[slot * a.hd + run.v0 + i] = dw[part][i];
-    }
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.hd; j += 256) {
-      float t = 0.0f;
-      for (uint32_t k = 0; k < 4 * wave_slots; ++k) t += sums[k * a.hd + j];
-      a.part[((int64_t)blockIdx.x * 2 + part) * a.hd + j] = t;
-    }
+  __syncthreads();
+  for (int j = threadIdx.x; j < 2 * a.hd; j += 256) {
+    const int part = j >= a.hd ? 1 : 0, col = j - part * a.hd;
+    float t = 0.0f;
+    for (uint32_t k = 0; k < 4 * wave_slots; ++k) t += sums[part][k * a.hd + col];
+    a.part[(int64_t)blockIdx.x * 2 * a.hd + j] = t;
   }
 }
 
 // Heads whose sections allow no such runs: a wave takes a head at a time, lane l the values
 // l, l + 64, ..., their partners straight from memory (the same lines).
-constexpr int kQkPer = kRopeMaxHd / 64;
-template <int DT, bool BACK>
+// PER: values of a lane.
+template <int DT, bool BACK, int PER>
 __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
   typedef typename RopeValue<DT>::type T;
   __shared__ float2 turns[kRopeTable];
-  __shared__ float sums[4][kRopeMaxHd];
+  __shared__ float sums[4][64 * PER];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float over = 1.0f / (float)a.hd;
   auto get = [](T v) { if constexpr (DT == MPX_F32) return v; else return h2f<DT>(v); };
   auto put = [](float v) { if constexpr (DT == MPX_F32) return v; else return f2h<DT>(v); };
   // the lane's values' pairs (-1: not turned) and partners
-  int pair[kQkPer], other[kQkPer];
-  bool second[kQkPer];
-  float dw[2][kQkPer];
+  int pair[PER], other[PER];
+  bool second[PER];
+  float dw[2][PER];
 #pragma unroll
-  for (int i = 0; i < kQkPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int j = lane + 64 * i;
     pair[i] = -1;
     other[i] = j;
@@ -326,9 +330,9 @@ __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
       T* y = Y + r * a.ldy + (int64_t)h * a.hd;
       const int part = h >= a.hq ? 1 : 0;
       const T* g = (const T*)(part ? a.wk : a.wq);
-      float xv[kQkPer], own[kQkPer], oth[kQkPer], ss = 0.0f, sp = 0.0f;
+      float xv[PER], own[PER], oth[PER], ss = 0.0f, sp = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kQkPer; ++i) {
+      for (int i = 0; i < PER; ++i) {
         const int j = lane + 64 * i;
         const bool in = j < a.hd;
         xv[i] = in ? get(x[j]) : 0.0f;
@@ -352,7 +356,7 @@ __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
       const float inv = rsqrtf(__builtin_fmaf(wave_sum(ss), over, a.eps));
       const float k = BACK ? inv * inv * (wave_sum(sp) * over) : 0.0f;
 #pragma unroll
-      for (int i = 0; i < kQkPer; ++i) {
+      for (int i = 0; i < PER; ++i) {
         const int j = lane + 64 * i;
         if (j >= a.hd) continue;
         if (BACK) {
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
     for (int part = 0; part < 2; ++part) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kQkPer; ++i) sums[wave][lane + 64 * i] = dw[part][i];
+      for (int i = 0; i < PER; ++i) sums[wave][lane + 64 * i] = dw[part][i];
       __syncthreads();
       for (int j = threadIdx.x; j < a.hd; j += 256)
         a.part[((int64_t)blockIdx.x * 2 + part) * a.hd + j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
@@ -408,15 +412,35 @@ __global__ __launch_bounds__(1024) void qk_gains_kernel(const float* part, int p
 
 constexpr int64_t kQkWorkgroups = 1024;  // of the backward
 
+template <int DT, int VW, bool INTER, bool NT>
+static void launch_qk_kernel(const QkArgs& a, bool back, unsigned blocks, hipStream_t s) {
+  if (back) qknorm_rope_bwd_kernel<DT, VW, INTER, NT><<<blocks, 256, 0, s>>>(a);
+  else qknorm_rope_kernel<DT, VW, INTER, NT><<<blocks, 256, 0, s>>>(a);
+}
 template <int DT, int VW>
 static void launch_qk(const QkArgs& a, bool back, unsigned blocks, hipStream_t s) {
-  if (back) {
-    if (a.interleaved) qknorm_rope_bwd_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
-    else qknorm_rope_bwd_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
-  } else {
-    if (a.interleaved) qknorm_rope_kernel<DT, VW, true><<<blocks, 256, 0, s>>>(a);
-    else qknorm_rope_kernel<DT, VW, false><<<blocks, 256, 0, s>>>(a);
+  if constexpr (VW * sizeof(typename RopeValue<DT>::type) == 16) {
+    if (a.stream) {
+      if (a.interleaved) launch_qk_kernel<DT, VW, true, true>(a, back, blocks, s);
+      else launch_qk_kernel<DT, VW, false, true>(a, back, blocks, s);
+      return;
+    }
   }
+  if (a.interleaved) launch_qk_kernel<DT, VW, true, false>(a, back, blocks, s);
+  else launch_qk_kernel<DT, VW, false, false>(a, back, blocks, s);
+}
+
+template <int DT, int PER>
+static void launch_qk_any(const QkArgs& a, bool back, unsigned blocks, hipStream_t s) {
+  if (back) qknorm_rope_any_kernel<DT, true, PER><<<blocks, 256, 0, s>>>(a);
+  else qknorm_rope_any_kernel<DT, false, PER><<<blocks, 256, 0, s>>>(a);
+}
+template <int DT>
+static void launch_qk_any(const QkArgs& a, bool back, unsigned blocks, hipStream_t s) {
+  if (a.hd <= 64) launch_qk_any<DT, 1>(a, back, blocks, s);
+  else if (a.hd <= 128) launch_qk_any<DT, 2>(a, back, blocks, s);
+  else if (a.hd <= 256) launch_qk_any<DT, 4>(a, back, blocks, s);
+  else launch_qk_any<DT, 8>(a, back, blocks, s);
 }
 
 static int64_t qk_workgroups(int64_t rows) { return std::min(rows, kQkWorkgroups); }
@@ -488,21 +512,22 @@ static int qknorm_rope(const char* fn, const void* X, int64_t ldx, const void* d
   a.part = (float*)workspace;
   a.eps = (float)eps;
   hipStream_t s = (hipStream_t)stream;
+  // past the last-level cache, around it
+  const double bytes = (double)rows * ((double)width * (in == Y ? 1.0 : 2.0) + (back ? (double)(heads_q + heads_k) * hd : 0.0)) *
+                       (dt == MPX_F32 ? 4.0 : 2.0);
+  a.stream = bytes > 256.0 * (1 << 20) ? 1 : 0;
   const bool any = vw == 1 || hd / vw > 64;
   a.chunks = any ? 64 : (int32_t)(hd / vw);
   const int64_t slots = any ? 4 : 4 * (64 / a.chunks);
-  int64_t wg_rows = std::min<int64_t>({4 * slots / a.heads_rot, slots, kRopeTable / a.npairs, rows / 1024});
+  const int64_t listed = a.heads_rot + (!any && !a.in_place && vw * (dt == MPX_F32 ? 4 : 2) == 16 ? heads_copy : 0);
+  int64_t wg_rows = std::min<int64_t>({8 * slots / listed, slots, kRopeTable / a.npairs, rows / 1024});
   wg_rows = std::max<int64_t>(wg_rows, 1);
   a.wg_rows = (int32_t)wg_rows;
   a.head_slots = (int32_t)(slots / wg_rows);
   a.tiles = (uint32_t)cdiv(rows, wg_rows);
   const unsigned blocks = (unsigned)(back ? std::min<int64_t>(a.tiles, workgroups) : a.tiles);
 #define MPX_QK(DTv, VWv) launch_qk<DTv, VWv>(a, back, blocks, s)
-#define MPX_QK_ANY(DTv)                                                        \
-  do {                                                                         \
-    if (back) qknorm_rope_any_kernel<DTv, true><<<blocks, 256, 0, s>>>(a);     \
-    else qknorm_rope_any_kernel<DTv, false><<<blocks, 256, 0, s>>>(a);         \
-  } while (0)
+#define MPX_QK_ANY(DTv) launch_qk_any<DTv>(a, back, blocks, s)
   if (dt == MPX_F32) {
     if (any) MPX_QK_ANY(MPX_F32);
     else if (vw == 4) MPX_QK(MPX_F32, 4);
