@@ -125,11 +125,11 @@ __global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, c
 }
 
 // out[i] = half(alpha sum over splits of part[s stride + i]), VEC: 4 a thread (n, stride and
-// part allow 16 bytes); workgroups past those: db[r] = half(alpha sum over p of dbp[r][p]),
+// part allow 16 bytes); rows of `width` sums, of which `cols` are kept; workgroups past those: db[r] = half(alpha sum over p of dbp[r][p]),
 // one wave a row, lanes p = l, l + 64, ..., then wave_sum.
 template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int splits, int64_t stride, int64_t n,
-                                                        uint16_t* out, const float* dbp, int dbparts, int64_t nrows,
+                                                        int32_t width, int32_t cols, uint16_t* out, const float* dbp, int dbparts, int64_t nrows,
                                                         uint16_t* db, const float* alpha, int32_t* nonfinite) {
   constexpr int PER = VEC ? 4 : 1;
   const int64_t blocks = (n + 256 * PER - 1) / (256 * PER);
@@ -148,11 +148,22 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int s
     }
     uint16_t h[PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      h[e] = f2h<DT>(s[e] * scale);
-      bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
+    for (int e = 0; e < PER; ++e) h[e] = f2h<DT>(s[e] * scale);
+    if (width == cols) {  // uniform
+#pragma unroll
+      for (int e = 0; e < PER; ++e) bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
+      __builtin_memcpy(out + i, h, sizeof(h));
+    } else {
+      const int64_t row = i / width;
+      const int c = (int)(i - row * width);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        if (c + e < cols) {
+          out[row * cols + c + e] = h[e];
+          bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
+        }
+      }
     }
-    __builtin_memcpy(out + i, h, sizeof(h));
   } else {
     const int64_t row = ((int64_t)blockIdx.x - blocks) * 4 + (threadIdx.x >> 6);
     if (row >= nrows) return;  // uniform over the wave
@@ -184,6 +195,17 @@ __global__ __launch_bounds__(256) void ce_colsum_kernel(const uint16_t* dz, int6
   const uint16_t h = f2h<DT>((lds[0][lane] + lds[1][lane] + lds[2][lane] + lds[3][lane]) * *alpha);
   db[c] = h;
   if (nonfinite) add_nonfinite(nonfinite, h_nonfinite<DT>(h) ? 1 : 0);
+}
+
+// Rows of X [M, K] and then of W [V, K] with zeros behind them, up to ld values (a multiple
+// of 8), 16-byte aligned: 8 values a thread.
+__global__ __launch_bounds__(256) void ce_pad_kernel(const uint16_t* X, int64_t M, const uint16_t* W, int64_t V,
+                                                     int64_t K, uint16_t* out, int64_t ld) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = ld / 8;
+  const int64_t row = i / chunks, k = (i - row * chunks) * 8;
+  if (row >= M + V) return;
+  const uint16_t* p = (row < M ? X + row * K : W + (row - M) * K) + k;
+  *reinterpret_cast<u32x4*>(out + row * ld + k) = load8(p, (int)max((int64_t)-8, min((int64_t)8, K - k)));
 }
 
 // ------------------------------------------------------------------ plans --
@@ -234,6 +256,15 @@ static RowChoice ce_dw(int64_t M, int64_t cols, int64_t K) {
   return choose_rows(kDwCost, cols, K, M, std::max<int64_t>(1, std::min<int64_t>(64, M / 192)), 2.0, 2.5e-6);
 }
 
+// Operands whose reduction is no multiple of 64 go to the direct tiles as padded copies
+// where these cost less than register staging (bf16, us, staged / padded): forward
+// from 1024 rows on (700 x 50000 x 700 86 / 92, 1500 x 50000 x 700 157 / 148, 4000 x 20000 x 300 104 /
+// 81) but for few columns (1500 x 1000 x 100 12.4 / 13.7), with gradient from 256 on (300 x 50000
+// x 700 248 / 224, 4000 x 50000 x 700 1867 / 1371; 100 x 50000 x 700 142 / 166).
+static int64_t ce_padded(int64_t K) { return cdiv(K, 64) * 64; }
+static bool ce_pads_fwd(int64_t M, int64_t V, int64_t K) { return K % 64 != 0 && M >= 1024 && V >= 4096; }
+static bool ce_pads_bwd(int64_t M, int64_t K) { return K % 64 != 0 && M >= 256; }
+
 // The backward's pieces of the vocabulary, all but the last of `cols` columns, and their
 // place in the workspace.
 struct CePlan {
@@ -241,7 +272,8 @@ struct CePlan {
   int dx_splits;                     // partial sums of dX: the most any piece takes
   bool dx_parts, twice;
   int64_t rows;  // of dz
-  size_t dz, dxp, dwp, dbp, x2, total;  // workspace offsets, scalars first
+  int64_t width;  // of dX's and dW's partial sums: K, or of padded operands a multiple of 4
+  size_t dz, dxp, dwp, dbp, x2, total;  // workspace offsets, scalars first; x2: other forms of X (and W)
 };
 
 static int64_t split_len(int64_t len, int splits) { return cdiv(cdiv(len, splits), 64) * 64; }
@@ -255,6 +287,7 @@ static int split_count(int64_t len, int splits) { return (int)cdiv(len, split_le
 static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   CePlan p{};
   p.twice = M <= 64;
+  p.width = ce_pads_bwd(M, K) ? cdiv(K, 4) * 4 : K;
   const int64_t rows = p.rows = p.twice ? 128 : cdiv(M, 64) * 64, Mr = p.twice ? 128 : M;
   const int64_t most = std::max<int64_t>(256, ((int64_t)128 << 20) / (2 * rows) / 256 * 256);
   const auto lay = [&](int64_t cols) {  // what is left after whole pieces: its own, or with the last
@@ -286,16 +319,17 @@ static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   for (const int64_t cols : {p.pieces > 1 ? p.cols : p.last, p.last}) {
     p.dx_splits = std::max(p.dx_splits, split_count(cols, ce_dx(Mr, cols, K, p.pieces > 1 || p.twice).splits));
     const int s = split_count(Mr, ce_dw(Mr, cols, K).splits);
-    dw = std::max(dw, s > 1 ? (size_t)s * cols * K * 4 : 0);
+    dw = std::max(dw, s > 1 ? (size_t)s * cols * p.width * 4 : 0);
     db = std::max(db, (size_t)s * cdiv(K, 64) * cols * 4);
   }
   p.dx_parts = p.twice || p.dx_parts || p.dx_splits > 1;
   p.dz = 256;
   p.dxp = p.dz + align256((size_t)rows * cdiv(p.most, 64) * 64 * 2);
-  p.dwp = p.dxp + (p.dx_parts ? align256((size_t)p.dx_splits * Mr * K * 4) : 0);
+  p.dwp = p.dxp + (p.dx_parts ? align256((size_t)p.dx_splits * Mr * p.width * 4) : 0);
   p.dbp = p.dwp + align256(dw);
   p.x2 = p.dbp + align256(db);
-  p.total = p.x2 + (p.twice ? align256((size_t)128 * cdiv(K, 8) * 8 * 2) : 0);
+  p.total = p.x2 + (p.twice ? align256((size_t)128 * cdiv(K, 8) * 8 * 2) : 0) +
+            (ce_pads_bwd(M, K) ? align256((size_t)(M + V) * ce_padded(K) * 2) : 0);
   return p;
 }
 
@@ -309,6 +343,18 @@ static GemmArgs ce_args(const void* A, const void* B, int64_t M, int64_t N, int6
   g.M = M; g.N = N; g.K = K;
   g.lda = lda; g.ldb = ldb;
   return g;
+}
+
+// Padded copies of both operands at `out`, and the product g on them.
+static hipError_t ce_pad(const void* X, int64_t M, const void* W, int64_t V, int64_t K, uint16_t* out, GemmArgs& g,
+                         hipStream_t s) {
+  const int64_t ld = ce_padded(K);
+  ce_pad_kernel<<<(unsigned)cdiv((M + V) * (ld / 8), 256), 256, 0, s>>>((const uint16_t*)X, M, (const uint16_t*)W, V,
+                                                                        K, out, ld);
+  g.A = out;
+  g.B = out + M * ld;
+  g.K = g.lda = g.ldb = ld;
+  return hipGetLastError();
 }
 
 static bool ce_misaligned(const void* p, int n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
@@ -338,7 +384,8 @@ using namespace mpx;
 
 extern "C" size_t mpx_linear_ce_fwd_workspace(int64_t M, int64_t V, int64_t K) {
   if (M < 1 || V < 1 || K < 1) return 0;
-  return align256((size_t)ce_parts(M, V, K) * M * 8) + align256((size_t)M * 4);
+  return align256((size_t)ce_parts(M, V, K) * M * 8) + align256((size_t)M * 4) +
+         (ce_pads_fwd(M, V, K) ? align256((size_t)(M + V) * ce_padded(K) * 2) : 0);
 }
 
 extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, const int32_t* targets, int64_t M,
@@ -363,7 +410,8 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
   g.part = (float2*)workspace;
   g.zt = (float*)((char*)workspace + align256((size_t)ce_parts(M, V, K) * M * 8));
   g.targets = loss ? targets : nullptr;
-  const RowTile t = ce_tile(M, V, K, dma_ok(g, operands_aligned(g), true, true), false, true);
+  if (ce_pads_fwd(M, V, K)) MPX_HIP(ce_pad(X, M, W, V, K, (uint16_t*)(g.zt + align256((size_t)M * 4) / 4), g, s));
+  const RowTile t = ce_tile(M, V, g.K, dma_ok(g, operands_aligned(g), true, true), false, true);
   const bool any = (t == STAGED_64 || t == STAGED_128) && staged_any(g, true, true);
   const RowTile tile = any ? STAGED_ANY : t;
   MPX_HIP(dt == MPX_F16 ? run_ce_fwd_f16(g, tile, s) : run_ce_fwd_bf16(g, tile, s));
@@ -408,9 +456,12 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   float* scalars = (float*)ws;
   uint16_t* dz = (uint16_t*)(ws + p.dz);
   // few rows: dz and what its rounding left, over X twice
-  const int64_t Mr = p.twice ? 128 : M, ldx = p.twice ? cdiv(K, 8) * 8 : K;
+  const int64_t Mr = p.twice ? 128 : M;
   uint16_t* X2 = (uint16_t*)(ws + p.x2);
-  const uint16_t* Xr = p.twice ? X2 : (const uint16_t*)X;
+  GemmArgs both = ce_args(X, W, M, V, K, K, K);  // X, W, or their padded copies
+  if (ce_pads_bwd(M, K)) MPX_HIP(ce_pad(X, M, W, V, K, X2, both, s));
+  const uint16_t* Xr = p.twice ? X2 : both.A;
+  const int64_t ldx = p.twice ? cdiv(K, 8) * 8 : both.ldb;
   const unsigned grid = p.twice && dW ? 129 : 1;
   if (dt == MPX_F16)
     ce_prepare_kernel<true><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X, K, X2, ldx);
@@ -431,7 +482,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     return by_type(dt, [&](auto type) {
       const auto launch = [&](auto kernel, int64_t per) {
         kernel<<<(unsigned)(cdiv(n, 256 * per) + cdiv(nrows, 4)), 256, 0, s>>>(
-            part, splits, stride, n, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
+            part, splits, stride, n, (int32_t)p.width, (int32_t)K, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
         return hipGetLastError();
       };
       return n % 4 == 0 && stride % 4 == 0 ? launch(ce_reduce_kernel<type, true>, 4)
@@ -441,9 +492,9 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   int dx_parts = 0;  // partial sums of dX so far
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t v0 = i * p.cols, cols = i + 1 < p.pieces ? p.cols : p.last, ldz = cdiv(cols, 64) * 64;
-    const uint16_t* Wp = (const uint16_t*)W + v0 * K;
+    const uint16_t* Wp = both.B + v0 * both.ldb;
     CeGradArgs z{};
-    static_cast<GemmArgs&>(z) = ce_args(X, Wp, M, cols, K, K, K);
+    static_cast<GemmArgs&>(z) = ce_args(both.A, Wp, M, cols, both.K, both.lda, both.ldb);
     z.bias = b ? (const uint16_t*)b + v0 : nullptr;
     z.C = dz;
     z.ldc = ldz;
@@ -459,7 +510,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     MPX_HIP(dt == MPX_F16 ? run_ce_grad_f16(z, t, s) : run_ce_grad_bf16(z, t, s));
     if (dX) {
       CeOutArgs g{};
-      static_cast<GemmArgs&>(g) = ce_args(dz, Wp, Mr, K, cols, ldz, K);
+      static_cast<GemmArgs&>(g) = ce_args(dz, Wp, Mr, p.dx_parts ? p.width : K, cols, ldz, both.ldb);
       g.C = (uint16_t*)dX;
       const RowChoice c = ce_dx(Mr, cols, K, p.pieces > 1 || p.twice);
       g.k_split = split_len(cols, c.splits);
@@ -479,6 +530,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       g.k_split = split_len(Mr, c.splits);
       g.splits = split_count(Mr, c.splits);
       g.part = g.splits > 1 ? (float*)(ws + p.dwp) : nullptr;
+      if (g.part) g.N = p.width;
       g.alpha = scalars;
       g.add = 0;
       g.nonfinite = d_nonfinite;
@@ -490,7 +542,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       MPX_HIP(run_out(g, false, tw));
       const int dbparts = (int)(g.splits * cdiv(K, tile_cols(tw)));
       if (g.part || g.dbp)
-        MPX_HIP(reduce(g.part, g.splits, cols * K, g.part ? cols * K : 0, g.C, g.dbp, dbparts, g.dbp ? cols : 0,
+        MPX_HIP(reduce(g.part, g.splits, cols * p.width, g.part ? cols * p.width : 0, g.C, g.dbp, dbparts, g.dbp ? cols : 0,
                        g.dbp ? (uint16_t*)db + v0 : nullptr, d_nonfinite));
     } else if (db) {
       MPX_HIP(by_type(dt, [&](auto type) {
@@ -502,7 +554,8 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   }
   if (dX && p.dx_parts)
     // few rows: each split's partial sums are two sets of 64 rows
-    MPX_HIP(reduce((const float*)(ws + p.dxp), p.twice ? 2 * dx_parts : dx_parts, p.twice ? 64 * K : M * K, M * K, dX,
+    MPX_HIP(reduce((const float*)(ws + p.dxp), p.twice ? 2 * dx_parts : dx_parts,
+                   (p.twice ? 64 : M) * p.width, M * p.width, dX,
                    nullptr, 0, 0, nullptr, nullptr));
   return MPX_OK;
 }

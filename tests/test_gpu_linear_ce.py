@@ -106,7 +106,8 @@ def _forward(x, w, b, t, fmt, off=0, loss=True, stats=True, mean=True):
 # one and few rows; every direct tile; ragged edges; register-staged; rows of < 8
 SHAPES = [(1, 1, 1), (1, 10, 64), (2, 1000, 64), (8, 4099, 128), (32, 300, 192), (33, 129, 64), (3, 7, 5),
           (65, 40, 7), (64, 257, 100), (130, 1003, 320), (300, 515, 72), (520, 2050, 64), (1030, 6500, 64),
-          (2100, 16500, 64), (2050, 70, 64), (700, 3001, 75)]
+          (2100, 16500, 64), (2050, 70, 64), (700, 3001, 75),
+          (1100, 4130, 70), (1027, 4099, 200), (256, 64, 1)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
