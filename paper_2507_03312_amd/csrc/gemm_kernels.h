@@ -779,7 +779,7 @@ __device__ __forceinline__ float frag_sum8(const uint4& f) {
 // elements apart; N, n0 and nw count columns of one).  With kRagged the reduction of a
 // product with an mn-major B may end inside a k tile: A has zeros behind it, up to the
 // tile's end, and B's last k row is read again there.  The sums of DBS go to dbp, or
-// without splits, where db is set, times db_scale() to db.
+// without splits, where db is set, ended by db_end() to db.
 template <class Args, int BM, int BN, int WM, int WN>
 constexpr int own_epilogue_bytes() {
   if constexpr (std::is_same_v<Args, GemmArgs>) return 0;
@@ -1032,7 +1032,7 @@ void gemm_tile_kernel(Args g) {
             g.dbp[row * ((int64_t)g.splits * db_cols) + (int64_t)split * db_cols + db_col] = v;
           } else {
             uint16_t h;
-            if constexpr (kOwn) h = f2h<DT>(v * g.db_scale());
+            if constexpr (kOwn) h = f2h<DT>(g.db_end(v, row));
             else h = f2h<DT>(v);
             g.db[row] = h;
             bad += h_nonfinite<DT>(h) ? 1 : 0;

@@ -102,10 +102,11 @@ struct CeFwdArgs : GemmArgs {
 // Backward, dz of a piece: the same product, C = dz [M rounded up to 64][ldc], with
 // zeros in rows behind M and columns behind N (up to ldc), as the products that reduce
 // over them need.  A masked logit (-inf) has no gradient, but in a row that is NaN.
-// twice (up to 64 rows): row 64 + r holds what rounding row r to half left, and the
-// products take both.  Few rows have few large dz (their targets'), whose roundings do
-// not average out: 4 rows of 170 columns bf16 3.3e-3 of dX's norm against 1.8e-3 for one
-// rounding of the result, while the second rows cost nothing beside the reading of W.
+// twice (few rows): row twice + r holds what rounding row r to half left, and the products
+// take both.  Few rows have few large dz (their targets'), whose roundings do not average
+// out: 4 rows of 170 columns bf16 3.3e-3 of dX's norm against 1.8e-3 for one rounding of
+// the result, while the second rows cost little beside the reading of W.  rest (nullable):
+// the same of the rows' targets alone, for db, whose sums of few rows cancel.
 struct CeGradArgs : GemmArgs {
   static constexpr bool kPair = false, kRagged = false, kNarrow = false;
   static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kHalfBytes; }
@@ -115,6 +116,7 @@ struct CeGradArgs : GemmArgs {
   const int32_t* targets;
   int32_t v0, vocabulary;  // the piece's first column, and the columns of all
   int32_t twice;
+  float* rest;  // [M]
   template <int TM>
   struct Rows {
     float2 stats[TM];
@@ -157,7 +159,7 @@ struct CeGradArgs : GemmArgs {
       const float c = row >= M ? -__builtin_inff()
                       : st.x == -__builtin_inff() ? 0.0f : -__builtin_fmaf(st.x, kLog2e, st.y * kLog2e);
       const bool plain = nv == 64 && !__ballot(t >= 0 && t < 64);  // uniform: no target, no edge
-      for (int low = 0; low <= twice; ++low) {
+      for (int low = 0; low <= (twice ? 1 : 0); ++low) {
         asm volatile("" ::: "memory");  // the wave's reads of the block before come first
         static_for<2>([&](auto j) {
 #pragma unroll
@@ -175,6 +177,7 @@ struct CeGradArgs : GemmArgs {
                 p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, c));
                 p[k] = f * (p[k] - (col == t && z != -__builtin_inff() ? 1.0f : 0.0f));
                 p[k] = col < nv ? p[k] : 0.0f;
+                if (rest && col == t && row < M) rest[row] = p[k] - h2f<DT>(f2h<DT>(p[k]));
               }
             }
             if (low) {
@@ -190,7 +193,7 @@ struct CeGradArgs : GemmArgs {
           const int r = (lane >> 3) + 8 * t4;
           const u32x4 w = *reinterpret_cast<const u32x4*>(lds + r * kHalfPitch + 8 * (lane & 7));
           if (mw + 32 * i + r < rows64)
-            *reinterpret_cast<u32x4*>(C + (mw + 32 * i + r + 64 * low) * ldc + nw + 8 * (lane & 7)) = w;
+            *reinterpret_cast<u32x4*>(C + (mw + 32 * i + r + (low ? twice : 0)) * ldc + nw + 8 * (lane & 7)) = w;
         }
       }
     });
@@ -205,7 +208,7 @@ struct CeOutArgs : GemmArgs {
   float* part;         // [splits][M][N]
   const float* alpha;  // 1 / c
   int32_t add;
-  __device__ __forceinline__ float db_scale() const { return *alpha; }
+  __device__ __forceinline__ float db_end(float sum, int64_t) const { return sum * *alpha; }
   template <int DT, int TM, int STG>
   __device__ __forceinline__ NoPrefetch prefetch(int64_t, int64_t, int) const { return {}; }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>

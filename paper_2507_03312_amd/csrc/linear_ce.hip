@@ -81,14 +81,14 @@ __global__ __launch_bounds__(1024) void ce_mean_kernel(const float* loss, const 
 
 // The backward's scalars, by workgroup 0: c (see linear_ce.h) from the largest |scale g|, and
 // without g_loss the number of rows with a target.  C16: float16.  The workgroups behind it
-// copy a row each of X twice over, 64 rows apart (zeros behind its own), for the products of
+// copy a row each of X twice over (zeros behind its own, half the grid apart), for the products of
 // dz and its remainders; rows of ld values.
 template <bool C16>
 __global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, const int32_t* targets, int64_t M,
                                                           const mpx_scale_state* state, float* scalars,
                                                           const uint16_t* X, int64_t K, uint16_t* twice, int64_t ld) {
   if (blockIdx.x > 0) {
-    const int64_t at = blockIdx.x - 1, row = at % 64;
+    const int64_t at = blockIdx.x - 1, row = at % ((gridDim.x - 1) / 2);
     for (int64_t k = threadIdx.x; k < ld; k += 1024)
       twice[at * ld + k] = row < M && k < K ? X[row * K + k] : (uint16_t)0;
     return;
@@ -130,7 +130,9 @@ __global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, c
 template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int splits, int64_t stride, int64_t n,
                                                         int32_t width, int32_t cols, uint16_t* out, const float* dbp, int dbparts, int64_t nrows,
-                                                        uint16_t* db, const float* alpha, int32_t* nonfinite) {
+                                                        uint16_t* db, const float* alpha, int32_t* nonfinite,
+                                                        const float* rest, const int32_t* targets, int32_t rows,
+                                                        int32_t v0) {
   constexpr int PER = VEC ? 4 : 1;
   const int64_t blocks = (n + 256 * PER - 1) / (256 * PER);
   const float scale = *alpha;
@@ -170,6 +172,9 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int s
     const int lane = threadIdx.x & 63;
     float s = 0.0f;
     for (int k = lane; k < dbparts; k += 64) s += dbp[row * dbparts + k];
+    if (rest) {  // what rounding left of the targets that are this column
+      for (int r = lane; r < rows; r += 64) s += targets[r] == v0 + row ? rest[r] : 0.0f;
+    }
     s = wave_sum(s);
     if (lane == 0) {
       const uint16_t h = f2h<DT>(s * scale);
@@ -180,21 +185,16 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int s
   if (nonfinite) add_nonfinite(nonfinite, bad);
 }
 
-// db of a piece where dW is not asked for: four groups of rows a workgroup, 64 columns.
+// db of a piece where dW is not asked for: partial sums dbp[column][4] for the reduction,
+// four groups of rows a workgroup, 64 columns.
 template <int DT>
 __global__ __launch_bounds__(256) void ce_colsum_kernel(const uint16_t* dz, int64_t ld, int64_t M, int64_t cols,
-                                                        uint16_t* db, const float* alpha, int32_t* nonfinite) {
-  __shared__ float lds[4][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;  // < ld, a multiple of 64
+                                                        float* dbp) {
+  const int g = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);  // < ld, a multiple of 64
   float s = 0.0f;
   for (int64_t m = g; m < M; m += 4) s += h2f<DT>(dz[m * ld + c]);
-  lds[g][lane] = s;
-  __syncthreads();
-  if (g != 0 || c >= cols) return;
-  const uint16_t h = f2h<DT>((lds[0][lane] + lds[1][lane] + lds[2][lane] + lds[3][lane]) * *alpha);
-  db[c] = h;
-  if (nonfinite) add_nonfinite(nonfinite, h_nonfinite<DT>(h) ? 1 : 0);
+  if (c < cols) dbp[c * 4 + g] = s;
 }
 
 // Rows of X [M, K] and then of W [V, K] with zeros behind them, up to ld values (a multiple
@@ -270,10 +270,10 @@ static bool ce_pads_bwd(int64_t M, int64_t K) { return K % 64 != 0 && M >= 256; 
 struct CePlan {
   int64_t cols, pieces, last, most;  // a multiple of 256; how many; the last one's and the largest's columns
   int dx_splits;                     // partial sums of dX: the most any piece takes
-  bool dx_parts, twice;
-  int64_t rows;  // of dz
+  bool dx_parts, rest;
+  int64_t twice, rows;  // rows between dz and what its rounding left (0: not kept), of all
   int64_t width;  // of dX's and dW's partial sums: K, or of padded operands a multiple of 4
-  size_t dz, dxp, dwp, dbp, x2, total;  // workspace offsets, scalars first; x2: other forms of X (and W)
+  size_t lo, dz, dxp, dwp, dbp, x2, total;  // workspace offsets, scalars first; x2: other forms of X (and W)
 };
 
 static int64_t split_len(int64_t len, int splits) { return cdiv(cdiv(len, splits), 64) * 64; }
@@ -286,9 +286,12 @@ static int split_count(int64_t len, int splits) { return (int)cdiv(len, split_le
 // time of 3 of 64 and one of 65).
 static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   CePlan p{};
-  p.twice = M <= 64;
+  // up to 128 rows dX's norm would lose up to a factor of 1.8 to the rounding of dz, with
+  // 256 1.45; db's, of few columns, of up to a thousand rows 2
+  p.twice = M <= 64 ? 64 : M <= 128 ? 128 : 0;
+  p.rest = !p.twice && M * V <= ((int64_t)1 << 22);
   p.width = ce_pads_bwd(M, K) ? cdiv(K, 4) * 4 : K;
-  const int64_t rows = p.rows = p.twice ? 128 : cdiv(M, 64) * 64, Mr = p.twice ? 128 : M;
+  const int64_t rows = p.rows = p.twice ? 2 * p.twice : cdiv(M, 64) * 64, Mr = p.twice ? p.rows : M;
   const int64_t most = std::max<int64_t>(256, ((int64_t)128 << 20) / (2 * rows) / 256 * 256);
   const auto lay = [&](int64_t cols) {  // what is left after whole pieces: its own, or with the last
     p.cols = cols;
@@ -317,18 +320,19 @@ static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   p.dx_parts = p.pieces > 1;
   size_t dw = 0, db = 0;  // bytes
   for (const int64_t cols : {p.pieces > 1 ? p.cols : p.last, p.last}) {
-    p.dx_splits = std::max(p.dx_splits, split_count(cols, ce_dx(Mr, cols, K, p.pieces > 1 || p.twice).splits));
+    p.dx_splits = std::max(p.dx_splits, split_count(cols, ce_dx(Mr, cols, K, p.pieces > 1 || p.twice > 0).splits));
     const int s = split_count(Mr, ce_dw(Mr, cols, K).splits);
     dw = std::max(dw, s > 1 ? (size_t)s * cols * p.width * 4 : 0);
-    db = std::max(db, (size_t)s * cdiv(K, 64) * cols * 4);
+    db = std::max(db, (size_t)std::max<int64_t>(4, s * cdiv(K, 64)) * cols * 4);
   }
-  p.dx_parts = p.twice || p.dx_parts || p.dx_splits > 1;
-  p.dz = 256;
+  p.dx_parts = p.twice > 0 || p.dx_parts || p.dx_splits > 1;
+  p.lo = 256;
+  p.dz = p.lo + (p.rest ? align256((size_t)M * 4) : 0);
   p.dxp = p.dz + align256((size_t)rows * cdiv(p.most, 64) * 64 * 2);
   p.dwp = p.dxp + (p.dx_parts ? align256((size_t)p.dx_splits * Mr * p.width * 4) : 0);
   p.dbp = p.dwp + align256(dw);
   p.x2 = p.dbp + align256(db);
-  p.total = p.x2 + (p.twice ? align256((size_t)128 * cdiv(K, 8) * 8 * 2) : 0) +
+  p.total = p.x2 + align256((size_t)2 * p.twice * cdiv(K, 8) * 8 * 2) +
             (ce_pads_bwd(M, K) ? align256((size_t)(M + V) * ce_padded(K) * 2) : 0);
   return p;
 }
@@ -455,14 +459,14 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   char* ws = (char*)workspace;
   float* scalars = (float*)ws;
   uint16_t* dz = (uint16_t*)(ws + p.dz);
-  // few rows: dz and what its rounding left, over X twice
-  const int64_t Mr = p.twice ? 128 : M;
+  // few rows: dz and what its rounding left, over X twice over
+  const int64_t Mr = p.twice ? p.rows : M;
   uint16_t* X2 = (uint16_t*)(ws + p.x2);
   GemmArgs both = ce_args(X, W, M, V, K, K, K);  // X, W, or their padded copies
   if (ce_pads_bwd(M, K)) MPX_HIP(ce_pad(X, M, W, V, K, X2, both, s));
   const uint16_t* Xr = p.twice ? X2 : both.A;
   const int64_t ldx = p.twice ? cdiv(K, 8) * 8 : both.ldb;
-  const unsigned grid = p.twice && dW ? 129 : 1;
+  const unsigned grid = p.twice && dW ? (unsigned)(1 + p.rows) : 1;
   if (dt == MPX_F16)
     ce_prepare_kernel<true><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X, K, X2, ldx);
   else
@@ -474,15 +478,16 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     return staged_any(g, ak, false) ? STAGED_ANY
            : cdiv(g.M, 64) * cdiv(g.N, 64) * g.splits <= 512 ? STAGED_64 : STAGED_128;
   };
+  float* rest = p.rest && db ? (float*)(ws + p.lo) : nullptr;
   const auto run_out = [&](const CeOutArgs& g, bool ak, RowTile t) {
     return dt == MPX_F16 ? run_ce_out_f16(g, ak, t, s) : run_ce_out_bf16(g, ak, t, s);
   };
   const auto reduce = [&](const float* part, int splits, int64_t stride, int64_t n, void* out, const float* dbp, int dbparts,
-                          int64_t nrows, void* dbo, int32_t* count) {
+                          int64_t nrows, void* dbo, int32_t* count, int32_t v0) {
     return by_type(dt, [&](auto type) {
       const auto launch = [&](auto kernel, int64_t per) {
         kernel<<<(unsigned)(cdiv(n, 256 * per) + cdiv(nrows, 4)), 256, 0, s>>>(
-            part, splits, stride, n, (int32_t)p.width, (int32_t)K, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count);
+            part, splits, stride, n, (int32_t)p.width, (int32_t)K, (uint16_t*)out, dbp, dbparts, nrows, (uint16_t*)dbo, scalars, count, rest, targets, (int32_t)M, v0);
         return hipGetLastError();
       };
       return n % 4 == 0 && stride % 4 == 0 ? launch(ce_reduce_kernel<type, true>, 4)
@@ -505,14 +510,15 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     z.v0 = (int32_t)v0;
     z.vocabulary = (int32_t)V;
     const bool dma = dma_ok(z, operands_aligned(z), true, true);
-    z.twice = p.twice ? 1 : 0;
+    z.twice = (int32_t)p.twice;
+    z.rest = rest;
     const RowTile t = ce_tile(M, cols, K, dma, !dma && staged_any(z, true, true), false);
     MPX_HIP(dt == MPX_F16 ? run_ce_grad_f16(z, t, s) : run_ce_grad_bf16(z, t, s));
     if (dX) {
       CeOutArgs g{};
       static_cast<GemmArgs&>(g) = ce_args(dz, Wp, Mr, p.dx_parts ? p.width : K, cols, ldz, both.ldb);
       g.C = (uint16_t*)dX;
-      const RowChoice c = ce_dx(Mr, cols, K, p.pieces > 1 || p.twice);
+      const RowChoice c = ce_dx(Mr, cols, K, p.pieces > 1 || p.twice > 0);
       g.k_split = split_len(cols, c.splits);
       g.splits = split_count(cols, c.splits);
       g.part = p.dx_parts ? (float*)(ws + p.dxp) : nullptr;
@@ -535,27 +541,29 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       g.add = 0;
       g.nonfinite = d_nonfinite;
       // db: summed by the first column of tiles and ended there, or shared by all columns
-      // and ended by the reduction, which is worth its launch from about 30 us on
-      if (db && g.splits == 1 && c.us < 30.0) g.db = (uint16_t*)db + v0;
+      // and ended by the reduction, which is worth its launch from about 30 us on, and
+      // needed where the targets' rests belong to it
+      if (db && !rest && g.splits == 1 && c.us < 30.0) g.db = (uint16_t*)db + v0;
       else if (db) g.dbp = (float*)(ws + p.dbp);
       const RowTile tw = out_tile(g, false, c.tile);
       MPX_HIP(run_out(g, false, tw));
       const int dbparts = (int)(g.splits * cdiv(K, tile_cols(tw)));
       if (g.part || g.dbp)
         MPX_HIP(reduce(g.part, g.splits, cols * p.width, g.part ? cols * p.width : 0, g.C, g.dbp, dbparts, g.dbp ? cols : 0,
-                       g.dbp ? (uint16_t*)db + v0 : nullptr, d_nonfinite));
+                       g.dbp ? (uint16_t*)db + v0 : nullptr, d_nonfinite, (int32_t)v0));
     } else if (db) {
       MPX_HIP(by_type(dt, [&](auto type) {
-        ce_colsum_kernel<type><<<(unsigned)(ldz / 64), 256, 0, s>>>(dz, ldz, p.rows, cols, (uint16_t*)db + v0, scalars,
-                                                                   d_nonfinite);
+        ce_colsum_kernel<type><<<(unsigned)(ldz / 64), 256, 0, s>>>(dz, ldz, p.rows, cols, (float*)(ws + p.dbp));
         return hipGetLastError();
       }));
+      MPX_HIP(reduce(nullptr, 0, 0, 0, nullptr, (const float*)(ws + p.dbp), 4, cols, (uint16_t*)db + v0, d_nonfinite,
+                     (int32_t)v0));
     }
   }
   if (dX && p.dx_parts)
-    // few rows: each split's partial sums are two sets of 64 rows
+    // few rows: each split's partial sums are two sets of rows
     MPX_HIP(reduce((const float*)(ws + p.dxp), p.twice ? 2 * dx_parts : dx_parts,
-                   (p.twice ? 64 : M) * p.width, M * p.width, dX,
-                   nullptr, 0, 0, nullptr, nullptr));
+                   (p.twice ? p.twice : M) * p.width, M * p.width, dX,
+                   nullptr, 0, 0, nullptr, nullptr, 0));
   return MPX_OK;
 }

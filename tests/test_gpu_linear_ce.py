@@ -160,8 +160,8 @@ def _gradient_bounds(x, w, z, dz, d, f, stats, fmt):
         p = np.exp(z - stats[:, :1] - stats[:, 1:])
         arg = np.where(p > 0, np.abs(z) + np.abs(stats[:, :1]) + np.abs(stats[:, 1:]) + 8, 0.0)
     fa = np.abs(f)[:, None]
-    # up to 64 rows what the rounding of dz leaves is kept, and rounded itself
-    step = HALF[fmt] ** 2 if len(x) <= 64 else HALF[fmt]
+    # up to 128 rows what the rounding of dz leaves is kept, and rounded itself
+    step = HALF[fmt] ** 2 if len(x) <= 128 else HALF[fmt]
     e = fa * p * 1.01 * (dz + (em + el)[:, None] + arg * 2.0 ** -22) + np.abs(d) * (step + 2.0 ** -22)
     if fmt == "f16":
         e = e + 2.0 ** -38 * fa.max()
