@@ -582,8 +582,8 @@ int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t 
  * negative, the row has no target (loss 0, no gradient); V or more gives NaN.  A bias
  * of -inf masks its column (probability 0, no gradient); a row of nothing but masked
  * ones has stats (-inf, 0) and loss inf.  A NaN or +inf logit makes its row's ln S and
- * loss NaN.  1 <= M <= 2^20, V <= 2^24, K <= 2^16; dt MPX_F16 or MPX_BF16; X and W
- * dense, all aligned to their element (stats 8 bytes).  Operands 16-byte aligned with K
+ * loss NaN.  1 <= M <= 2^20, V <= 2^24, K <= 2^16, M V <= 2^36, (M + V) K <= 2^33;
+ * dt MPX_F16 or MPX_BF16; X and W dense, all aligned to their element (stats 8 bytes).  Operands 16-byte aligned with K
  * a multiple of 64 go the fastest way.  workspace:
  * mpx_linear_ce_fwd_workspace(M, V, K) bytes, 16-byte aligned, not shared by calls
  * that overlap; results do not depend on what else runs (no atomics). */
@@ -599,7 +599,8 @@ size_t mpx_linear_ce_fwd_workspace(int64_t M, int64_t V, int64_t K);
  * (d_state NULL: 1; any subset, the others NULL).  The logits are computed again, in
  * pieces of the vocabulary: a piece's dz is held in the half type in the workspace
  * (float16: scaled by a power of two that keeps small probabilities, and back), dX's
- * sums over the pieces in float32.  A row whose stats are NaN, or whose target is V
+ * sums over the pieces in float32.  Up to 128 rows, what that rounding leaves is kept as
+ * well.  A row whose stats are NaN, or whose target is V
  * or more, makes its dX and all of dW NaN.  d_nonfinite (nullable) counts non-finite
  * dW and db elements.  workspace: mpx_linear_ce_bwd_workspace(M, V, K) bytes, 16-byte
  * aligned.  Sizes and types as the forward's; outputs overlap nothing. */

@@ -9,7 +9,8 @@ namespace mpx {
 // 16 columns of H for up to 32 rows of X, its four waves a quarter of the reduction
 // each, with as many loads in flight as that has steps.  A = 16 gate rows of W and the
 // 16 other ones, B = X: lane l has row l % 32 of X, accumulators i and 8 + i are G and U of
-// the same column.  The waves' sums are added in wave order.
+// the same column.  The waves' sums are added in wave order.  4 x 2048 x 768 bf16 about 6 us
+// for 6.3 MB: latency, of a launch and of one round of loads (128 workgroups).
 template <int DT, int ACT>
 __global__ __launch_bounds__(256) void gated_few_kernel(GemmArgs g) {
   __shared__ float part[4][16][64];

@@ -104,7 +104,8 @@ struct NoPrefetch {};
 
 // Which tile a product with an end of its own takes: direct-to-LDS ones by size, or
 // register-staged ones (any alignment; STAGED_ANY: also rows of fewer than 8 values).
-enum RowTile { TILE_32x128, TILE_64x128, TILE_128x128, TILE_256x256, TILE_192x128, STAGED_64, STAGED_128, STAGED_ANY };
+enum RowTile { TILE_32x128, TILE_64x128, TILE_128x128, TILE_192x128, TILE_256x256, STAGED_64, STAGED_128, STAGED_ANY };
+constexpr unsigned bit(RowTile t) { return 1u << t; }
 constexpr int tile_cols(RowTile t) {
   return t == TILE_256x256 ? 256 : t == STAGED_64 || t == STAGED_ANY ? 64 : 128;
 }
@@ -154,21 +155,25 @@ hipError_t launch_row_tiles(const Args& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-// AK, BKM: the operands' layouts; DBS: with the sums of A's rows.  32 x 128 tiles (waves of
-// 32 columns) only where Args can end them.
+// AK, BKM: the operands' layouts; DBS: with the sums of A's rows.  Tiles of 32
+// rows and of 256 are compiled where Args::kTiles has them, of 64 for a k-major A.
 template <int DT, class Args, bool AK, bool BKM, bool DBS>
 hipError_t launch_rows(const Args& g, RowTile t, hipStream_t s) {
+  constexpr unsigned tiles = Args::kTiles;
   switch (t) {
     case TILE_32x128:
-      if constexpr (Args::kNarrow)
+      if constexpr (tiles & bit(TILE_32x128))
         return launch_row_tiles<DT, Args, AK, BKM, DBS, 32, 128, 32, 32, 4, 0>(g, s);
-      return hipErrorInvalidValue;
+      break;
     case TILE_64x128:
       if constexpr (AK) return launch_row_tiles<DT, Args, AK, BKM, DBS, 64, 128, 32, 64, 3, 0>(g, s);
-      return hipErrorInvalidValue;
+      break;
     case TILE_128x128: return launch_row_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 0>(g, s);
     case TILE_192x128: return launch_row_tiles<DT, Args, AK, BKM, DBS, 192, 128, 96, 64, 2, 0>(g, s);
-    case TILE_256x256: return launch_row_tiles<DT, Args, AK, BKM, DBS, 256, 256, 128, 64, 2, 0>(g, s);
+    case TILE_256x256:
+      if constexpr (tiles & bit(TILE_256x256))
+        return launch_row_tiles<DT, Args, AK, BKM, DBS, 256, 256, 128, 64, 2, 0>(g, s);
+      break;
     case STAGED_64: return launch_row_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 1>(g, s);
     case STAGED_128: return launch_row_tiles<DT, Args, AK, BKM, DBS, 128, 128, 64, 64, 2, 1>(g, s);
     case STAGED_ANY: return launch_row_tiles<DT, Args, AK, BKM, DBS, 64, 64, 32, 64, 2, 2>(g, s);

@@ -61,7 +61,8 @@ def test_silu_is_no_activation_of_plain_layers(mx):
 @pytest.mark.parametrize("change, match", [
     ({0: None}, "NULL"), ({1: None}, "NULL"), ({3: None}, "targets"), ({4: 0}, ">= 1"), ({5: 0}, ">= 1"),
     ({6: 0}, ">= 1"), ({4: (1 << 20) + 1}, "too large"), ({5: (1 << 24) + 1}, "too large"),
-    ({6: (1 << 16) + 1}, "too large"), ({7: None, 8: None}, "nothing to compute"), ({7: None}, "its mean"),
+    ({6: (1 << 16) + 1}, "too large"), ({4: 1 << 20, 5: (1 << 16) + 1}, "too large"),
+    ({5: 1 << 20, 6: 1 << 13}, "too large"), ({7: None, 8: None}, "nothing to compute"), ({7: None}, "its mean"),
     ({10: 0}, "MPX_F16"), ({10: 9}, "MPX_F16"), ({0: 257}, "aligned"), ({2: 257}, "aligned"), ({3: 258}, "aligned"),
     ({7: 258}, "aligned"), ({8: 260}, "aligned"), ({11: None}, "workspace"), ({12: 10}, "workspace"),
     ({11: 264}, "workspace")])
