@@ -518,7 +518,8 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     const bool dma = dma_ok(z, operands_aligned(z), true, true);
     z.twice = (int32_t)p.twice;
     z.rest = rest;
-    const RowTile t = ce_tile(M, cols, K, dma, !dma && staged_any(z, true, true), false);
+    RowTile t = ce_tile(M, cols, K, dma, !dma && staged_any(z, true, true), false);
+    if (t == TILE_256x256 && (z.twice || rest)) t = TILE_192x128;  // the large tiles make neither
     MPX_HIP(dt == MPX_F16 ? run_ce_grad_f16(z, t, s) : run_ce_grad_bf16(z, t, s));
     if (dX) {
       CeOutArgs g{};
