@@ -117,7 +117,7 @@ struct CeGradArgs : GemmArgs {
   static constexpr unsigned kTiles = bit(TILE_256x256);
   static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kHalfBytes; }
   const float2* stats;
-  const float* scalars;  // {1 / c, c scale, or c scale / rows with a target when g_loss is NULL}
+  const float* unit;  // c scale, or c scale / rows with a target when g_loss is NULL (nullable: 1)
   const float* g_loss;
   const int32_t* targets;
   int32_t v0, vocabulary;  // the piece's first column, and the columns of all
@@ -133,7 +133,7 @@ struct CeGradArgs : GemmArgs {
   template <int DT, int TM, int STG>
   __device__ __forceinline__ Rows<TM> prefetch(int64_t mw, int64_t, int lane) const {
     Rows<TM> r;
-    r.unit = scalars[1];
+    r.unit = unit ? *unit : 1.0f;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t row = min(mw + 32 * i + (lane & 31), M - 1);
@@ -216,9 +216,9 @@ struct CeOutArgs : GemmArgs {
   static constexpr unsigned kTiles = bit(TILE_256x256);
   static constexpr int lds_bytes(int bm, int bn, int wm, int wn) { return bm / wm * (bn / wn) * kRowsBytes; }
   float* part;         // [splits][M][N]
-  const float* alpha;  // 1 / c
+  const float* alpha;  // 1 / c (nullable: 1)
   int32_t add;
-  __device__ __forceinline__ float db_end(float sum, int64_t) const { return sum * *alpha; }
+  __device__ __forceinline__ float db_end(float sum, int64_t) const { return alpha ? sum * *alpha : sum; }
   template <int DT, int TM, int STG>
   __device__ __forceinline__ NoPrefetch prefetch(int64_t, int64_t, int) const { return {}; }
   template <int DT, int BM, int BN, int WM, int WN, int TM, int TN>
@@ -231,7 +231,7 @@ struct CeOutArgs : GemmArgs {
     const int nc = (int)min<int64_t>(8, N - nw - c8);
     if (mv <= 0 || N - nw <= 0) return;  // uniform over the wave
     float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
-    const float scale = part ? 1.0f : *alpha;
+    const float scale = part || !alpha ? 1.0f : *alpha;
     const bool whole = nc == 8 && N % 4 == 0, more = split < add;
     int bad = 0;
     static_for<TM>([&](auto i) {

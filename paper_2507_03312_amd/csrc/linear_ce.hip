@@ -124,67 +124,89 @@ __global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, c
   scalars[1] = unit * __builtin_bit_cast(float, (uint32_t)(127 + e) << 23);
 }
 
-// out[i] = half(alpha sum over splits of part[s stride + i]), VEC: 4 a thread (n, stride and
-// part allow 16 bytes); rows of `width` sums, of which `cols` are kept.  Workgroups past
+// out[i] = half(alpha sum over splits of part[s stride + i]); rows of `width` sums, of which
+// `cols` are kept.
+struct CeSum {
+  const float* part;
+  int64_t stride, n;
+  int32_t splits;
+  uint16_t* out;
+  int32_t* nonfinite;
+};
+struct CeReduce {
+  CeSum first, second;  // n = 0: none
+  int32_t width, cols;
+  const float* dbp;  // [nrows][dbparts]
+  int64_t nrows;
+  int32_t dbparts;
+  uint16_t* db;
+  int32_t* nonfinite;
+  const float *alpha, *rest;  // nullable: 1, none
+  const int32_t* targets;
+  int32_t rows, v0;
+};
+
+// Both sums, VEC: 4 values a thread (n, stride and part allow 16 bytes).  Workgroups past
 // those: db[r] = half(alpha (sum over p of dbp[r][p], and of the rests of the rows whose
 // target is r)), one wave a row, its lanes in strides of 64 and then wave_sum (one lane
 // a row took 95 us for the rests of 509 rows of 1000 columns).
 template <int DT, bool VEC>
-__global__ __launch_bounds__(256) void ce_reduce_kernel(const float* part, int splits, int64_t stride, int64_t n,
-                                                        int32_t width, int32_t cols, uint16_t* out, const float* dbp,
-                                                        int dbparts, int64_t nrows, uint16_t* db, const float* alpha,
-                                                        int32_t* nonfinite, const float* rest, const int32_t* targets,
-                                                        int32_t rows, int32_t v0) {
+__global__ __launch_bounds__(256) void ce_reduce_kernel(CeReduce a) {
   constexpr int PER = VEC ? 4 : 1;
-  const int64_t blocks = (n + 256 * PER - 1) / (256 * PER);
-  const float scale = *alpha;
+  const int64_t blocks1 = (a.first.n + 256 * PER - 1) / (256 * PER);
+  const int64_t blocks = blocks1 + (a.second.n + 256 * PER - 1) / (256 * PER);
+  const float scale = a.alpha ? *a.alpha : 1.0f;
   int bad = 0;
+  int32_t* count = a.nonfinite;
   if (blockIdx.x < blocks) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * PER;
-    if (i >= n) return;
+    const bool one = blockIdx.x < blocks1;
+    const CeSum u = one ? a.first : a.second;
+    const int64_t i = ((blockIdx.x - (one ? 0 : blocks1)) * 256 + threadIdx.x) * PER;
+    if (i >= u.n) return;
+    count = u.nonfinite;
     float s[PER] = {};
 #pragma unroll 8
-    for (int k = 0; k < splits; ++k) {
+    for (int k = 0; k < u.splits; ++k) {
       float t[PER];
-      __builtin_memcpy(t, part + k * stride + i, sizeof(t));
+      __builtin_memcpy(t, u.part + k * u.stride + i, sizeof(t));
 #pragma unroll
       for (int e = 0; e < PER; ++e) s[e] += t[e];
     }
     uint16_t h[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) h[e] = f2h<DT>(s[e] * scale);
-    if (width == cols) {  // uniform
+    if (a.width == a.cols) {  // uniform
 #pragma unroll
       for (int e = 0; e < PER; ++e) bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
-      __builtin_memcpy(out + i, h, sizeof(h));
+      __builtin_memcpy(u.out + i, h, sizeof(h));
     } else {
-      const int64_t row = i / width;
-      const int c = (int)(i - row * width);
+      const int64_t row = i / a.width;
+      const int c = (int)(i - row * a.width);
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        if (c + e < cols) {
-          out[row * cols + c + e] = h[e];
+        if (c + e < a.cols) {
+          u.out[row * a.cols + c + e] = h[e];
           bad += h_nonfinite<DT>(h[e]) ? 1 : 0;
         }
       }
     }
   } else {
     const int64_t row = ((int64_t)blockIdx.x - blocks) * 4 + (threadIdx.x >> 6);
-    if (row >= nrows) return;  // uniform over the wave
+    if (row >= a.nrows) return;  // uniform over the wave
     const int lane = threadIdx.x & 63;
     float s = 0.0f;
-    for (int k = lane; k < dbparts; k += 64) s += dbp[row * dbparts + k];
-    if (rest) {  // what rounding left of the targets that are this column
-      for (int r = lane; r < rows; r += 64) s += targets[r] == v0 + row ? rest[r] : 0.0f;
+    for (int k = lane; k < a.dbparts; k += 64) s += a.dbp[row * a.dbparts + k];
+    if (a.rest) {  // what rounding left of the targets that are this column
+      for (int r = lane; r < a.rows; r += 64) s += a.targets[r] == a.v0 + row ? a.rest[r] : 0.0f;
     }
     s = wave_sum(s);
     if (lane == 0) {
       const uint16_t h = f2h<DT>(s * scale);
-      db[row] = h;
+      a.db[row] = h;
       bad = h_nonfinite<DT>(h) ? 1 : 0;
     }
   }
-  if (nonfinite) add_nonfinite(nonfinite, bad);
+  if (count) add_nonfinite(count, bad);
 }
 
 // db of a piece where dW is not asked for: partial sums dbp[column][4] for the reduction,
@@ -424,7 +446,10 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
   const RowTile tile = any ? STAGED_ANY : t;
   MPX_HIP(dt == MPX_F16 ? run_ce_fwd_f16(g, tile, s) : run_ce_fwd_bf16(g, tile, s));
   const int parts = (int)cdiv(V, tile_cols(tile));
-  if (M >= 2048)
+  if (parts <= 16)
+    ce_join_kernel<128><<<(unsigned)cdiv(M, 128), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
+                                                                (float2*)stats);
+  else if (M >= 2048)
     ce_join_kernel<32><<<(unsigned)cdiv(M, 32), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
                                                               (float2*)stats);
   else
@@ -471,12 +496,16 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   const uint16_t* Xr = p.twice ? X2 : both.A;
   const int64_t ldx = p.twice ? cdiv(K, 8) * 8 : both.ldb;
   const unsigned grid = p.twice && dW ? (unsigned)(1 + p.rows) : 1;
-  if (dt == MPX_F16)
-    ce_prepare_kernel<true><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X, K, X2, ldx);
-  else
-    ce_prepare_kernel<false><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X, K, X2,
-                                                   ldx);
-  MPX_LAUNCHED();
+  // bf16 with cotangents of its own: c = 1 and the scale as it stands, nothing to prepare
+  const bool plain = dt == MPX_BF16 && g_loss;
+  const float* unit = !plain ? scalars + 1 : d_state ? &d_state->scale : nullptr;
+  const float* alpha = plain ? nullptr : scalars;
+  if (!plain || grid > 1)
+    MPX_HIP(by_type(dt, [&](auto type) {
+      ce_prepare_kernel<type == MPX_F16><<<grid, 1024, 0, s>>>(g_loss, targets, M, d_state, scalars, (const uint16_t*)X,
+                                                               K, X2, ldx);
+      return hipGetLastError();
+    }));
   // the reductions' own operands: dz is aligned, X and W as they come
   const auto out_tile = [&](const GemmArgs& g, bool ak, RowTile direct) {
     if ((reinterpret_cast<uintptr_t>(g.B) & 15u) == 0 && g.ldb % 8 == 0) return direct;
@@ -487,17 +516,24 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   const auto run_out = [&](const CeOutArgs& g, bool ak, RowTile t) {
     return dt == MPX_F16 ? run_ce_out_f16(g, ak, t, s) : run_ce_out_bf16(g, ak, t, s);
   };
-  const auto reduce = [&](const float* part, int splits, int64_t stride, int64_t n, void* out, const float* dbp,
-                          int dbparts, int64_t nrows, void* dbo, int32_t* count, int32_t v0) {
+  CeReduce sums{};  // of a piece, and with the last one's dX's
+  sums.width = (int32_t)p.width;
+  sums.cols = (int32_t)K;
+  sums.nonfinite = d_nonfinite;
+  sums.alpha = alpha;
+  sums.rest = rest;
+  sums.targets = targets;
+  sums.rows = (int32_t)M;
+  const auto reduce = [&] {
+    const auto fits = [](const CeSum& u) { return u.n % 4 == 0 && u.stride % 4 == 0; };
+    const bool vec = fits(sums.first) && fits(sums.second);
+    const int64_t per = vec ? 1024 : 256;
+    const unsigned blocks =
+        (unsigned)(cdiv(sums.first.n, per) + cdiv(sums.second.n, per) + cdiv(sums.nrows, 4));
     return by_type(dt, [&](auto type) {
-      const auto launch = [&](auto kernel, int64_t per) {
-        kernel<<<(unsigned)(cdiv(n, 256 * per) + cdiv(nrows, 4)), 256, 0, s>>>(
-            part, splits, stride, n, (int32_t)p.width, (int32_t)K, (uint16_t*)out, dbp, dbparts, nrows,
-            (uint16_t*)dbo, scalars, count, rest, targets, (int32_t)M, v0);
-        return hipGetLastError();
-      };
-      return n % 4 == 0 && stride % 4 == 0 ? launch(ce_reduce_kernel<type, true>, 4)
-                                           : launch(ce_reduce_kernel<type, false>, 1);
+      if (vec) ce_reduce_kernel<type, true><<<blocks, 256, 0, s>>>(sums);
+      else ce_reduce_kernel<type, false><<<blocks, 256, 0, s>>>(sums);
+      return hipGetLastError();
     });
   };
   int dx_parts = 0;  // partial sums of dX so far
@@ -510,7 +546,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     z.C = dz;
     z.ldc = ldz;
     z.stats = (const float2*)stats;
-    z.scalars = scalars;
+    z.unit = unit;
     z.g_loss = g_loss;
     z.targets = targets;
     z.v0 = (int32_t)v0;
@@ -529,7 +565,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       g.k_split = split_len(cols, c.splits);
       g.splits = split_count(cols, c.splits);
       g.part = p.dx_parts ? (float*)(ws + p.dxp) : nullptr;
-      g.alpha = scalars;
+      g.alpha = alpha;
       // the last piece may take another count than those before: what it adds to stands there
       g.add = i > 0 ? dx_parts : 0;
       dx_parts = std::max(dx_parts, g.splits);
@@ -544,7 +580,7 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       g.splits = split_count(Mr, c.splits);
       g.part = g.splits > 1 ? (float*)(ws + p.dwp) : nullptr;
       if (g.part) g.N = p.width;
-      g.alpha = scalars;
+      g.alpha = alpha;
       g.add = 0;
       g.nonfinite = d_nonfinite;
       // db: summed by the first column of tiles and ended there, or shared by all columns
@@ -554,23 +590,28 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       else if (db) g.dbp = (float*)(ws + p.dbp);
       const RowTile tw = out_tile(g, false, c.tile);
       MPX_HIP(run_out(g, false, tw));
-      const int dbparts = (int)(g.splits * cdiv(K, tile_cols(tw)));
-      if (g.part || g.dbp)
-        MPX_HIP(reduce(g.part, g.splits, cols * p.width, g.part ? cols * p.width : 0, g.C, g.dbp, dbparts,
-                       g.dbp ? cols : 0, g.dbp ? (uint16_t*)db + v0 : nullptr, d_nonfinite, (int32_t)v0));
+      sums.dbparts = (int)(g.splits * cdiv(K, tile_cols(tw)));
+      sums.dbp = g.dbp;
+      if (g.part) sums.first = {g.part, cols * p.width, cols * p.width, g.splits, g.C, d_nonfinite};
     } else if (db) {
+      sums.dbp = (float*)(ws + p.dbp);
+      sums.dbparts = 4;
       MPX_HIP(by_type(dt, [&](auto type) {
         ce_colsum_kernel<type><<<(unsigned)(ldz / 64), 256, 0, s>>>(dz, ldz, p.rows, cols, (float*)(ws + p.dbp));
         return hipGetLastError();
       }));
-      MPX_HIP(reduce(nullptr, 0, 0, 0, nullptr, (const float*)(ws + p.dbp), 4, cols, (uint16_t*)db + v0, d_nonfinite,
-                     (int32_t)v0));
     }
+    if (sums.dbp) {
+      sums.nrows = cols;
+      sums.db = (uint16_t*)db + v0;
+      sums.v0 = (int32_t)v0;
+    }
+    if (dX && p.dx_parts && i + 1 == p.pieces)
+      // few rows: each split's partial sums are two sets of rows
+      sums.second = {(const float*)(ws + p.dxp), (p.twice ? p.twice : M) * p.width, M * p.width,
+                     p.twice ? 2 * dx_parts : dx_parts, (uint16_t*)dX, nullptr};
+    if (sums.first.n || sums.second.n || sums.nrows) MPX_HIP(reduce());
+    sums.first.n = sums.nrows = 0;
   }
-  if (dX && p.dx_parts)
-    // few rows: each split's partial sums are two sets of rows
-    MPX_HIP(reduce((const float*)(ws + p.dxp), p.twice ? 2 * dx_parts : dx_parts,
-                   (p.twice ? p.twice : M) * p.width, M * p.width, dX,
-                   nullptr, 0, 0, nullptr, nullptr, 0));
   return MPX_OK;
 }
