@@ -150,7 +150,7 @@ struct CeGradArgs : GemmArgs {
     // neither of twice and rest comes with tiles of 256: there they spilled (118 -> 164 us)
     constexpr bool kExact = BM < 256;
     __syncthreads();
-    const int64_t rows64 = (M + 63) / 64 * 64;
+    const int64_t rows64 = twice ? twice : (M + 63) / 64 * 64;
     if (mw >= rows64 || nw >= ldc) return;  // uniform over the wave
     uint16_t* lds = reinterpret_cast<uint16_t*>(smem + wave * kHalfBytes);
     const int hi = lane >> 5, nv = (int)min<int64_t>(64, N - nw);  // >= 1: ldc is N rounded up to 64

@@ -12,7 +12,9 @@ __device__ __forceinline__ float2 ce_join(float2 a, float2 b) {
                             b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
 }
 
-// Joins the tile columns' (m, S) of R rows, 1024 / R threads to a row; a fixed order.
+// Joins the tile columns' (m, S) of R rows, 1024 / R threads to a row; a fixed order.  R is
+// what a row's parts leave threads for, and 16 (whole lines of 128 bytes) where there are rows
+// enough: 2019 rows of 710 parts 11 us by 4, 7.1 by 16.
 template <int R>
 __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* part, const float* zt, const int32_t* targets,
                                                        int64_t M, int32_t V, int parts, float* loss, float2* stats) {
@@ -20,6 +22,9 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* part, const
   __shared__ float2 lds[G][R];
   const int r = threadIdx.x % R, g = threadIdx.x / R;
   const int64_t row = (int64_t)blockIdx.x * R + r, rc = min(row, M - 1);
+  // ahead of the join: zt has no value of a row without a target, which is not used either
+  const int32_t t = loss && g == 0 ? targets[rc] : -1;
+  const float z = loss && g == 0 ? zt[rc] : 0.0f;
   float2 a = make_float2(-__builtin_inff(), 0.0f);
   constexpr int U = 4;
   for (int c = g; c < parts; c += U * G) {
@@ -39,12 +44,10 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* part, const
   const float ln = a.x == -__builtin_inff() ? 0.0f : logf(a.y);
   if (stats) stats[row] = make_float2(a.x, ln);
   if (loss) {
-    const int32_t t = targets[row];
     float l = 0.0f;
     if (t >= V) {
       l = __builtin_nanf("");
     } else if (t >= 0) {
-      const float z = zt[row];
       l = ln != ln ? ln : z == -__builtin_inff() ? __builtin_inff() : (a.x - z) + ln;
     }
     loss[row] = l;
@@ -150,28 +153,44 @@ struct CeReduce {
 // those: db[r] = half(alpha (sum over p of dbp[r][p], and of the rests of the rows whose
 // target is r)), one wave a row, its lanes in strides of 64 and then wave_sum (one lane
 // a row took 95 us for the rests of 509 rows of 1000 columns).
-template <int DT, bool VEC>
+// G threads a value where there are few values and many splits, each every G-th split, then
+// added in order.
+template <int DT, bool VEC, int G>
 __global__ __launch_bounds__(256) void ce_reduce_kernel(CeReduce a) {
-  constexpr int PER = VEC ? 4 : 1;
-  const int64_t blocks1 = (a.first.n + 256 * PER - 1) / (256 * PER);
-  const int64_t blocks = blocks1 + (a.second.n + 256 * PER - 1) / (256 * PER);
+  constexpr int PER = VEC ? 4 : 1, AT = 256 / G;  // AT threads' worth of values
+  __shared__ float lds[G > 1 ? G : 1][PER][AT];
+  const int64_t blocks1 = (a.first.n + AT * PER - 1) / (AT * PER);
+  const int64_t blocks = blocks1 + (a.second.n + AT * PER - 1) / (AT * PER);
   const float scale = a.alpha ? *a.alpha : 1.0f;
   int bad = 0;
   int32_t* count = a.nonfinite;
   if (blockIdx.x < blocks) {
     const bool one = blockIdx.x < blocks1;
     const CeSum u = one ? a.first : a.second;
-    const int64_t i = ((blockIdx.x - (one ? 0 : blocks1)) * 256 + threadIdx.x) * PER;
-    if (i >= u.n) return;
+    const int at = threadIdx.x % AT, g = threadIdx.x / AT;
+    const int64_t i = ((blockIdx.x - (one ? 0 : blocks1)) * AT + at) * PER;
+    const bool in = i < u.n;
     count = u.nonfinite;
     float s[PER] = {};
 #pragma unroll 8
-    for (int k = 0; k < u.splits; ++k) {
+    for (int k = g; k < u.splits; k += G) {
       float t[PER];
-      __builtin_memcpy(t, u.part + k * u.stride + i, sizeof(t));
+      if (in) __builtin_memcpy(t, u.part + k * u.stride + i, sizeof(t));
 #pragma unroll
-      for (int e = 0; e < PER; ++e) s[e] += t[e];
+      for (int e = 0; e < PER; ++e) s[e] += in ? t[e] : 0.0f;
     }
+    if constexpr (G > 1) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) lds[g][e][at] = s[e];
+      __syncthreads();
+      if (g > 0) return;
+#pragma unroll
+      for (int k = 1; k < G; ++k) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) s[e] += lds[k][e][at];
+      }
+    }
+    if (!in) return;
     uint16_t h[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) h[e] = f2h<DT>(s[e] * scale);
@@ -252,10 +271,11 @@ static const RowCost kDwCost[] = {{TILE_128x128, 128, 128, 2, {0.60, 0.77, 0}, 2
                                   {TILE_192x128, 192, 128, 2, {0.82, 1.04, 0}, 4.92},
                                   {TILE_256x256, 256, 256, 1, {1.29, 0, 0}, 13.3}};
 
-// Tile of a product of two k-major operands (forward and dz).
+// Tile of a product of two k-major operands (forward and dz).  Staged ones of at most 64
+// rows: 11 x 51223 x 183 f16 dz 18.3 us by 128 x 128, 12.5 by 64 x 64.
 static RowTile ce_tile(int64_t M, int64_t N, int64_t K, bool dma, bool any, bool forward) {
   if (any) return STAGED_ANY;
-  if (!dma) return cdiv(M, 64) * cdiv(N, 64) <= 512 ? STAGED_64 : STAGED_128;
+  if (!dma) return M <= 64 || cdiv(M, 64) * cdiv(N, 64) <= 512 ? STAGED_64 : STAGED_128;
   if (forward && M <= 32) return TILE_32x128;
   return choose_rows(forward ? kFwdCost : kGradCost, M, N, K).tile;
 }
@@ -310,9 +330,10 @@ static int split_count(int64_t len, int splits) { return (int)cdiv(len, split_le
 // time of 3 of 64 and one of 65).
 static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   CePlan p{};
-  // up to 128 rows dX's norm would lose up to a factor of 1.8 to the rounding of dz, with
+  // 32, 64 or 128 rows of each (20 x 63884 x 256 bf16 of 64 each 72 us, of 32 62): up to
+  // 128 rows dX's norm would lose up to a factor of 1.8 to the rounding of dz, with
   // 256 1.45; db's, of few columns, of up to a thousand rows 2
-  p.twice = M <= 64 ? 64 : M <= 128 ? 128 : 0;
+  p.twice = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 0;
   p.rest = !p.twice && M * V <= ((int64_t)1 << 22);
   p.width = ce_pads_bwd(M, K) ? cdiv(K, 4) * 4 : K;
   const int64_t rows = p.rows = p.twice ? 2 * p.twice : cdiv(M, 64) * 64, Mr = p.twice ? p.rows : M;
@@ -449,8 +470,8 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
   if (parts <= 16)
     ce_join_kernel<128><<<(unsigned)cdiv(M, 128), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
                                                                 (float2*)stats);
-  else if (M >= 2048)
-    ce_join_kernel<32><<<(unsigned)cdiv(M, 32), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
+  else if (M >= 512)
+    ce_join_kernel<16><<<(unsigned)cdiv(M, 16), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
                                                               (float2*)stats);
   else
     ce_join_kernel<4><<<(unsigned)cdiv(M, 4), 1024, 0, s>>>(g.part, g.zt, targets, M, (int32_t)V, parts, loss,
@@ -527,12 +548,15 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   const auto reduce = [&] {
     const auto fits = [](const CeSum& u) { return u.n % 4 == 0 && u.stride % 4 == 0; };
     const bool vec = fits(sums.first) && fits(sums.second);
-    const int64_t per = vec ? 1024 : 256;
-    const unsigned blocks =
-        (unsigned)(cdiv(sums.first.n, per) + cdiv(sums.second.n, per) + cdiv(sums.nrows, 4));
+    // 20 x 256 sums of 128 parts: one thread a value 6.8 us, 8 of them 4.5
+    const int64_t per = vec ? 4 : 1, n = sums.first.n + sums.second.n;
+    const bool few = n / per <= 16384 && std::max(sums.first.splits, sums.second.splits) >= 16;
+    const int64_t at = (few ? 32 : 256) * per;
+    const unsigned blocks = (unsigned)(cdiv(sums.first.n, at) + cdiv(sums.second.n, at) + cdiv(sums.nrows, 4));
     return by_type(dt, [&](auto type) {
-      if (vec) ce_reduce_kernel<type, true><<<blocks, 256, 0, s>>>(sums);
-      else ce_reduce_kernel<type, false><<<blocks, 256, 0, s>>>(sums);
+      const auto kernel = vec ? (few ? ce_reduce_kernel<type, true, 8> : ce_reduce_kernel<type, true, 1>)
+                              : (few ? ce_reduce_kernel<type, false, 8> : ce_reduce_kernel<type, false, 1>);
+      kernel<<<blocks, 256, 0, s>>>(sums);
       return hipGetLastError();
     });
   };
@@ -611,7 +635,8 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       sums.second = {(const float*)(ws + p.dxp), (p.twice ? p.twice : M) * p.width, M * p.width,
                      p.twice ? 2 * dx_parts : dx_parts, (uint16_t*)dX, nullptr};
     if (sums.first.n || sums.second.n || sums.nrows) MPX_HIP(reduce());
-    sums.first.n = sums.nrows = 0;
+    sums.first = {};
+    sums.nrows = 0;
   }
   return MPX_OK;
 }
