@@ -242,6 +242,45 @@ def test_several_pieces(fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("M, V, K", [(20, 1049001, 64), (50, 530003, 40), (100, 262500, 72), (129, 350001, 36),
+                                     (300, 210011, 72)])
+def test_few_rows_over_several_pieces(fmt, M, V, K):
+    """Few rows, with what the rounding of dz leaves, over a vocabulary of more than one piece:
+    dW and db element by element, dX in norm (half a step of every element, 2^-12 for its
+    float32 logits, exponents and sums; past 128 rows half a step of every dz more); subsets
+    and the padded rows of the reduction."""
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.empty(M, K, device="cuda").normal_(generator=g).to(TYPES[fmt])
+    w = (2.0 * K ** -0.5 * torch.empty(V, K, device="cuda").normal_(generator=g)).to(TYPES[fmt])
+    b = (0.5 * torch.empty(V, device="cuda").normal_(generator=g)).to(TYPES[fmt])
+    t = torch.randint(-1, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    t[0], t[1] = V - 1, 0   # the first and the last piece's own
+    st = torch.empty(M, 2, device="cuda")
+    ws = torch.empty(mx.mpx_linear_ce_fwd_workspace(M, V, K), dtype=torch.uint8, device="cuda")
+    mx.mpx_linear_ce_fwd(x.data_ptr(), w.data_ptr(), b.data_ptr(), None, M, V, K, None, st.data_ptr(), None,
+                         mx.DTYPES[fmt], ws.data_ptr(), ws.numel(), _s())
+    wt = (torch.rand(M, generator=g, device="cuda") + 0.5) / M
+    got = _backward((x, w, b, t), st, wt.cpu().numpy(), fmt, M, V, K)
+    z = x.double() @ w.double().t() + b.double()
+    d = torch.softmax(z, 1)
+    d[torch.arange(M, device="cuda"), t.long().clamp(min=0)] -= (t >= 0).double()
+    d *= (torch.where(t < 0, 0.0, wt.double()) * SCALE)[:, None]
+    ref = d @ w.double()
+    left = 0.0 if M <= 128 else HALF[fmt] * float((d.abs() @ w.double().abs()).norm() / ref.norm())
+    assert float((got[0].double() - ref).norm() / ref.norm()) <= HALF[fmt] + 2.0 ** -12 + left
+    step = 2.0 ** -12 + (HALF[fmt] ** 2 if M <= 128 else HALF[fmt])
+    least = 2.0 ** -38 * float(wt.max()) * SCALE if fmt == "f16" else 0.0   # float16's smallest dz
+    for o, q in ((got[1], x.double()), (got[2][:, None], torch.ones(M, 1, dtype=torch.float64, device="cuda"))):
+        ref, size = d.t() @ q, d.t().abs() @ q.abs()
+        bound = (step + 2.0 * M * 2.0 ** -24) * size + least * q.abs().sum(0) + 0.5 * torch.from_numpy(
+            ulp(ref.cpu().numpy(), fmt)).cuda() * (1 + 2.0 ** -10)
+        assert ((o.double() - ref).abs() <= bound).all()
+    for use in ({"dw": False, "db": False}, {"dx": False, "db": False}):
+        only = _backward((x, w, b, t), st, wt.cpu().numpy(), fmt, M, V, K, **use)
+        assert all(o is None or torch.equal(o, p) for o, p in zip(only, got))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("M", [5, 40])
 def test_masks_targets_and_not_finite_rows(fmt, M):
     """A bias of -inf masks its column; a target outside the vocabulary, a masked one,
