@@ -284,6 +284,45 @@ struct CeOutArgs : GemmArgs {
   }
 };
 
+// dW and dX of a piece in one launch, 128 columns and four waves a tile each: small ones leave
+// most of the chip empty while they wait for memory, large ones share their last rounds.
+struct CePairPlace {
+  uint32_t group, in_row;  // of a product's workgroups, its tiles
+  __device__ __forceinline__ uint32_t tile() const { return group % in_row; }
+  __device__ __forceinline__ uint32_t tiles() const { return in_row; }
+  __device__ __forceinline__ uint32_t batch() const { return group / in_row; }
+};
+template <int DT, bool DBS, int BMW, int BMX>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void ce_out_pair_kernel(CeOutArgs w, uint32_t wtiles, uint32_t wgroups, CeOutArgs x, uint32_t xtiles) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[std::max(
+      gemm_tile_lds<BMW, 128, BMW / 2, 64, CeOutArgs>(), gemm_tile_lds<BMX, 128, BMX / 2, 64, CeOutArgs>())];
+  const uint32_t b = blockIdx.x;
+  if (b < wgroups)
+    gemm_tile<DT, BMW, 128, BMW / 2, 64, false, false, 0, DBS, 0, false>(w, smem, CePairPlace{b, wtiles});
+  else
+    gemm_tile<DT, BMX, 128, BMX / 2, 64, true, false, 0, false, 0, false>(x, smem, CePairPlace{b - wgroups, xtiles});
+}
+template <int DT, int BMW, int BMX>
+hipError_t launch_ce_out_pair(const CeOutArgs& w, const CeOutArgs& x, hipStream_t s) {
+  const uint32_t wt = (uint32_t)(cdiv(w.M, BMW) * cdiv(w.N, 128)), xt = (uint32_t)(cdiv(x.M, BMX) * cdiv(x.N, 128));
+  const uint32_t wg = wt * w.splits, groups = wg + xt * x.splits;
+  if (w.dbp || w.db) ce_out_pair_kernel<DT, true, BMW, BMX><<<groups, 256, 0, s>>>(w, wt, wg, x, xt);
+  else ce_out_pair_kernel<DT, false, BMW, BMX><<<groups, 256, 0, s>>>(w, wt, wg, x, xt);
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_ce_out_pair(const CeOutArgs& w, RowTile tw, const CeOutArgs& x, RowTile tx, hipStream_t s) {
+  if (tw == TILE_128x128) {
+    if (tx == TILE_64x128) return launch_ce_out_pair<DT, 128, 64>(w, x, s);
+    if (tx == TILE_128x128) return launch_ce_out_pair<DT, 128, 128>(w, x, s);
+    return launch_ce_out_pair<DT, 128, 192>(w, x, s);
+  }
+  if (tx == TILE_64x128) return launch_ce_out_pair<DT, 192, 64>(w, x, s);
+  if (tx == TILE_128x128) return launch_ce_out_pair<DT, 192, 128>(w, x, s);
+  return launch_ce_out_pair<DT, 192, 192>(w, x, s);
+}
+
 // Launchers, compiled once per half type.  The layouts: forward and dz k-major operands,
 // dX a k-major A, dW neither.
 hipError_t run_ce_fwd_f16(const CeFwdArgs& g, RowTile t, hipStream_t s);
@@ -292,5 +331,7 @@ hipError_t run_ce_grad_f16(const CeGradArgs& g, RowTile t, hipStream_t s);
 hipError_t run_ce_grad_bf16(const CeGradArgs& g, RowTile t, hipStream_t s);
 hipError_t run_ce_out_f16(const CeOutArgs& g, bool ak, RowTile t, hipStream_t s);
 hipError_t run_ce_out_bf16(const CeOutArgs& g, bool ak, RowTile t, hipStream_t s);
+hipError_t run_ce_out_pair_f16(const CeOutArgs& w, RowTile tw, const CeOutArgs& x, RowTile tx, hipStream_t s);
+hipError_t run_ce_out_pair_bf16(const CeOutArgs& w, RowTile tw, const CeOutArgs& x, RowTile tx, hipStream_t s);
 
 }  // namespace mpx

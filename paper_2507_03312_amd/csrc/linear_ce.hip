@@ -581,42 +581,49 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     RowTile t = ce_tile(M, cols, K, dma, !dma && staged_any(z, true, true), false);
     if (t == TILE_256x256 && (z.twice || rest)) t = TILE_192x128;  // the large tiles make neither
     MPX_HIP(dt == MPX_F16 ? run_ce_grad_f16(z, t, s) : run_ce_grad_bf16(z, t, s));
+    CeOutArgs x{}, w{};
+    RowTile tx{}, tw{};
     if (dX) {
-      CeOutArgs g{};
-      static_cast<GemmArgs&>(g) = ce_args(dz, Wp, Mr, p.dx_parts ? p.width : K, cols, ldz, both.ldb);
-      g.C = (uint16_t*)dX;
+      static_cast<GemmArgs&>(x) = ce_args(dz, Wp, Mr, p.dx_parts ? p.width : K, cols, ldz, both.ldb);
+      x.C = (uint16_t*)dX;
       const RowChoice c = ce_dx(Mr, cols, K, p.pieces > 1 || p.twice > 0);
-      g.k_split = split_len(cols, c.splits);
-      g.splits = split_count(cols, c.splits);
-      g.part = p.dx_parts ? (float*)(ws + p.dxp) : nullptr;
-      g.alpha = alpha;
+      x.k_split = split_len(cols, c.splits);
+      x.splits = split_count(cols, c.splits);
+      x.part = p.dx_parts ? (float*)(ws + p.dxp) : nullptr;
+      x.alpha = alpha;
       // the last piece may take another count than those before: what it adds to stands there
-      g.add = i > 0 ? dx_parts : 0;
-      dx_parts = std::max(dx_parts, g.splits);
-      MPX_HIP(run_out(g, true, out_tile(g, true, c.tile)));
+      x.add = i > 0 ? dx_parts : 0;
+      dx_parts = std::max(dx_parts, x.splits);
+      tx = out_tile(x, true, c.tile);
     }
     if (dW) {
-      CeOutArgs g{};
-      static_cast<GemmArgs&>(g) = ce_args(dz, Xr, cols, K, Mr, ldz, ldx);
-      g.C = (uint16_t*)dW + v0 * K;
+      static_cast<GemmArgs&>(w) = ce_args(dz, Xr, cols, K, Mr, ldz, ldx);
+      w.C = (uint16_t*)dW + v0 * K;
       const RowChoice c = ce_dw(Mr, cols, K);
-      g.k_split = split_len(Mr, c.splits);
-      g.splits = split_count(Mr, c.splits);
-      g.part = g.splits > 1 ? (float*)(ws + p.dwp) : nullptr;
-      if (g.part) g.N = p.width;
-      g.alpha = alpha;
-      g.add = 0;
-      g.nonfinite = d_nonfinite;
+      w.k_split = split_len(Mr, c.splits);
+      w.splits = split_count(Mr, c.splits);
+      w.part = w.splits > 1 ? (float*)(ws + p.dwp) : nullptr;
+      if (w.part) w.N = p.width;
+      w.alpha = alpha;
+      w.add = 0;
+      w.nonfinite = d_nonfinite;
       // db: summed by the first column of tiles and ended there, or shared by all columns
       // and ended by the reduction, which is worth its launch from about 30 us on, and
       // needed where the targets' rests belong to it
-      if (db && !rest && g.splits == 1 && c.us < 30.0) g.db = (uint16_t*)db + v0;
-      else if (db) g.dbp = (float*)(ws + p.dbp);
-      const RowTile tw = out_tile(g, false, c.tile);
-      MPX_HIP(run_out(g, false, tw));
-      sums.dbparts = (int)(g.splits * cdiv(K, tile_cols(tw)));
-      sums.dbp = g.dbp;
-      if (g.part) sums.first = {g.part, cols * p.width, cols * p.width, g.splits, g.C, d_nonfinite};
+      if (db && !rest && w.splits == 1 && c.us < 30.0) w.db = (uint16_t*)db + v0;
+      else if (db) w.dbp = (float*)(ws + p.dbp);
+      tw = out_tile(w, false, c.tile);
+    }
+    if (dX && dW && tx <= TILE_192x128 && tw <= TILE_192x128) {
+      MPX_HIP(dt == MPX_F16 ? run_ce_out_pair_f16(w, tw, x, tx, s) : run_ce_out_pair_bf16(w, tw, x, tx, s));
+    } else {
+      if (dX) MPX_HIP(run_out(x, true, tx));
+      if (dW) MPX_HIP(run_out(w, false, tw));
+    }
+    if (dW) {
+      sums.dbparts = (int)(w.splits * cdiv(K, tile_cols(tw)));
+      sums.dbp = w.dbp;
+      if (w.part) sums.first = {w.part, cols * p.width, cols * p.width, w.splits, w.C, d_nonfinite};
     } else if (db) {
       sums.dbp = (float*)(ws + p.dbp);
       sums.dbparts = 4;

@@ -1,0 +1,10 @@
+// Linear cross entropy for bf16 operands: dW and dX in one launch (see linear_ce.h).
+#include "linear_ce.h"
+
+namespace mpx {
+
+hipError_t run_ce_out_pair_bf16(const CeOutArgs& w, RowTile tw, const CeOutArgs& x, RowTile tx, hipStream_t s) {
+  return launch_ce_out_pair<MPX_BF16>(w, tw, x, tx, s);
+}
+
+}  // namespace mpx
