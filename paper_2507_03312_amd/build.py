@@ -20,7 +20,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 SOURCES = ["gemm_f16.hip", "gemm_bf16.hip", "gemm_staged_f16.hip", "gemm_staged_bf16.hip",
            "gemm_wide_f16.hip", "gemm_wide_bf16.hip", "support.hip", "attention.hip", "sweep.hip",
            "gemm_act8_f16.hip", "gemm_act8_bf16.hip",
-           "gated_f16.hip", "gated_bf16.hip", "linear_ce_f16.hip", "linear_ce_bf16.hip", "linear_ce_pair_f16.hip", "linear_ce_pair_bf16.hip",
+           "gated_f16.hip", "gated_bf16.hip", "linear_ce_f16.hip", "linear_ce_bf16.hip",
+           "linear_ce_pair_f16.hip", "linear_ce_pair_bf16.hip",
            "gemm.hip", "gemm_f32.hip", "support_f32.hip", "act8.hip", "rope.hip", "logprob.hip",
            "gated.hip", "linear_ce.hip", "qknorm_rope.hip", "dropout.hip"]
 

@@ -107,7 +107,11 @@ __global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, c
     unit = n ? scale / (float)n : 0.0f;
     a = fabsf(unit);
   } else if (C16) {
-    for (int64_t i = threadIdx.x; i < M; i += 1024) a = fmaxf(a, targets[i] < 0 ? 0.0f : fabsf(g_loss[i] * scale));
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < M; i += 1024) {
+      const float g = fabsf(g_loss[i] * scale);
+      a = fmaxf(a, targets[i] < 0 ? 0.0f : g);
+    }
     most[threadIdx.x] = a;
     for (int h = 512; h >= 1; h /= 2) {
       __syncthreads();
@@ -151,8 +155,8 @@ struct CeReduce {
 
 // Both sums, VEC: 4 values a thread (n, stride and part allow 16 bytes).  Workgroups past
 // those: db[r] = half(alpha (sum over p of dbp[r][p], and of the rests of the rows whose
-// target is r)), one wave a row, its lanes in strides of 64 and then wave_sum (one lane
-// a row took 95 us for the rests of 509 rows of 1000 columns).
+// target is r)), one wave a row, or with rests a workgroup, in strides of 64 or 256 and then in
+// order (12616 x 16 x 224 f16 with gradient: the rests by a wave 133 us, by a workgroup 46).
 // G threads a value where there are few values and many splits, each every G-th split, then
 // added in order.
 template <int DT, bool VEC, int G>
@@ -210,16 +214,27 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(CeReduce a) {
       }
     }
   } else {
-    const int64_t row = ((int64_t)blockIdx.x - blocks) * 4 + (threadIdx.x >> 6);
-    if (row >= a.nrows) return;  // uniform over the wave
-    const int lane = threadIdx.x & 63;
+    __shared__ float waves[4];
+    const bool whole = a.rest != nullptr;  // uniform
+    const int wave = threadIdx.x >> 6, span = whole ? 256 : 64, first = threadIdx.x % span;
+    const int64_t row = ((int64_t)blockIdx.x - blocks) * (whole ? 1 : 4) + (whole ? 0 : wave);
+    if (row >= a.nrows) return;  // uniform over the wave, none with rests
     float s = 0.0f;
-    for (int k = lane; k < a.dbparts; k += 64) s += a.dbp[row * a.dbparts + k];
-    if (a.rest) {  // what rounding left of the targets that are this column
-      for (int r = lane; r < a.rows; r += 64) s += a.targets[r] == a.v0 + row ? a.rest[r] : 0.0f;
+    for (int k = first; k < a.dbparts; k += span) s += a.dbp[row * a.dbparts + k];
+    if (whole) {  // what rounding left of the targets that are this column
+#pragma unroll 8
+      for (int r = first; r < a.rows; r += 256) {
+        const float v = a.rest[r];
+        s += a.targets[r] == a.v0 + row ? v : 0.0f;
+      }
     }
     s = wave_sum(s);
-    if (lane == 0) {
+    if (whole) {
+      if ((threadIdx.x & 63) == 0) waves[wave] = s;
+      __syncthreads();
+      s = (waves[0] + waves[1]) + (waves[2] + waves[3]);
+    }
+    if (first == 0) {
       const uint16_t h = f2h<DT>(s * scale);
       a.db[row] = h;
       bad = h_nonfinite<DT>(h) ? 1 : 0;
@@ -552,7 +567,8 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
     const int64_t per = vec ? 4 : 1, n = sums.first.n + sums.second.n;
     const bool few = n / per <= 16384 && std::max(sums.first.splits, sums.second.splits) >= 16;
     const int64_t at = (few ? 32 : 256) * per;
-    const unsigned blocks = (unsigned)(cdiv(sums.first.n, at) + cdiv(sums.second.n, at) + cdiv(sums.nrows, 4));
+    const unsigned blocks = (unsigned)(cdiv(sums.first.n, at) + cdiv(sums.second.n, at) +
+                                       (rest ? sums.nrows : cdiv(sums.nrows, 4)));
     return by_type(dt, [&](auto type) {
       const auto kernel = vec ? (few ? ce_reduce_kernel<type, true, 8> : ce_reduce_kernel<type, true, 1>)
                               : (few ? ce_reduce_kernel<type, false, 8> : ce_reduce_kernel<type, false, 1>);
