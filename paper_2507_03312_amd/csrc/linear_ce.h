@@ -210,7 +210,7 @@ struct CeGradArgs : GemmArgs {
 
 // Backward, products of a piece: C = half(alpha acc), or (part set) float32 partial
 // sums per split, on top of an earlier piece's in the first `add` of them.  Of pieces of
-// 4096 x 16384 x 768 bf16 dX 110 us and dW 98 (0.94 and 1.05 PFLOP/s; the bare product 91).
+// 4096 x 16384 x 768 bf16 dX 110 us and dW 98 alone (0.94 and 1.05 PFLOP/s; the bare product 91).
 struct CeOutArgs : GemmArgs {
   static constexpr bool kPair = false, kRagged = true;
   static constexpr unsigned kTiles = bit(TILE_256x256);

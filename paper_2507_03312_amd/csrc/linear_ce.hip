@@ -73,6 +73,7 @@ __global__ __launch_bounds__(1024) void ce_mean_kernel(const float* loss, const 
   __shared__ int counts[1024];
   float s = 0.0f;
   int n = 0;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < M; i += 1024) {
     s += loss[i];
     n += targets[i] >= 0 ? 1 : 0;
@@ -102,6 +103,7 @@ __global__ __launch_bounds__(1024) void ce_prepare_kernel(const float* g_loss, c
   float a = 0.0f, unit = scale;
   if (!g_loss) {
     int n = 0;
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < M; i += 1024) n += targets[i] >= 0 ? 1 : 0;
     n = ce_sum1024(n, counts);
     unit = n ? scale / (float)n : 0.0f;
