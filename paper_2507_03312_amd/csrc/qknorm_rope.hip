@@ -275,9 +275,11 @@ void qknorm_rope_bwd_kernel(QkArgs a) {
   }
 }
 
-// Heads whose sections allow no such runs: a wave takes a head at a time, lane l the values
-// l, l + 64, ..., their partners straight from memory (the same lines).
-// PER: values of a lane.
+// Heads whose sections allow no such runs: a wave takes a head at a time, U heads in flight,
+// lane l the values l, l + 64, ..., their partners straight from memory (the same lines).
+// Bound by latency and narrow accesses: 6304 rows of 36 heads of 128 bf16, sections of 21 and
+// 43, 65 us, backward 92 (one head in flight 113 and 157; whole runs 30 and 52).  PER: values
+// of a lane.
 template <int DT, bool BACK, int PER>
 __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
   typedef typename RopeValue<DT>::type T;
@@ -290,7 +292,8 @@ __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
   // the lane's values' pairs (-1: not turned) and partners
   int pair[PER], other[PER];
   bool second[PER];
-  float dw[2][PER];
+  float dw[2][PER], gain[2][PER], gain_other[2][PER];
+  constexpr int U = PER <= 2 ? 4 : PER == 4 ? 2 : 1;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int j = lane + 64 * i;
@@ -318,6 +321,16 @@ __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
       }
     }
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool in = lane + 64 * i < a.hd;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const T* g = (const T*)(part ? a.wk : a.wq);
+      gain[part][i] = in && g ? get(g[lane + 64 * i]) : 1.0f;
+      gain_other[part][i] = in && g ? get(g[other[i]]) : 1.0f;
+    }
+  }
   for (uint32_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
     const uint32_t row0 = tile * a.wg_rows, nrows = min((uint32_t)a.wg_rows, a.rows - row0);
     const T* X = (const T*)a.X + (int64_t)row0 * a.ldx;
@@ -327,49 +340,62 @@ __global__ __launch_bounds__(256) void qknorm_rope_any_kernel(QkArgs a) {
     __syncthreads();
     rope_copies<DT>(a, D, ldd, Y, nrows);
     rope_turns(a, row0, nrows, turns);
-    for (uint32_t item = wave; item < nrows * a.heads_rot; item += 4) {
-      const uint32_t r = item / a.heads_rot, h = item % a.heads_rot;
-      const T* x = X + r * a.ldx + (int64_t)h * a.hd;
-      const T* d = D + r * ldd + (int64_t)h * a.hd;
-      T* y = Y + r * a.ldy + (int64_t)h * a.hd;
-      const int part = h >= a.hq ? 1 : 0;
-      const T* g = (const T*)(part ? a.wk : a.wq);
-      float xv[PER], own[PER], oth[PER], ss = 0.0f, sp = 0.0f;
+    const uint32_t items = nrows * a.heads_rot;
+    for (uint32_t item0 = wave; item0 < items; item0 += 4 * U) {
+      float xv[U][PER], own[U][PER], oth[U][PER];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int j = lane + 64 * i;
-        const bool in = j < a.hd;
-        xv[i] = in ? get(x[j]) : 0.0f;
-        const float w = in && g ? get(g[j]) : 1.0f, wo = in && g ? get(g[other[i]]) : 1.0f;
-        own[i] = in ? get(d[j]) : 0.0f;
-        oth[i] = in ? get(d[other[i]]) : 0.0f;
-        if (pair[i] >= 0) {
-          float2 t = turns[r * a.npairs + pair[i]];
-          if (!second[i]) t.y = -t.y;
-          own[i] = BACK ? __builtin_fmaf(own[i], t.x, oth[i] * t.y)
-                        : __builtin_fmaf(own[i], w * t.x, oth[i] * (wo * t.y));
-        } else if (!BACK) {
-          own[i] *= w;
-        }
-        ss = __builtin_fmaf(xv[i], xv[i], ss);
-        if (BACK) {
-          oth[i] = w * own[i];
-          sp = __builtin_fmaf(oth[i], xv[i], sp);
+      for (int u = 0; u < U; ++u) {
+        const uint32_t item = min(item0 + 4 * u, items - 1), r = item / a.heads_rot, h = item % a.heads_rot;
+        const T* x = X + r * a.ldx + (int64_t)h * a.hd;
+        const T* d = D + r * ldd + (int64_t)h * a.hd;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int j = lane + 64 * i;
+          const bool in = j < a.hd;
+          xv[u][i] = in ? get(x[j]) : 0.0f;
+          if constexpr (BACK) own[u][i] = in ? get(d[j]) : 0.0f;
+          else own[u][i] = xv[u][i];
+          oth[u][i] = in ? get(d[other[i]]) : 0.0f;
         }
       }
-      const float inv = rsqrtf(__builtin_fmaf(wave_sum(ss), over, a.eps));
-      const float k = BACK ? inv * inv * (wave_sum(sp) * over) : 0.0f;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int j = lane + 64 * i;
-        if (j >= a.hd) continue;
-        if (BACK) {
-          const float t = own[i] * (xv[i] * inv);
-          dw[0][i] += part ? 0.0f : t;
-          dw[1][i] += part ? t : 0.0f;
-          y[j] = put(inv * __builtin_fmaf(-xv[i], k, oth[i]));
-        } else {
-          y[j] = put(inv * own[i]);
+      for (int u = 0; u < U; ++u) {
+        const uint32_t item = item0 + 4 * u, r = item / a.heads_rot, h = item % a.heads_rot;
+        if (item >= items) break;  // uniform over the wave
+        const int part = h >= a.hq ? 1 : 0;
+        float ss = 0.0f, sp = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const float w = part ? gain[1][i] : gain[0][i], wo = part ? gain_other[1][i] : gain_other[0][i];
+          if (pair[i] >= 0) {
+            float2 t = turns[r * a.npairs + pair[i]];
+            if (!second[i]) t.y = -t.y;
+            own[u][i] = BACK ? __builtin_fmaf(own[u][i], t.x, oth[u][i] * t.y)
+                             : __builtin_fmaf(own[u][i], w * t.x, oth[u][i] * (wo * t.y));
+          } else if (!BACK) {
+            own[u][i] *= w;
+          }
+          ss = __builtin_fmaf(xv[u][i], xv[u][i], ss);
+          if (BACK) {
+            oth[u][i] = w * own[u][i];
+            sp = __builtin_fmaf(oth[u][i], xv[u][i], sp);
+          }
+        }
+        const float inv = rsqrtf(__builtin_fmaf(wave_sum(ss), over, a.eps));
+        const float k = BACK ? inv * inv * (wave_sum(sp) * over) : 0.0f;
+        T* y = Y + r * a.ldy + (int64_t)h * a.hd;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int j = lane + 64 * i;
+          if (j >= a.hd) continue;
+          if (BACK) {
+            const float t = own[u][i] * (xv[u][i] * inv);
+            dw[0][i] += part ? 0.0f : t;
+            dw[1][i] += part ? t : 0.0f;
+            y[j] = put(inv * __builtin_fmaf(-xv[u][i], k, oth[u][i]));
+          } else {
+            y[j] = put(inv * own[u][i]);
+          }
         }
       }
     }
@@ -524,10 +550,13 @@ static int qknorm_rope(const char* fn, const void* X, int64_t ldx, const void* d
   a.chunks = any ? 64 : (int32_t)(hd / vw);
   const int64_t slots = any ? 4 : 4 * (64 / a.chunks);
   const int64_t listed = a.heads_rot + (!any && !a.in_place && vw * (dt == MPX_F32 ? 4 : 2) == 16 ? heads_copy : 0);
-  int64_t wg_rows = std::min<int64_t>({8 * slots / listed, slots, kRopeTable / a.npairs, rows / 1024});
+  // a wave a head: forward small workgroups for whole rounds, backward one round of them
+  int64_t wg_rows = any ? (back ? std::min<int64_t>(16, cdiv(rows, kQkWorkgroups)) : std::min<int64_t>(2, rows / 1024))
+                        : std::min<int64_t>({8 * slots / listed, slots, rows / 1024});
+  wg_rows = std::min<int64_t>(wg_rows, kRopeTable / a.npairs);
   wg_rows = std::max<int64_t>(wg_rows, 1);
   a.wg_rows = (int32_t)wg_rows;
-  a.head_slots = (int32_t)(slots / wg_rows);
+  a.head_slots = (int32_t)std::max<int64_t>(1, slots / wg_rows);
   a.tiles = (uint32_t)cdiv(rows, wg_rows);
   const unsigned blocks = (unsigned)(back ? std::min<int64_t>(a.tiles, workgroups) : a.tiles);
 #define MPX_QK(DTv, VWv) launch_qk<DTv, VWv>(a, back, blocks, s)
