@@ -582,7 +582,7 @@ int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t 
  * negative, the row has no target (loss 0, no gradient); V or more gives NaN.  A bias
  * of -inf masks its column (probability 0, no gradient); a row of nothing but masked
  * ones has stats (-inf, 0) and loss inf.  A NaN or +inf logit makes its row's ln S and
- * loss NaN.  1 <= M <= 2^20, V <= 2^24, K <= 2^16, M V <= 2^36, (M + V) K <= 2^33;
+ * loss NaN (m, the largest of the others, too, if that would be -inf).  1 <= M <= 2^20, V <= 2^24, K <= 2^16, M V <= 2^36, (M + V) K <= 2^33;
  * dt MPX_F16 or MPX_BF16; X and W dense, all aligned to their element (stats 8 bytes).  Operands 16-byte aligned with K
  * a multiple of 64 go the fastest way.  workspace:
  * mpx_linear_ce_fwd_workspace(M, V, K) bytes, 16-byte aligned, not shared by calls

@@ -41,8 +41,10 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* part, const
     if (g < h) lds[g][r] = a = ce_join(a, lds[g + h][r]);
   }
   if (g != 0 || row >= M) return;
-  const float ln = a.x == -__builtin_inff() ? 0.0f : logf(a.y);
-  if (stats) stats[row] = make_float2(a.x, ln);
+  // S is 0 where everything is masked and nowhere else.  m passes over NaN logits, S does not:
+  // beside nothing but them and masked ones m is no -inf, which would say all masked
+  const float ln = a.y == 0.0f ? 0.0f : logf(a.y);
+  if (stats) stats[row] = make_float2(ln != ln && a.x == -__builtin_inff() ? ln : a.x, ln);
   if (loss) {
     float l = 0.0f;
     if (t >= V) {
