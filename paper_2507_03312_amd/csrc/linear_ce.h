@@ -78,11 +78,13 @@ struct CeFwdArgs : GemmArgs {
         for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
       });
       m = fmaxf(m, other_half(m));
-      const float at = m == -__builtin_inff() ? 0.0f : m * kLog2e;  // nothing but masked ones: S = 0
+      const float at = m == -__builtin_inff() ? 0.0f : m;  // nothing but masked ones: S = 0
+      // m first, which is exact near it: the largest one's own term is 1 and ln S never below 0,
+      // while z log2 e - m log2 e in one rounding would leave m log2 e's (2^-24 m in ln S)
       float s = 0.0f;
       static_for<TN>([&](auto j) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, -at));
+        for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - at) * kLog2e);
       });
       s += other_half(s);
       if (hi == 0) rows[wc * BM + wr * WM + 32 * i + lane] = make_float2(m, s);
@@ -162,10 +164,10 @@ struct CeGradArgs : GemmArgs {
       const int64_t t = (int64_t)target - v0 - nw;
       const float f = row >= M || target < 0 ? 0.0f
                       : target >= vocabulary ? __builtin_nanf("") : early.g[i] * early.unit;
-      // f p = f 2^(z log2 e + c): a masked z gives 0, a NaN in ln or f a NaN row.  All
-      // masked (m = -inf): c = 0
-      const float c = row >= M ? -__builtin_inff()
-                      : st.x == -__builtin_inff() ? 0.0f : -__builtin_fmaf(st.x, kLog2e, st.y * kLog2e);
+      // f p = f 2^((z - m) log2 e + c), m first as in the forward (a certain target's p - 1 is never
+      // above 0): a masked z gives 0, a NaN in m, ln S or f a NaN row.  All masked: m = 0
+      const float at = st.x == -__builtin_inff() ? 0.0f : st.x;
+      const float c = row >= M ? -__builtin_inff() : -(st.y * kLog2e);
       const bool plain = nv == 64 && !__ballot(t >= 0 && t < 64);  // uniform: no target, no edge
       for (int low = 0; low <= (kExact && twice ? 1 : 0); ++low) {
         asm volatile("" ::: "memory");  // the wave's reads of the block before come first
@@ -176,13 +178,13 @@ struct CeGradArgs : GemmArgs {
             if (plain) {
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                p[k] = f * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + k], kLog2e, c));
+                p[k] = f * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + k] - at, kLog2e, c));
             } else {
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const int col = 32 * j + 8 * q + 4 * hi + k;
                 const float z = acc[i][j][4 * q + k];
-                p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, c));
+                p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z - at, kLog2e, c));
                 p[k] = f * (p[k] - (col == t && z != -__builtin_inff() ? 1.0f : 0.0f));
                 p[k] = col < nv ? p[k] : 0.0f;
                 if (kExact && rest && col == t && row < M) rest[row] = p[k] - h2f<DT>(f2h<DT>(p[k]));
