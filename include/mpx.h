@@ -585,7 +585,8 @@ int mpx_logprob_bwd(const void* Z, int64_t ldz, const int32_t* targets, int64_t 
  * loss NaN (m, the largest of the others, too, if that would be -inf).  1 <= M <= 2^20, V <= 2^24, K <= 2^16, M V <= 2^36, (M + V) K <= 2^33;
  * dt MPX_F16 or MPX_BF16; X and W dense, all aligned to their element (stats 8 bytes).  Operands 16-byte aligned with K
  * a multiple of 64 go the fastest way.  workspace:
- * mpx_linear_ce_fwd_workspace(M, V, K) bytes, 16-byte aligned, not shared by calls
+ * mpx_linear_ce_fwd_workspace(M, V, K) bytes, which never falls as M grows (so a buffer for
+ * the largest batch serves every smaller one), 16-byte aligned, not shared by calls
  * that overlap; results do not depend on what else runs (no atomics). */
 int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, const int32_t* targets, int64_t M,
                       int64_t V, int64_t K, float* loss, float* stats, float* d_mean, mpx_dtype dt,
@@ -602,8 +603,8 @@ size_t mpx_linear_ce_fwd_workspace(int64_t M, int64_t V, int64_t K);
  * sums over the pieces in float32.  Up to 128 rows, what that rounding leaves is kept as
  * well.  A row whose stats are NaN, or whose target is V
  * or more, makes its dX and all of dW NaN.  d_nonfinite (nullable) counts non-finite
- * dW and db elements.  workspace: mpx_linear_ce_bwd_workspace(M, V, K) bytes, 16-byte
- * aligned.  Sizes and types as the forward's; outputs overlap nothing. */
+ * dW and db elements.  workspace: mpx_linear_ce_bwd_workspace(M, V, K) bytes, which never
+ * falls as M grows, 16-byte aligned.  Sizes and types as the forward's; outputs overlap nothing. */
 int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, const int32_t* targets, int64_t M,
                       int64_t V, int64_t K, const float* stats, const float* g_loss,
                       const mpx_scale_state* d_state, void* dX, void* dW, void* db, mpx_dtype dt,

@@ -290,33 +290,40 @@ static const RowCost kDwCost[] = {{TILE_128x128, 128, 128, 2, {0.60, 0.77, 0}, 2
                                   {TILE_192x128, 192, 128, 2, {0.82, 1.04, 0}, 4.92},
                                   {TILE_256x256, 256, 256, 1, {1.29, 0, 0}, 13.3}};
 
+// The most rows that take 64 x 64 staged tiles: one row of tiles, or up to two tiles per CU.
+static int64_t ce_narrow_rows(int64_t N) { return std::max<int64_t>(64, 512 / cdiv(N, 64) * 64); }
+
 // Tile of a product of two k-major operands (forward and dz).  Staged ones of at most 64
 // rows: 11 x 51223 x 183 f16 dz 18.3 us by 128 x 128, 12.5 by 64 x 64.
 static RowTile ce_tile(int64_t M, int64_t N, int64_t K, bool dma, bool any, bool forward) {
   if (any) return STAGED_ANY;
-  if (!dma) return M <= 64 || cdiv(M, 64) * cdiv(N, 64) <= 512 ? STAGED_64 : STAGED_128;
+  if (!dma) return M <= ce_narrow_rows(N) ? STAGED_64 : STAGED_128;
   if (forward && M <= 32) return TILE_32x128;
   return choose_rows(forward ? kFwdCost : kGradCost, M, N, K).tile;
 }
 
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Forward workspace: (m, S) of every tile column, whatever the operands' alignment,
-// and the targets' logits.
-static int64_t ce_parts(int64_t M, int64_t V, int64_t K) {
-  return std::max(cdiv(V, tile_cols(ce_tile(M, V, K, true, false, true))),
-                  cdiv(V, tile_cols(ce_tile(M, V, K, false, K < 8, true))));
+// Forward workspace: (m, S) of every row and tile column, whatever the operands' alignment,
+// and the targets' logits.  Never less than fewer rows take, whose tiles may be narrower.
+static int64_t ce_pairs(int64_t M, int64_t V, int64_t K) {
+  const int64_t narrow = K < 8 ? M : std::min(M, ce_narrow_rows(V));
+  return std::max(cdiv(V, tile_cols(STAGED_64)) * narrow, cdiv(V, tile_cols(STAGED_128)) * M);
 }
 
 // Tile and splits of a piece's reductions over direct operands; at least 192 values a split,
-// none of them empty.  Register-staged ones take the splits and a tile of their own.
+// none of them empty.  Register-staged ones take the splits and a tile of their own.  At most
+// three rounds of the smallest tiles, which bounds the partial sums of any number of rows (of
+// 20000 drawn products of K <= 2048 it changes the splits of 0.06%).
+constexpr int64_t kDxGroups = 3 * 768, kDwGroups = 3 * 512;
 static RowChoice ce_dx(int64_t M, int64_t cols, int64_t K, bool parts) {
+  const int64_t most = std::min({(int64_t)64, cols / 192, kDxGroups / (cdiv(M, 64) * cdiv(K, 128))});
   // without partial sums a split also costs the kernel that adds them
-  return choose_rows(kDxCost, M, K, cols, std::max<int64_t>(1, std::min<int64_t>(64, cols / 192)), parts ? 0.0 : 3.0,
-                     1.25e-6, !parts);
+  return choose_rows(kDxCost, M, K, cols, std::max<int64_t>(1, most), parts ? 0.0 : 3.0, 1.25e-6, !parts);
 }
 static RowChoice ce_dw(int64_t M, int64_t cols, int64_t K) {
-  return choose_rows(kDwCost, cols, K, M, std::max<int64_t>(1, std::min<int64_t>(64, M / 192)), 2.0, 2.5e-6);
+  const int64_t most = std::min({(int64_t)64, M / 192, kDwGroups / (cdiv(cols, 128) * cdiv(K, 128))});
+  return choose_rows(kDwCost, cols, K, M, std::max<int64_t>(1, most), 2.0, 2.5e-6);
 }
 
 // Operands whose reduction is no multiple of 64 go to the direct tiles as padded copies
@@ -336,8 +343,15 @@ struct CePlan {
   bool dx_parts, rest;
   int64_t twice, rows;  // rows between dz and what its rounding left (0: not kept), of all
   int64_t width;  // of dX's and dW's partial sums: K, or of padded operands a multiple of 4
-  size_t lo, dz, dxp, dwp, dbp, x2, total;  // workspace offsets, scalars first; x2: other forms of X (and W)
+  size_t lo, dz, dxp, dwp, dbp, x2;  // workspace offsets, scalars first; x2: other forms of X (and W)
 };
+
+// Rows of dz that what its rounding left is kept for, in as many rows more: 32, 64 or 128 of each
+// (20 x 63884 x 256 bf16 of 64 each 72 us, of 32 62).  Up to 128 rows dX's norm would lose up to
+// a factor of 1.8 to the rounding of dz, with 256 1.45; db's, of few columns, of up to a
+// thousand rows 2: there, up to kCeRest logits, what the targets' dz left.
+static int64_t ce_twice(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 0; }
+constexpr int64_t kCeRest = (int64_t)1 << 22, kCeDz = (int64_t)64 << 20;  // kCeDz: values of a piece's dz
 
 static int64_t split_len(int64_t len, int splits) { return cdiv(cdiv(len, splits), 64) * 64; }
 // splits of that length that cover len: none is empty
@@ -349,14 +363,11 @@ static int split_count(int64_t len, int splits) { return (int)cdiv(len, split_le
 // time of 3 of 64 and one of 65).
 static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   CePlan p{};
-  // 32, 64 or 128 rows of each (20 x 63884 x 256 bf16 of 64 each 72 us, of 32 62): up to
-  // 128 rows dX's norm would lose up to a factor of 1.8 to the rounding of dz, with
-  // 256 1.45; db's, of few columns, of up to a thousand rows 2
-  p.twice = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 0;
-  p.rest = !p.twice && M * V <= ((int64_t)1 << 22);
+  p.twice = ce_twice(M);
+  p.rest = !p.twice && M * V <= kCeRest;
   p.width = ce_pads_bwd(M, K) ? cdiv(K, 4) * 4 : K;
   const int64_t rows = p.rows = p.twice ? 2 * p.twice : cdiv(M, 64) * 64, Mr = p.twice ? p.rows : M;
-  const int64_t most = std::max<int64_t>(256, ((int64_t)128 << 20) / (2 * rows) / 256 * 256);
+  const int64_t most = std::max<int64_t>(256, kCeDz / rows / 256 * 256);
   const auto lay = [&](int64_t cols) {  // what is left after whole pieces: its own, or with the last
     p.cols = cols;
     p.pieces = std::max<int64_t>(1, cdiv(V - 256, cols));
@@ -396,9 +407,27 @@ static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
   p.dwp = p.dxp + (p.dx_parts ? align256((size_t)p.dx_splits * Mr * p.width * 4) : 0);
   p.dbp = p.dwp + align256(dw);
   p.x2 = p.dbp + align256(db);
-  p.total = p.x2 + align256((size_t)2 * p.twice * cdiv(K, 8) * 8 * 2) +
-            (ce_pads_bwd(M, K) ? align256((size_t)(M + V) * ce_padded(K) * 2) : 0);
   return p;
+}
+
+// A workspace that holds the plan of any number of rows up to M, part by part the largest:
+// few rows take two sets, wide pieces and many splits, many rows the most of the others.
+static size_t ce_bwd_bytes(int64_t M, int64_t V, int64_t K) {
+  const int64_t twice = M > 128 ? 128 : ce_twice(M), width = cdiv(K, 4) * 4, tiles = cdiv(K, 128);
+  const int64_t rows = std::max(2 * twice, M > 128 ? cdiv(M, 64) * 64 : 0), Mr = std::max(2 * twice, M);
+  const int64_t most_cols = std::min(V, kCeDz / 64 + 256);  // of a piece, of the fewest rows
+  // a piece's columns times rows: kCeDz or 256 columns, and up to 256 columns more
+  const int64_t dz = std::min(rows * cdiv(V, 64) * 64, std::max(kCeDz, rows * 256) + rows * 256);
+  const int64_t dx_splits = std::max<int64_t>(1, std::min<int64_t>(64, V / 192));
+  const int64_t dx = std::max(Mr * width, std::min(dx_splits * Mr * width, kDxGroups * 64 / tiles * width));
+  const int64_t dw_splits = Mr / 192;
+  const int64_t dw = dw_splits < 2 ? 0 : std::min(dw_splits * V * width, kDwGroups * 128 / tiles * width);
+  // a split's column of sums for each 64 of K, two in a tile
+  const int64_t db = std::max(std::max<int64_t>(4, cdiv(K, 64)) * most_cols, dw ? kDwGroups * 128 * 2 : 0);
+  const size_t x2 = align256((size_t)2 * twice * cdiv(K, 8) * 8 * 2);
+  return 256 + (M > 128 ? align256((size_t)std::min(M, kCeRest / V) * 4) : 0) + align256((size_t)dz * 2) +
+         align256((size_t)dx * 4) + align256((size_t)dw * 4) + align256((size_t)db * 4) +
+         std::max(x2, ce_pads_bwd(M, K) ? align256((size_t)(M + V) * ce_padded(K) * 2) : 0);
 }
 
 static GemmArgs ce_args(const void* A, const void* B, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb) {
@@ -454,7 +483,7 @@ using namespace mpx;
 
 extern "C" size_t mpx_linear_ce_fwd_workspace(int64_t M, int64_t V, int64_t K) {
   if (M < 1 || V < 1 || K < 1) return 0;
-  return align256((size_t)ce_parts(M, V, K) * M * 8) + align256((size_t)M * 4) +
+  return align256((size_t)ce_pairs(M, V, K) * 8) + align256((size_t)M * 4) +
          (ce_pads_fwd(M, V, K) ? align256((size_t)(M + V) * ce_padded(K) * 2) : 0);
 }
 
@@ -478,7 +507,7 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
   static_cast<GemmArgs&>(g) = ce_args(X, W, M, V, K, K, K);
   g.bias = (const uint16_t*)b;
   g.part = (float2*)workspace;
-  g.zt = (float*)((char*)workspace + align256((size_t)ce_parts(M, V, K) * M * 8));
+  g.zt = (float*)((char*)workspace + align256((size_t)ce_pairs(M, V, K) * 8));
   g.targets = loss ? targets : nullptr;
   if (ce_pads_fwd(M, V, K)) MPX_HIP(ce_pad(X, M, W, V, K, (uint16_t*)(g.zt + align256((size_t)M * 4) / 4), g, s));
   const RowTile t = ce_tile(M, V, g.K, dma_ok(g, operands_aligned(g), true, true), false, true);
@@ -505,7 +534,7 @@ extern "C" int mpx_linear_ce_fwd(const void* X, const void* W, const void* b, co
 
 extern "C" size_t mpx_linear_ce_bwd_workspace(int64_t M, int64_t V, int64_t K) {
   if (M < 1 || V < 1 || K < 1) return 0;
-  return ce_plan(M, V, K).total;
+  return ce_bwd_bytes(M, V, K);
 }
 
 extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, const int32_t* targets, int64_t M,
@@ -519,11 +548,12 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
   MPX_REQUIRE(!ce_misaligned(stats, 8) && !ce_misaligned(g_loss, 4) && !ce_misaligned(d_state, 4) &&
                   !ce_misaligned(dX, 2) && !ce_misaligned(dW, 2) && !ce_misaligned(db, 2),
               "pointers must be aligned to their element (stats to 8 bytes)");
-  const CePlan p = ce_plan(M, V, K);
-  if (!workspace || ws_bytes < p.total || ce_misaligned(workspace, 16)) {
-    set_error("mpx_linear_ce_bwd: workspace of " + std::to_string(p.total) + " bytes, 16-byte aligned, required");
+  const size_t need = mpx_linear_ce_bwd_workspace(M, V, K);
+  if (!workspace || ws_bytes < need || ce_misaligned(workspace, 16)) {
+    set_error("mpx_linear_ce_bwd: workspace of " + std::to_string(need) + " bytes, 16-byte aligned, required");
     return MPX_ERR_WORKSPACE;
   }
+  const CePlan p = ce_plan(M, V, K);
   hipStream_t s = (hipStream_t)stream;
   char* ws = (char*)workspace;
   float* scalars = (float*)ws;
