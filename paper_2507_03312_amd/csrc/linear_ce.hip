@@ -357,8 +357,9 @@ static int64_t split_len(int64_t len, int splits) { return cdiv(cdiv(len, splits
 // splits of that length that cover len: none is empty
 static int split_count(int64_t len, int splits) { return (int)cdiv(len, split_len(len, splits)); }
 
-// dz takes at most 128 MiB (so that its readers find much of it in the last-level cache),
-// or 256 columns.  Among the column counts that allow: the one of least estimated time
+// dz takes at most 128 MiB (so that its readers find much of it in the last-level cache), or
+// 256 columns; the only or last piece up to 256 columns more, so that none is narrow (65536
+// rows: 160 MiB at most, 2^20: 1 GiB).  Among the column counts that allow: the one of least estimated time
 // (whole rounds of tiles: 4096 x 65537 in 5 equal pieces of 52 tile columns 1.10 of the
 // time of 3 of 64 and one of 65).
 static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {

@@ -23,3 +23,15 @@ def test_workspaces_never_fall_as_rows_grow(V, K):
         sizes = [f(m, V, K) for m in rows]
         falls = [(a, b) for a, b, x, y in zip(rows, rows[1:], sizes, sizes[1:]) if y < x]
         assert not falls, (f.__name__, falls[:3])
+
+
+@pytest.mark.parametrize("M, V, K", [(128, 131072, 768), (4096, 131072, 768), (65536, 65536, 768), (65536, 1280, 64),
+                                     (1 << 20, 65536, 64), (1 << 20, 512, 64)])
+def test_a_piece_is_what_the_workspace_holds_of_the_logits(M, V, K):
+    """dz of 128 MiB or 256 columns, 256 columns more in the last piece; beside it dX's sums
+    (float32) and the bounded ones of splits."""
+    from paper_2507_03312_amd import binding as mx
+    rows = max(M, 256)   # up to 128 rows two sets of them
+    columns = max((64 << 20) // rows, 256) + 256
+    splits = 4 * (3 * 768 * 64 + 3 * 512 * 128) * 128 + (64 << 20)   # of dX and dW; db's
+    assert mx.mpx_linear_ce_bwd_workspace(M, V, K) <= 2 * rows * min(V, columns) + 4 * rows * K + splits + (1 << 20)
