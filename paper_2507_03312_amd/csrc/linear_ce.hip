@@ -247,16 +247,22 @@ __global__ __launch_bounds__(256) void ce_reduce_kernel(CeReduce a) {
   if (count) add_nonfinite(count, bad);
 }
 
-// db of a piece where dW is not asked for: partial sums dbp[column][4] for the reduction,
-// four groups of rows a workgroup, 64 columns.
+// db of a piece where dW is not asked for: partial sums dbp[column][part] for the reduction,
+// four groups of kColsumRows rows a workgroup, 64 columns.  Equal dz (a uniform softmax's) round
+// every step of a chain the same way: in chains of 2^18 float16's lost 2^-8.5, ones of
+// kColsumRows / 4 are exact for it (and spread the rows: 12616 x 16 x 224 f16 db alone 771 us with
+// chains of all rows, 40 so).
+constexpr int64_t kColsumRows = 256;
+static int64_t ce_colsum_parts(int64_t rows) { return 4 * cdiv(rows, kColsumRows); }
 template <int DT>
 __global__ __launch_bounds__(256) void ce_colsum_kernel(const uint16_t* dz, int64_t ld, int64_t M, int64_t cols,
                                                         float* dbp) {
   const int g = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);  // < ld, a multiple of 64
+  const int64_t m0 = blockIdx.y * kColsumRows, end = min(M, m0 + kColsumRows);
   float s = 0.0f;
-  for (int64_t m = g; m < M; m += 4) s += h2f<DT>(dz[m * ld + c]);
-  if (c < cols) dbp[c * 4 + g] = s;
+  for (int64_t m = m0 + g; m < end; m += 4) s += h2f<DT>(dz[m * ld + c]);
+  if (c < cols) dbp[(c * gridDim.y + blockIdx.y) * 4 + g] = s;
 }
 
 // Rows of X [M, K] and then of W [V, K] with zeros behind them, up to ld values (a multiple
@@ -399,7 +405,7 @@ static CePlan ce_plan(int64_t M, int64_t V, int64_t K) {
     p.dx_splits = std::max(p.dx_splits, split_count(cols, ce_dx(Mr, cols, K, p.pieces > 1 || p.twice > 0).splits));
     const int s = split_count(Mr, ce_dw(Mr, cols, K).splits);
     dw = std::max(dw, s > 1 ? (size_t)s * cols * p.width * 4 : 0);
-    db = std::max(db, (size_t)std::max<int64_t>(4, s * cdiv(K, 64)) * cols * 4);
+    db = std::max(db, (size_t)std::max(ce_colsum_parts(rows), s * cdiv(K, 64)) * cols * 4);
   }
   p.dx_parts = p.twice > 0 || p.dx_parts || p.dx_splits > 1;
   p.lo = 256;
@@ -423,8 +429,9 @@ static size_t ce_bwd_bytes(int64_t M, int64_t V, int64_t K) {
   const int64_t dx = std::max(Mr * width, std::min(dx_splits * Mr * width, kDxGroups * 64 / tiles * width));
   const int64_t dw_splits = Mr / 192;
   const int64_t dw = dw_splits < 2 ? 0 : std::min(dw_splits * V * width, kDwGroups * 128 / tiles * width);
-  // a split's column of sums for each 64 of K, two in a tile
-  const int64_t db = std::max(std::max<int64_t>(4, cdiv(K, 64)) * most_cols, dw ? kDwGroups * 128 * 2 : 0);
+  // a split's column of sums for each 64 of K, two in a tile; or four for every kColsumRows rows of dz
+  const int64_t db = std::max({cdiv(K, 64) * most_cols, dw ? kDwGroups * 128 * 2 : 0,
+                               4 * (most_cols + dz / kColsumRows)});
   const size_t x2 = align256((size_t)2 * twice * cdiv(K, 8) * 8 * 2);
   return 256 + (M > 128 ? align256((size_t)std::min(M, kCeRest / V) * 4) : 0) + align256((size_t)dz * 2) +
          align256((size_t)dx * 4) + align256((size_t)dw * 4) + align256((size_t)db * 4) +
@@ -677,9 +684,10 @@ extern "C" int mpx_linear_ce_bwd(const void* X, const void* W, const void* b, co
       if (w.part) sums.first = {w.part, cols * p.width, cols * p.width, w.splits, w.C, d_nonfinite};
     } else if (db) {
       sums.dbp = (float*)(ws + p.dbp);
-      sums.dbparts = 4;
+      sums.dbparts = (int)ce_colsum_parts(p.rows);
       MPX_HIP(by_type(dt, [&](auto type) {
-        ce_colsum_kernel<type><<<(unsigned)(ldz / 64), 256, 0, s>>>(dz, ldz, p.rows, cols, (float*)(ws + p.dbp));
+        const dim3 grid((unsigned)(ldz / 64), (unsigned)cdiv(p.rows, kColsumRows));
+        ce_colsum_kernel<type><<<grid, 256, 0, s>>>(dz, ldz, p.rows, cols, (float*)(ws + p.dbp));
         return hipGetLastError();
       }));
     }
