@@ -247,7 +247,8 @@ int mpx_linear_bwd_noalloc(const void* X, const void* W, const void* dY, const v
  *   H [M, N]    = half(act(g) u)       (one rounding)
  *   Pre [M, 2N] = [half(g) | half(u)]  (nullable: what the backward pass needs)
  * act: MPX_ACT_SILU (x / (1 + e^-x)) or MPX_ACT_GELU_TANH.  All dense, row-major,
- * pointers aligned to their element; H and Pre overlap nothing.  1 <= M < 2^31, 1 <= N, K <= 2^24.  The down
+ * pointers aligned to their element; H and Pre overlap nothing.  1 <= M < 2^31, 1 <= N, K <= 2^24,
+ * M N up to about 2^36 (the tiles' threads fit 32 bits).  The down
  * projection is mpx_linear_fwd on H (with the block's residual).  Up to 32 rows
  * (single tokens of some sequences) take a kernel that reads W once.  dt ==
  * MPX_F32: full precision; Pre is then required (the sums are left there). */

@@ -153,7 +153,7 @@ static bool misaligned(const void* p, mpx_dtype dt) {
 
 using namespace mpx;
 
-// sizes past these would not fit a launch's 2^31 tiles, or an element count 63 bits
+// sizes past these would not fit an element count's 63 bits (tiles_fit: a launch)
 static constexpr int64_t kMostRows = (int64_t)1 << 31, kMostCols = (int64_t)1 << 24;
 
 extern "C" int mpx_gated_fwd(const void* X, const void* W, const void* b, void* H, void* Pre, int64_t M,
@@ -184,6 +184,7 @@ extern "C" int mpx_gated_fwd(const void* X, const void* W, const void* b, void* 
     return MPX_OK;
   }
   const RowTile t = gated_tile(g, true);
+  MPX_REQUIRE(tiles_fit(t, M, 2 * N), "too large");
   MPX_HIP(dt == MPX_F16 ? run_gated_fwd_f16(g, N * K, t, s) : run_gated_fwd_bf16(g, N * K, t, s));
   return MPX_OK;
 }
@@ -225,6 +226,7 @@ extern "C" int mpx_linear_bwd_gated(const void* X, const void* W, const void* dY
       GemmArgs g = gated_args(dY, W, dPre, M, K, N, K, 2 * K, act);
       g.dact = (const uint16_t*)Pre;
       const RowTile t = gated_tile(g, false);
+      MPX_REQUIRE(tiles_fit(t, M, K), "too large");
       MPX_HIP(dt == MPX_F16 ? run_gated_bwd_f16(g, t, s) : run_gated_bwd_bf16(g, t, s));
     }
   }

@@ -109,6 +109,15 @@ constexpr unsigned bit(RowTile t) { return 1u << t; }
 constexpr int tile_cols(RowTile t) {
   return t == TILE_256x256 ? 256 : t == STAGED_64 || t == STAGED_ANY ? 64 : 128;
 }
+constexpr int tile_rows(RowTile t) {
+  return t == TILE_32x128 ? 32 : t == TILE_192x128 ? 192 : t == TILE_256x256 ? 256
+         : t == TILE_128x128 || t == STAGED_128 ? 128 : 64;
+}
+// Whether the threads of a launch of these tiles fit its 32 bits.
+constexpr bool tiles_fit(RowTile t, int64_t M, int64_t cols) {
+  const int64_t threads = t == STAGED_64 || t == STAGED_ANY ? 128 : t == TILE_256x256 ? 512 : 256;
+  return cdiv(M, tile_rows(t)) * cdiv(cols, tile_cols(t)) < ((int64_t)1 << 32) / threads;
+}
 
 // Direct-to-LDS tiles by estimated time: a chip of 256 CUs runs 256 x per_cu workgroups at
 // a time; a round of o per CU takes its k tiles of 64 x k_us[o - 1] plus o x tile_us for what
