@@ -600,9 +600,10 @@ size_t mpx_linear_ce_fwd_workspace(int64_t M, int64_t V, int64_t K);
  *   dX [M, K] = half(dz W);  dW [V, K] = half(dz^T X);  db [V] = half(sum_r dz)
  * (d_state NULL: 1; any subset, the others NULL).  The logits are computed again, in
  * pieces of the vocabulary: a piece's dz is held in the half type in the workspace
- * (float16: scaled by a power of two that keeps small probabilities, and back), dX's
- * sums over the pieces in float32.  Up to 128 rows, what that rounding leaves is kept as
- * well.  A row whose stats are NaN, or whose target is V
+ * (float16: scaled by a power of two, and back; one for all rows: g p from 2^-28 of the
+ * largest |g| on has all its bits, so a row of a much smaller |g| loses those of its
+ * small probabilities), dX's sums over the pieces in float32.  Up to 128 rows, what that
+ * rounding leaves is kept as well.  A row whose stats are NaN, or whose target is V
  * or more, makes its dX and all of dW NaN.  d_nonfinite (nullable) counts non-finite
  * dW and db elements.  workspace: mpx_linear_ce_bwd_workspace(M, V, K) bytes, which never
  * falls as M grows, 16-byte aligned.  Sizes and types as the forward's; outputs overlap nothing. */

@@ -34,8 +34,9 @@ __device__ __forceinline__ void gate_act_grad(float x, float& a, float& d) {
 
 // Forward: operand B is the pair of W's gate and other rows, so a wave's two
 // accumulator columns are G and U of the same 32 columns of H.  The matrix units and the
-// stores behind them share the time: 12608 x 2048 x 768 bf16 with Pre 107 us, 0.74 PFLOP/s
-// (the bare product of 4096 columns 91); 8320 x 1024 x 384 f16 26 us, 59 MB.  Rounded before they pass LDS, at half its traffic: 112 -> 107.
+// stores behind them share the time: 12608 x 2048 x 768 bf16 with Pre 97 to 112 us, 0.73 PFLOP/s
+// (the bare product of 4096 columns 91), without it 85; 8320 x 1024 x 384 f16 28 us, 59 MB, without
+// 23.5.  Rounded before they pass LDS, at half its traffic: the first 5 us less.
 template <int ACT>
 struct GatedArgs : GemmArgs {  // C = H, pre = [G | U] or NULL, bias [2 N] or NULL
   static constexpr bool kPair = true, kRagged = false;
@@ -99,8 +100,9 @@ struct GatedArgs : GemmArgs {  // C = H, pre = [G | U] or NULL, bias [2 N] or NU
 };
 
 // Backward: an ordinary dX product, whose float32 results meet G and U in the row
-// layout (dact = [G | U], C = [dG | dU], rows of 2 N).  12608 x 2048 x 768 bf16 75 us, of
-// which the bare product 44; the 207 MB of G, U and their gradients take the rest.
+// layout (dact = [G | U], C = [dG | dU], rows of 2 N).  12608 x 2048 x 768 bf16 85 to 93 us,
+// the matrix units busy 19% of them; repeated on one set of operands (in the last-level cache) 75
+// to 78, of which the bare product 44.  The 207 MB of G, U and their gradients take the rest.
 template <int ACT>
 struct GatedBwdArgs : GemmArgs {
   static constexpr bool kPair = false, kRagged = false;
@@ -119,7 +121,7 @@ struct GatedBwdArgs : GemmArgs {
     float* lds = reinterpret_cast<float*>(smem + wave * kRowsBytes);
     static_for<TM>([&](auto i) {
       // all in flight before the first is used.  (Loaded ahead of the main loop they cost
-      // more than they hide: 12608 x 2048 x 768 74.5 -> 77.9 us, 8320 x 1024 x 384 21.5 -> 23.6)
+      // more than they hide: 12608 x 2048 x 768, one set, 74.5 -> 77.9 us, 8320 x 1024 x 384 21.5 -> 23.6)
       u32x4 gw[4], uw[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {

@@ -21,9 +21,9 @@ __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32);
 
 // Forward.  A = X, B = W; lane l of a 32 x 32 block has row l % 32 and 16 of its 32
 // columns, so a row's maximum and sum take one exchange beside the lane's own values.
-// The matrix units bound the large ones: 4096 x 65537 x 768 bf16 412 us, 1.00 PFLOP/s (the
-// exponentials of 2.7e8 logits, two values an instruction pair, are what keeps it off
-// the 387 us of the bare product); W's 201 MB the few rows: 2 x 131072 x 768 42 us, 4.8 TB/s.
+// The matrix units bound the large ones: 4096 x 65537 x 768 bf16 400 to 416 us, 0.99 to 1.03 PFLOP/s
+// (the exponentials of 2.7e8 logits are what keeps it off the 387 us of the bare
+// product); W's 201 MB the few rows: 2 x 131072 x 768 42 us, 4.8 TB/s.
 struct CeFwdArgs : GemmArgs {
   static constexpr bool kPair = false, kRagged = false;
   static constexpr unsigned kTiles = bit(TILE_32x128) | bit(TILE_256x256);
@@ -105,8 +105,8 @@ struct CeFwdArgs : GemmArgs {
   }
 };
 
-// Backward, dz of a piece (bound as the forward: 4096 x 16384 x 768 bf16 118 us, 0.87 PFLOP/s,
-// the 128 MiB of dz go out while it runs): the same product, C = dz [M rounded up to 64][ldc], with
+// Backward, dz of a piece (bound as the forward: 4096 x 15872 x 768 bf16 115 us, 0.87 PFLOP/s,
+// the 130 MB of dz go out while it runs): the same product, C = dz [M rounded up to 64][ldc], with
 // zeros in rows behind M and columns behind N (up to ldc), as the products that reduce
 // over them need.  A masked logit (-inf) has no gradient, but in a row that is NaN.
 // twice (few rows): row twice + r holds what rounding row r to half left, and the products

@@ -186,8 +186,9 @@ __global__ __launch_bounds__(256) void qknorm_rope_kernel(QkArgs a) {
 // Backward, likewise, over a grid that strides over the rows.  A thread's sums of dw for its
 // run of values stand in LDS (their 16 registers serve the loads in flight); a workgroup
 // adds up its threads' in order, and qk_gains_kernel the workgroups'.  Bound by HBM as well:
-// 29997 rows of 16 + 4 heads and 4 copied ones of 128 f16 117 us, 4.5 TB/s (sums in registers,
-// no loads ahead: 185).
+// 29997 rows of 16 + 4 heads and 4 copied ones of 128 f16 113 to 119 us, 4.5 TB/s (sums in
+// registers, no loads ahead: 185).  At four waves a SIMD four of the variants of 8 values
+// (halves within the caches and, of bf16, past them; f16 interleaved within) spill 2 or 3 registers.
 template <int DT, int VW, bool INTER, bool NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void qknorm_rope_bwd_kernel(QkArgs a) {
